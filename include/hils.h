@@ -108,7 +108,16 @@ typedef enum {
  * fp32 path, decode and the backward. */
 #define HILS_FLAG_UNION_PACKING 8u
 
-typedef enum { HILS_OP_PREFILL = 0, HILS_OP_DECODE = 1, HILS_OP_BWD = 2, HILS_OP_LANDMARK = 3 } hils_op;
+typedef enum {
+    HILS_OP_PREFILL = 0,
+    HILS_OP_DECODE = 1,
+    HILS_OP_BWD = 2,
+    HILS_OP_LANDMARK = 3,
+    HILS_OP_DECODE_Q8 = 4,
+    HILS_OP_Q8_APPEND = 5,
+    HILS_OP_Q8_LANDMARK = 6,
+    HILS_OP_CACHE_EVICT = 7
+} hils_op;
 
 typedef struct {
     int B;          /* sequences */
@@ -281,6 +290,96 @@ int hils_landmark_fwd(const hils_params* p, const void* lq, const void* k, void*
 int hils_landmark_bwd(const hils_params* p, const void* lq, const void* k, const void* dlmk,
                       const float* dlmk_bias, void* dlq, void* dk, void* workspace, size_t ws_bytes,
                       void* stream);
+
+/*
+ * The 8-bit cache.  A page holds one chunk (S tokens) of one sequence for every KV
+ * head and landmark head, as 8-bit floats (e4m3: 4 exponent bits, 3 mantissa bits,
+ * largest finite value 448, no infinities):
+ *   k_pages   [num_pages, Hkv, S, d]   a stored x stands for x * kv_scale[page, g, 0]
+ *   v_pages   [num_pages, Hkv, d, S]   dim-major; x stands for x * kv_scale[page, g, 1]
+ *   kv_scale  [num_pages, Hkv, 2] f32
+ *   lmk_pages [num_pages, Hl, d]       landmark k'_c of the page's chunk, x stands for
+ *                                      x * kv_scale[page, g, 0], g the head's KV group
+ *   bias_pages [num_pages, Hl] f32     landmark bias b'_c
+ * and chunk c of sequence b is page block_table[b, c] ([B, L/S] int32, device; an
+ * entry outside [0, num_pages) is clamped into it; entries of chunks at or past a
+ * sequence's length are not read).  k_pages, v_pages and lmk_pages are 16-byte
+ * aligned, kv_scale 8-byte aligned.
+ *
+ * hils_q8_append writes new tokens' keys and values: sequence b appends the first
+ * newlens[b] rows of k_new and v_new ([B, Hkv, N, d], dtype; newlens [B] int32, NULL: N
+ * each; clamped into [0, N] and to the length) at positions len - newlens[b] .. len - 1,
+ * where len = seqlens[b] counts the new tokens (NULL: L; clamped into [0, L]).  Per page,
+ * KV head and K or V, with a the largest finite magnitude among the chunk's new values:
+ * the scale is the smallest power of two 2^e, e >= -100, with a <= 448 * 2^e, or, where
+ * the chunk holds older tokens, the scale it has if that is larger.  New values are
+ * divided by the scale and rounded to nearest, ties to even; infinities and NaN are
+ * stored as NaN.  Where the scale of a page in use grows, its older values are rounded
+ * to it (exactly, between powers of two, but for values below 2^-6 times the new scale).
+ * Bytes of tokens at or past len are left as they were.  Chunks that hold older tokens
+ * must be a sequence's own (copy a shared page before appending to it); two sequences
+ * of a call that append to one page give meaningless values in it.  Uses B, Hq, Hkv,
+ * N, L, d, chunk and dtype of `p`.
+ */
+int hils_q8_append(const hils_params* p, const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                   float* kv_scale, const int32_t* block_table, int num_pages, const int32_t* seqlens,
+                   const int32_t* newlens, void* stream);
+
+/*
+ * Landmark compression (hils_landmark_fwd) over the 8-bit cache: the landmark rows and
+ * biases of the chunks that the last newlens[b] tokens completed, from the stored keys
+ * (the ones that attention will see).  Chunks that are still incomplete, and pages of
+ * other chunks, are left as they were.
+ *   lq  [B, Hl, C, d], C = (N + S - 1) / S (the most chunks that N tokens complete):
+ *       entry j is the landmark query of the j-th chunk that this call completes; or
+ *       [Hl, d] under HILS_FLAG_SHARED_LMK_QUERY
+ * The rows are stored in units of the page's K scale, rounded to nearest.  seqlens and
+ * newlens as for hils_q8_append, to be called after it.  Uses scale and dtype (of lq) too.
+ */
+int hils_q8_landmark_fwd(const hils_params* p, const void* lq, const void* k_pages, const float* kv_scale,
+                         const int32_t* block_table, int num_pages, const int32_t* seqlens, const int32_t* newlens,
+                         void* lmk_pages, float* bias_pages, void* stream);
+
+/*
+ * Decode forward over the 8-bit cache: hils_decode_paged_fwd (arguments, positions,
+ * limits) on the values that the pages stand for; q, q_route and out are of `dtype`
+ * (float32 or bf16), products and sums in float32.  bias_pages NULL: b' = 0.
+ *   weights  [B, Hkv, N, K + P] f32, P = (window + 62) / 64 + 1, written unless NULL: the
+ *            attention weight of each part of a row, summed over the group's heads: of
+ *            the selected chunks (slot k as in idx; 0 for -1 entries) and of the window's
+ *            pieces (entry K + j: chunk |C_i| + j; 0 past the query's position).  A row's
+ *            weights add up to Hq / Hkv.
+ * Every position's own token must have been appended, the landmarks of every candidate
+ * chunk written.  HILS_FLAG_HEAD_NORM_SELECT returns HILS_ERR_UNSUPPORTED.  The
+ * workspace is hils_workspace_size(p, HILS_OP_DECODE_Q8); calls that may overlap (other
+ * streams, captured graphs replayed side by side) need one each.
+ */
+int hils_decode_q8_fwd(const hils_params* p, const void* q, const void* k_pages, const void* v_pages,
+                       const float* kv_scale, const void* lmk_pages, const float* bias_pages, const void* q_route,
+                       const int32_t* block_table, int num_pages, const int32_t* seqlens, void* out, float* lse,
+                       int32_t* idx, float* weights, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Eviction from a paged cache (bf16, fp32 or 8-bit) by accumulated attention weight.
+ * With weights and idx of a decode call (same p; NULL weights: nothing to add), every
+ * chunk's total first takes what it received: acc[b, c] += sum over KV groups and new
+ * queries, in that order.  Then a sequence with more than `budget` candidate chunks
+ * (|C_i| of the last position, len - 1) loses the excess, at most max_evict: the chunks
+ * with the least totals among sink .. |C_i| - 1, ties to the lower index (NaN totals
+ * stay).  The rows of block_table and acc close up over them (their last entries become
+ * -1 and 0), the length falls by S per chunk, so that any decode entry point runs on
+ * the result: positions serve the chunk partition only (rotations are the caller's).
+ *   acc, acc_out         [B, L/S] f32       block_table, table_out [B, L/S] int32
+ *   seqlens, seqlens_out [B] int32 (seqlens NULL: L; values are clamped into [N, L])
+ *   freed  [B, max_evict] int32: the pages given up, in the order of their chunks, -1
+ *          past nfreed[b] (NULL if max_evict is 0)
+ *   nfreed [B] int32
+ * The outputs may be the inputs themselves (in place), but not overlap them otherwise.
+ * Uses B, Hkv, N, L, topk and window of `p`.  Deterministic.
+ */
+int hils_cache_evict(const hils_params* p, const float* acc, const int32_t* block_table, const int32_t* seqlens,
+                     const float* weights, const int32_t* idx, int budget, int sink, int max_evict, float* acc_out,
+                     int32_t* table_out, int32_t* seqlens_out, int32_t* freed, int32_t* nfreed, void* stream);
 
 /*
  * Prefill (bf16, chunk-major): the most bytes of per-slot records (the chunk

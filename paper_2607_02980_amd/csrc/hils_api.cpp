@@ -48,7 +48,7 @@ int ok() {
 
 int check_params(const hils_params* p, int op) {
     if (!p) return fail(HILS_ERR_INVALID, "params is NULL");
-    if (op != HILS_OP_PREFILL && op != HILS_OP_DECODE && op != HILS_OP_BWD && op != HILS_OP_LANDMARK)
+    if (op < HILS_OP_PREFILL || op > HILS_OP_CACHE_EVICT)
         return fail(HILS_ERR_INVALID, "unknown op %d", op);
     if (p->B < 1 || p->Hq < 1 || p->Hkv < 1 || p->N < 1 || p->L < 1 || p->d < 1)
         return fail(HILS_ERR_INVALID, "B, Hq, Hkv, N, L and d must be >= 1 (B=%d Hq=%d Hkv=%d N=%d L=%d d=%d)",
@@ -70,17 +70,23 @@ int check_params(const hils_params* p, int op) {
     if (p->flags & ~(HILS_FLAG_GIVEN_IDX | HILS_FLAG_SHARED_LMK_QUERY | HILS_FLAG_HEAD_NORM_SELECT |
                      HILS_FLAG_UNION_PACKING))
         return fail(HILS_ERR_INVALID, "unknown flags 0x%x", p->flags);
+    const bool q8_cache = op == HILS_OP_Q8_APPEND || op == HILS_OP_Q8_LANDMARK || op == HILS_OP_CACHE_EVICT;
+    if (q8_cache && (p->flags & ~(op == HILS_OP_Q8_LANDMARK ? HILS_FLAG_SHARED_LMK_QUERY : 0u)))
+        return fail(HILS_ERR_INVALID, "flags 0x%x do not apply to this entry point", p->flags);
     if ((p->flags & HILS_FLAG_HEAD_NORM_SELECT) && op == HILS_OP_LANDMARK)
         return fail(HILS_ERR_INVALID, "HILS_FLAG_HEAD_NORM_SELECT does not apply to the landmark compression");
-    if ((p->flags & HILS_FLAG_SHARED_LMK_QUERY) && op != HILS_OP_LANDMARK)
+    if ((p->flags & HILS_FLAG_SHARED_LMK_QUERY) && op != HILS_OP_LANDMARK && op != HILS_OP_Q8_LANDMARK)
         return fail(HILS_ERR_INVALID, "HILS_FLAG_SHARED_LMK_QUERY applies to the landmark compression only");
     if ((p->flags & HILS_FLAG_GIVEN_IDX) && op == HILS_OP_LANDMARK)
         return fail(HILS_ERR_INVALID, "HILS_FLAG_GIVEN_IDX does not apply to the landmark compression");
-    if (op == HILS_OP_DECODE && p->N > p->L)
+    const bool decode = op == HILS_OP_DECODE || op == HILS_OP_DECODE_Q8;
+    if (q8_cache && p->N > p->L)
+        return fail(HILS_ERR_INVALID, "N <= L new tokens per sequence are needed (N=%d L=%d)", p->N, p->L);
+    if (decode && p->N > p->L)
         return fail(HILS_ERR_INVALID, "decode needs N <= L new queries per sequence (N=%d L=%d)", p->N, p->L);
-    if (op == HILS_OP_DECODE && (long)p->B * p->N > 65535)
+    if (decode && (long)p->B * p->N > 65535)
         return fail(HILS_ERR_INVALID, "decode needs B * N <= 65535 (B=%d N=%d)", p->B, p->N);
-    if (op != HILS_OP_DECODE && op != HILS_OP_LANDMARK && p->N > p->L)
+    if (!decode && !q8_cache && op != HILS_OP_LANDMARK && p->N > p->L)
         return fail(HILS_ERR_INVALID, "prefill/backward need N <= L (N=%d L=%d)", p->N, p->L);
     if (p->B > 65535 || p->Hkv > 65535) return fail(HILS_ERR_INVALID, "B and Hkv must be <= 65535");
     if (op == HILS_OP_BWD && (p->flags & HILS_FLAG_GIVEN_IDX))
@@ -92,8 +98,10 @@ int check_params(const hils_params* p, int op) {
     if (G != 1 && G != 2 && G != 4 && G != 8)
         return fail(HILS_ERR_UNSUPPORTED, "group size G=%d: kernels exist for G in {1, 2, 4, 8}", G);
     if (p->topk > 64) return fail(HILS_ERR_UNSUPPORTED, "topk=%d: kernels exist for topk <= 64", p->topk);
-    if (op == HILS_OP_DECODE && p->window > 4032)
+    if ((decode || op == HILS_OP_CACHE_EVICT) && p->window > 4032)
         return fail(HILS_ERR_UNSUPPORTED, "window=%d: the decode kernels cover windows <= 4032", p->window);
+    if (op == HILS_OP_DECODE_Q8 && (p->flags & HILS_FLAG_HEAD_NORM_SELECT))
+        return fail(HILS_ERR_UNSUPPORTED, "HILS_FLAG_HEAD_NORM_SELECT: no kernel over the 8-bit cache");
     return HILS_OK;
 }
 
@@ -109,6 +117,12 @@ size_t ws_bytes_for(const hils_params* p, int op) {
         case HILS_OP_DECODE:
             return hils::decode_workspace_bytes(p->B, p->N, p->Hkv, p->Hq / p->Hkv, p->d, p->L, p->topk, p->window,
                                                 (p->flags & HILS_FLAG_HEAD_NORM_SELECT) != 0);
+        case HILS_OP_DECODE_Q8:
+            return hils::q8_decode_workspace_bytes(p->B, p->N, p->Hkv, p->Hq / p->Hkv, p->d, p->L, p->topk, p->window);
+        case HILS_OP_Q8_APPEND:
+        case HILS_OP_Q8_LANDMARK:
+        case HILS_OP_CACHE_EVICT:
+            return 0;
         default:
             return hils::prefill_workspace_bytes(p->B, p->Hq, p->Hkv, p->N, p->L, p->d, p->topk,
                                                  p->dtype == HILS_BF16,
@@ -131,6 +145,13 @@ int hip_status(hipError_t e, const char* what) {
 
 #define REQUIRE(ptr) \
     if (!(ptr)) return fail(HILS_ERR_INVALID, "required pointer '%s' is NULL", #ptr)
+
+// Waves of a cache-writing launch, four to a workgroup of a one-dimensional grid.
+int check_q8_grid(const hils_params* p, long waves) {
+    if ((waves + 3) / 4 > 0x7fffffffl)
+        return fail(HILS_ERR_UNSUPPORTED, "B=%d Hkv=%d N=%d: more workgroups than one grid holds", p->B, p->Hkv, p->N);
+    return HILS_OK;
+}
 
 hils::FwdArgs fwd_args(const hils_params* p, const void* q, const void* k, const void* v, const void* lmk,
                        const float* bias, const void* q_route, const int32_t* seqlens, void* out, float* lse,
@@ -345,6 +366,80 @@ int hils_landmark_bwd(const hils_params* p, const void* lq, const void* k, const
     a.lq = lq; a.k = k; a.dlmk = dlmk; a.dbias = dlmk_bias; a.dlq = dlq; a.dk = dk;
     a.ws = static_cast<float*>(workspace);
     return hip_status(hils::launch_landmark_bwd(a, (hipStream_t)stream), "hils_landmark_bwd launch");
+}
+
+int hils_q8_append(const hils_params* p, const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                   float* kv_scale, const int32_t* block_table, int num_pages, const int32_t* seqlens,
+                   const int32_t* newlens, void* stream) {
+    int rc = check_params(p, HILS_OP_Q8_APPEND);
+    if (rc) return rc;
+    REQUIRE(k_new); REQUIRE(v_new); REQUIRE(k_pages); REQUIRE(v_pages); REQUIRE(kv_scale); REQUIRE(block_table);
+    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    rc = check_q8_grid(p, 2l * p->B * p->Hkv * ((p->N + 62l) / 64 + 1));
+    if (rc) return rc;
+    hils::Q8AppendArgs a;
+    a.k_new = k_new; a.v_new = v_new; a.k_pages = k_pages; a.v_pages = v_pages; a.kv_scale = kv_scale;
+    a.block_table = block_table; a.seqlens = seqlens; a.newlens = newlens;
+    a.num_pages = num_pages; a.B = p->B; a.Hkv = p->Hkv; a.N = p->N; a.L = p->L; a.d = p->d;
+    a.bf16 = p->dtype == HILS_BF16;
+    return hip_status(hils::launch_q8_append(a, (hipStream_t)stream), "hils_q8_append launch");
+}
+
+int hils_q8_landmark_fwd(const hils_params* p, const void* lq, const void* k_pages, const float* kv_scale,
+                         const int32_t* block_table, int num_pages, const int32_t* seqlens, const int32_t* newlens,
+                         void* lmk_pages, float* bias_pages, void* stream) {
+    int rc = check_params(p, HILS_OP_Q8_LANDMARK);
+    if (rc) return rc;
+    REQUIRE(lq); REQUIRE(k_pages); REQUIRE(kv_scale); REQUIRE(block_table); REQUIRE(lmk_pages); REQUIRE(bias_pages);
+    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    rc = check_q8_grid(p, (long)p->B * p->Hkv * ((p->N + 63l) / 64));
+    if (rc) return rc;
+    hils::Q8LandmarkArgs a;
+    a.lq = lq; a.k_pages = k_pages; a.kv_scale = kv_scale; a.lmk_pages = lmk_pages; a.bias_pages = bias_pages;
+    a.block_table = block_table; a.seqlens = seqlens; a.newlens = newlens;
+    a.num_pages = num_pages; a.B = p->B; a.Hkv = p->Hkv; a.Hl = p->Hl; a.G = p->Hq / p->Hkv; a.N = p->N; a.L = p->L;
+    a.d = p->d; a.bf16 = p->dtype == HILS_BF16; a.shared = (p->flags & HILS_FLAG_SHARED_LMK_QUERY) != 0;
+    a.scale = p->scale;
+    return hip_status(hils::launch_q8_landmark(a, (hipStream_t)stream), "hils_q8_landmark_fwd launch");
+}
+
+int hils_decode_q8_fwd(const hils_params* p, const void* q, const void* k_pages, const void* v_pages,
+                       const float* kv_scale, const void* lmk_pages, const float* bias_pages, const void* q_route,
+                       const int32_t* block_table, int num_pages, const int32_t* seqlens, void* out, float* lse,
+                       int32_t* idx, float* weights, void* workspace, size_t ws_bytes, void* stream) {
+    int rc = check_params(p, HILS_OP_DECODE_Q8);
+    if (rc) return rc;
+    REQUIRE(q); REQUIRE(k_pages); REQUIRE(v_pages); REQUIRE(kv_scale); REQUIRE(lmk_pages); REQUIRE(block_table);
+    REQUIRE(out); REQUIRE(lse); REQUIRE(idx);
+    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    rc = check_ws(p, HILS_OP_DECODE_Q8, workspace, ws_bytes);
+    if (rc) return rc;
+    hils::Q8DecodeArgs a;
+    a.f = fwd_args(p, q, k_pages, v_pages, lmk_pages, bias_pages, q_route, seqlens, out, lse, idx, workspace, ws_bytes);
+    a.f.block_table = block_table;
+    a.f.num_pages = num_pages;
+    a.kv_scale = kv_scale;
+    a.weights = weights;
+    return hip_status(hils::launch_q8_decode(a, (hipStream_t)stream), "hils_decode_q8_fwd launch");
+}
+
+int hils_cache_evict(const hils_params* p, const float* acc, const int32_t* block_table, const int32_t* seqlens,
+                     const float* weights, const int32_t* idx, int budget, int sink, int max_evict, float* acc_out,
+                     int32_t* table_out, int32_t* seqlens_out, int32_t* freed, int32_t* nfreed, void* stream) {
+    int rc = check_params(p, HILS_OP_CACHE_EVICT);
+    if (rc) return rc;
+    REQUIRE(acc); REQUIRE(block_table); REQUIRE(acc_out); REQUIRE(table_out); REQUIRE(seqlens_out); REQUIRE(nfreed);
+    if (weights && !idx) return fail(HILS_ERR_INVALID, "weights are given, so idx must be non-NULL");
+    if (budget < 0 || sink < 0 || max_evict < 0)
+        return fail(HILS_ERR_INVALID, "budget, sink and max_evict must be >= 0 (budget=%d sink=%d max_evict=%d)", budget,
+                    sink, max_evict);
+    if (max_evict > 0 && !freed) return fail(HILS_ERR_INVALID, "max_evict=%d, so freed must be non-NULL", max_evict);
+    hils::EvictArgs a;
+    a.acc = acc; a.table = block_table; a.seqlens = seqlens; a.weights = weights; a.idx = idx;
+    a.acc_out = acc_out; a.table_out = table_out; a.seqlens_out = seqlens_out; a.freed = freed; a.nfreed = nfreed;
+    a.B = p->B; a.Hkv = p->Hkv; a.N = p->N; a.L = p->L; a.K = p->topk; a.W = p->window;
+    a.budget = budget; a.sink = sink; a.most = max_evict;
+    return hip_status(hils::launch_evict(a, (hipStream_t)stream), "hils_cache_evict launch");
 }
 
 }  // extern "C"

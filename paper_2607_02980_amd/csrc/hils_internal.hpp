@@ -72,6 +72,51 @@ struct LmkArgs {
     int shared;          // one landmark query per head for every chunk (Sec. 4.1)
 };
 
+// The 8-bit cache (layout: hils_q8.hpp).  New tokens: the last fresh_b <= N of len_b.
+struct Q8AppendArgs {
+    const void* k_new;           // [B, Hkv, N, d], row n of sequence b at position len - fresh + n
+    const void* v_new;
+    void* k_pages;
+    void* v_pages;
+    float* kv_scale;
+    const int32_t* block_table;  // [B, L/S]
+    const int32_t* seqlens;      // nullable: L
+    const int32_t* newlens;      // nullable: N
+    int num_pages, B, Hkv, N, L, d, bf16;
+};
+struct Q8LandmarkArgs {
+    const void* lq;              // [B, Hl, ceil(N/S), d], or [Hl, d] if shared
+    const void* k_pages;
+    const float* kv_scale;
+    void* lmk_pages;
+    float* bias_pages;
+    const int32_t* block_table;
+    const int32_t* seqlens;
+    const int32_t* newlens;
+    int num_pages, B, Hkv, Hl, G, N, L, d, bf16, shared;
+    float scale;
+};
+// Decode over the 8-bit cache: f.k, f.v, f.lmk, f.bias are the pools.
+struct Q8DecodeArgs {
+    FwdArgs f;
+    const float* kv_scale;
+    float* weights;              // nullable: [B, Hkv, N, K + window pieces]
+};
+// Eviction by accumulated weight; the outputs may be the inputs.
+struct EvictArgs {
+    const float* acc;            // [B, L/S]
+    const int32_t* table;        // [B, L/S]
+    const int32_t* seqlens;      // nullable: L
+    const float* weights;        // nullable: nothing to add; else [B, Hkv, N, K + window pieces]
+    const int32_t* idx;          // [B, Hkv, N, K]
+    float* acc_out;
+    int32_t* table_out;
+    int32_t* seqlens_out;
+    int32_t* freed;              // [B, most], -1 past nfreed[b]
+    int32_t* nfreed;
+    int B, Hkv, N, L, K, W, budget, sink, most;
+};
+
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Optional per-kernel timing (hils_timing_enable): every launch is bracketed by
@@ -157,6 +202,13 @@ hipError_t decode_noalloc_scratch(void** ptr);
 hipError_t launch_landmark_fwd(const LmkArgs& a, hipStream_t s);
 hipError_t launch_landmark_bwd(const LmkArgs& a, hipStream_t s);
 size_t landmark_workspace_bytes(int B, int Hl, int nC, int d, bool shared);
+hipError_t launch_q8_append(const Q8AppendArgs& a, hipStream_t s);
+hipError_t launch_q8_landmark(const Q8LandmarkArgs& a, hipStream_t s);
+size_t q8_decode_workspace_bytes(int B, int N, int Hkv, int G, int d, int L, int K, int W);
+hipError_t launch_q8_decode(const Q8DecodeArgs& a, hipStream_t s);
+hipError_t launch_q8_decode_d64(const Q8DecodeArgs& a, hipStream_t s);
+hipError_t launch_q8_decode_d128(const Q8DecodeArgs& a, hipStream_t s);
+hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
 hipError_t launch_bwd(const BwdArgs& a, hipStream_t s);
 hipError_t launch_bwd_f32(const BwdArgs& a, hipStream_t s);   // fp32 storage
 size_t bwd_f32_workspace_bytes(int B, int Hq, int Hkv, int N, int L, int d, int K, int W);

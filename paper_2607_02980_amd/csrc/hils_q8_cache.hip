@@ -1,0 +1,294 @@
+// Writing the 8-bit cache (gfx950): new tokens' keys and values, and the landmark rows of the
+// chunks that they complete.  Layout of the cache: hils_q8.hpp.
+#include "hils_dispatch.hpp"
+#include "hils_q8.hpp"
+
+namespace hils {
+
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kWaves = kBlock / kWave;
+
+// Smallest e >= -100 with amax <= 448 * 2^e, from the float's exponent and whether its
+// significand is above 448 / 256; 2^e and 2^-e are then normal floats for every finite amax.
+__device__ __forceinline__ float scale_for(float amax) {
+    const uint32_t u = __float_as_uint(amax);
+    const int ex = (int)(u >> 23) - 127;
+    int e = (u & 0x7fffffu) > 0x600000u ? ex - 7 : ex - 8;
+    e = e < -100 ? -100 : e;
+    return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+__device__ __forceinline__ float finite_abs(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
+template <typename T>
+__device__ __forceinline__ void load_pair(const T* p, float& x, float& y) {
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t u = *reinterpret_cast<const uint32_t*>(p);
+        x = __uint_as_float(u << 16);
+        y = __uint_as_float(u & 0xffff0000u);
+    } else {
+        const float2 f = *reinterpret_cast<const float2*>(p);
+        x = f.x;
+        y = f.y;
+    }
+}
+
+// ---- new tokens ------------------------------------------------------------------
+//
+// One wave per (sequence, chunk that gets tokens, KV head, K or V).  With a the largest finite
+// magnitude among the chunk's new rows, s = scale_for(a), or the scale the chunk has if it
+// holds older tokens and that one is larger; new x -> e4m3(x / s).  Where s grew, older codes
+// y -> e4m3(y * s_old / s): powers of two, so exact unless the result falls below e4m3's
+// normal range.  Infinities, which e4m3 lacks, become NaN, as the conversion makes them.  Bytes of rows at or past the sequence's end are left as they were.
+//
+// A lane holds two neighbouring dims of its rows (d = 64: of half the rows), so that a row is
+// one coalesced load, a chunk's values are in registers between the maximum and the
+// conversion, and V's dim-major row of 64 keys is 64 contiguous bytes of one lane.
+template <typename T, int D>
+__global__ __launch_bounds__(kBlock) void k_q8_append(Q8AppendArgs a, int most) {
+    constexpr int LPR = D / 2, TH = kWave / LPR, ROWS = kChunk / TH;  // lanes per row, row groups, rows per lane
+    const int lane = threadIdx.x % kWave, dd = (lane % LPR) * 2, th = lane / LPR;
+    // unit: (sequence, head, chunk, K or V), the last fastest
+    const long unit = (long)blockIdx.x * kWaves + wave_id();
+    const int which = unit & 1;
+    long u = unit >> 1;
+    const int j = (int)(u % most);
+    u /= most;
+    const int g = (int)(u % a.Hkv), b = (int)(u / a.Hkv);
+    if (b >= a.B) return;
+    int fresh;
+    const int len = q8_tokens(a, b, fresh), start = len - fresh;
+    const int c = start / kChunk + j;
+    const int r0 = j == 0 ? start % kChunk : 0, r1 = min(kChunk, len - c * kChunk);  // the chunk's new rows
+    if (fresh == 0 || r1 <= r0) return;
+    const size_t page = clamp_page(a.block_table[(size_t)b * (a.L / kChunk) + c], a.num_pages);
+    const size_t pg = page * a.Hkv + g;
+    uint8_t* dst = static_cast<uint8_t*>(which ? a.v_pages : a.k_pages) + pg * kChunk * D;
+    float* scale = a.kv_scale + pg * 2 + which;
+    // row r of the chunk is new token c * 64 + r - start
+    const T* src = as<T>(which ? a.v_new : a.k_new) + ((size_t)b * a.Hkv + g) * a.N * D +
+                   ((long)c * kChunk - start) * D + dd;
+    if (r0 == 0 && r1 == kChunk) {  // a whole chunk, in registers
+        float x[ROWS][2];
+        float m = 0.f;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) load_pair(src + (size_t)(th * ROWS + r) * D, x[r][0], x[r][1]);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) m = fmaxf(m, fmaxf(finite_abs(x[r][0]), finite_abs(x[r][1])));
+        const float s = scale_for(wave_max(m)), inv = 1.f / s;
+        if (lane == 0) *scale = s;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            x[r][0] *= inv;
+            x[r][1] *= inv;
+        }
+        if (which) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < ROWS; r += 16) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        w[i] = f32x4_to_e4m3(x[r + 4 * i][t], x[r + 4 * i + 1][t], x[r + 4 * i + 2][t],
+                                             x[r + 4 * i + 3][t]);
+                    *reinterpret_cast<uint4*>(dst + (dd + t) * kChunk + th * ROWS + r) =
+                        make_uint4(w[0], w[1], w[2], w[3]);
+                }
+        } else {
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+                *reinterpret_cast<uint16_t*>(dst + (th * ROWS + r) * D + dd) =
+                    (uint16_t)f32x4_to_e4m3(x[r][0], x[r][1], 0.f, 0.f);
+        }
+        return;
+    }
+    float m = 0.f;
+#pragma unroll 4
+    for (int r = r0 + th; r < r1; r += TH) {
+        float x, y;
+        load_pair(src + (long)r * D, x, y);
+        m = fmaxf(m, fmaxf(finite_abs(x), finite_abs(y)));
+    }
+    float s = scale_for(wave_max(m));
+    if (r0 > 0) {
+        const float old = *scale;
+        s = fmaxf(s, old);
+        if (s != old) {  // the older codes at the new scale
+            const float f = old / s;
+            auto moved = [&](uint32_t w) {
+                float y[4];
+                e4m3_to_f32x4(w, y);
+                return f32x4_to_e4m3(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+            };
+            if (which) {
+                const int quads = (r0 + 3) / 4;  // dwords of a dim's row with older keys
+                for (int e = lane; e < quads * D; e += kWave) {
+                    uint32_t* w = reinterpret_cast<uint32_t*>(dst + (e % D) * kChunk) + e / D;
+                    const int n = r0 - e / D * 4;
+                    const uint32_t keep = n >= 4 ? 0xffffffffu : (1u << (8 * n)) - 1u, was = *w;
+                    *w = (moved(was) & keep) | (was & ~keep);
+                }
+            } else {
+                uint32_t* w = reinterpret_cast<uint32_t*>(dst);
+                for (int e = lane; e < r0 * D / 4; e += kWave) w[e] = moved(w[e]);
+            }
+            // the new keys' bytes may share a dword with the older ones'
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+    }
+    if (lane == 0) *scale = s;
+    const float inv = 1.f / s;
+#pragma unroll 4
+    for (int r = r0 + th; r < r1; r += TH) {
+        float x, y;
+        load_pair(src + (long)r * D, x, y);
+        const uint32_t w = f32x4_to_e4m3(x * inv, y * inv, 0.f, 0.f);
+        if (which) {
+            dst[dd * kChunk + r] = (uint8_t)w;
+            dst[(dd + 1) * kChunk + r] = (uint8_t)(w >> 8);
+        } else {
+            *reinterpret_cast<uint16_t*>(dst + r * D + dd) = (uint16_t)w;
+        }
+    }
+}
+
+// ---- landmark rows -----------------------------------------------------------------
+//
+// Prop. 3.1 on the stored keys k_j = x_j ks: one wave per (sequence, completed chunk, KV head),
+// the group's landmark heads as MFMA columns: S^T = K Q'^T, the softmax over the lane groups,
+// b' = log l - sum_j p_j s_j (s from its maximum), then sum_j p_j x_j per dim from the wave's
+// copy of K in LDS, P in float32: k' / ks, as e4m3.
+template <typename T, int D, int G>
+struct LmkSmem {
+    uint8_t k[kChunk * D];
+    float p[kChunk][G];
+};
+template <typename T, int D, int G>
+__global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int most) {
+    constexpr int DJ = D / 64, LPR = D / 2, TH = kWave / LPR;
+    __shared__ __align__(16) LmkSmem<T, D, G> sm_all[kWaves];
+    LmkSmem<T, D, G>& sm = sm_all[wave_id()];
+    const int lane = threadIdx.x % kWave, lg = lane / 16, n16 = lane % 16;
+    const long unit = (long)blockIdx.x * kWaves + wave_id();
+    const int g = (int)(unit % a.Hkv);
+    const int j = (int)(unit / a.Hkv % most), b = (int)(unit / a.Hkv / most);
+    if (b >= a.B) return;
+    int fresh;
+    const int len = q8_tokens(a, b, fresh);
+    const int c = (len - fresh) / kChunk + j;
+    if (c >= len / kChunk) return;
+    const size_t page = clamp_page(a.block_table[(size_t)b * (a.L / kChunk) + c], a.num_pages);
+    const uint8_t* kp = static_cast<const uint8_t*>(a.k_pages) + (page * a.Hkv + g) * kChunk * D;
+    const float ks = a.kv_scale[(page * a.Hkv + g) * 2];
+    const int gl = a.Hl / a.Hkv;  // landmark heads of the group: G or 1
+    // key of row m = 4 a + i of block kb: 16 a + 4 kb + i, so that lane group lg ends with keys 16 lg + 0..15
+    uint4 kx[4][DJ];
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int t = 0; t < DJ; ++t)
+            kx[kb][t] = *reinterpret_cast<const uint4*>(kp + ((n16 / 4) * 16 + kb * 4 + n16 % 4) * D + t * 64 + lg * 16);
+    QRow<T, D> q;
+    {
+        const int hl = g * gl + min(n16, gl - 1);
+        const size_t row = a.shared ? hl : ((size_t)b * a.Hl + hl) * most + j;
+        q.load(as<T>(a.lq) + row * D, lg, n16 < gl);
+    }
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int t = 0; t < DJ; ++t)
+            *reinterpret_cast<uint4*>(sm.k + ((n16 / 4) * 16 + kb * 4 + n16 % 4) * D + t * 64 + lg * 16) = kx[kb][t];
+    const float c1 = a.scale * ks;
+    float s[16], mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+        const f32x4 st = mfma_row<T, D>(kx[kb], q, zero4());
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[kb * 4 + i] = st[i] * c1;
+            mx = fmaxf(mx, s[kb * 4 + i]);
+        }
+    }
+    mx = group4_max(mx);
+    float l = 0.f, ps = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float t = s[i] - mx;
+        s[i] = fexp2(t * kLog2e);
+        l += s[i];
+        ps += s[i] * t;
+    }
+    l = group4_sum(l);
+    ps = group4_sum(ps);
+    const float inv = 1.f / l;
+    if (n16 < gl) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sm.p[lg * 16 + i][n16] = s[i] * inv;
+        if (lg == 0) a.bias_pages[page * a.Hl + g * gl + n16] = logf(l) - ps * inv;
+    }
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int dd = (lane % LPR) * 2, th = lane / LPR;
+    float acc[G][2] = {};
+#pragma unroll 8
+    for (int r = th; r < kChunk; r += TH) {
+        typedef __attribute__((ext_vector_type(2))) float f32x2;
+        const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(*reinterpret_cast<const uint16_t*>(sm.k + r * D + dd), false);
+#pragma unroll
+        for (int h = 0; h < G; ++h)
+            if (h < gl) {
+                acc[h][0] += sm.p[r][h] * x[0];
+                acc[h][1] += sm.p[r][h] * x[1];
+            }
+    }
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+        if (h >= gl) break;
+        if constexpr (TH == 2) {
+            acc[h][0] += __shfl_xor(acc[h][0], LPR, kWave);
+            acc[h][1] += __shfl_xor(acc[h][1], LPR, kWave);
+        }
+        // (a convex combination of codes: above 448 by the sum's rounding at most, which rounds back to it)
+        const uint32_t w = f32x4_to_e4m3(acc[h][0], acc[h][1], 0.f, 0.f);
+        if (th == 0)
+            *reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(a.lmk_pages) + (page * a.Hl + g * gl + h) * D + dd) =
+                (uint16_t)w;
+    }
+}
+
+}  // namespace
+
+hipError_t launch_q8_append(const Q8AppendArgs& a, hipStream_t s) {
+    const int most = (a.N + 62) / kChunk + 1;  // chunks that N tokens reach into
+    const long waves = (long)a.B * a.Hkv * most * 2;
+    const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves)), block(kBlock);
+    if (a.bf16) {
+        if (a.d == 64) HILS_LAUNCH("k_q8_append", (k_q8_append<bf16, 64>), grid, block, 0, s, a, most);
+        else HILS_LAUNCH("k_q8_append", (k_q8_append<bf16, 128>), grid, block, 0, s, a, most);
+    } else {
+        if (a.d == 64) HILS_LAUNCH("k_q8_append", (k_q8_append<float, 64>), grid, block, 0, s, a, most);
+        else HILS_LAUNCH("k_q8_append", (k_q8_append<float, 128>), grid, block, 0, s, a, most);
+    }
+    return hipGetLastError();
+}
+
+namespace {
+struct Q8LandmarkRun {
+    template <typename T, int D, int G>
+    static hipError_t run(const Q8LandmarkArgs& a, hipStream_t s) {
+        const int most = (a.N + kChunk - 1) / kChunk;  // chunks that N tokens complete, at most
+        const long waves = (long)a.B * a.Hkv * most;
+        HILS_LAUNCH("k_q8_landmark", (k_q8_landmark<T, D, G>), dim3((unsigned)((waves + kWaves - 1) / kWaves)),
+                    dim3(kBlock), 0, s, a, most);
+        return hipGetLastError();
+    }
+};
+}  // namespace
+
+hipError_t launch_q8_landmark(const Q8LandmarkArgs& a, hipStream_t s) {
+    return dispatch<Q8LandmarkRun>(a.bf16, a.d, a.G, a, s);
+}
+
+}  // namespace hils

@@ -2,7 +2,8 @@
 
 The entry points keep the C names (``hils_prefill_fwd``, ``hils_decode_fwd``,
 ``hils_decode_fwd_noalloc``, ``hils_decode_paged_fwd``, ``hils_bwd``,
-``hils_landmark_fwd``, ``hils_landmark_bwd``,
+``hils_landmark_fwd``, ``hils_landmark_bwd``, ``hils_q8_append``,
+``hils_q8_landmark_fwd``, ``hils_decode_q8_fwd``, ``hils_cache_evict``,
 ``hils_workspace_size``, ``hils_prefill_record_cap``, ``hils_last_error``, ``hils_version``).
 They take torch tensors already resident on the GPU, check dtype, shape,
 device and contiguity, allocate missing outputs and the workspace with
@@ -13,6 +14,7 @@ if ``libhils.so`` is missing or fails to load, importing this module raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -29,6 +31,7 @@ HILS_FLAG_SHARED_LMK_QUERY = 2
 HILS_FLAG_HEAD_NORM_SELECT = 4
 HILS_FLAG_UNION_PACKING = 8
 HILS_OP_PREFILL, HILS_OP_DECODE, HILS_OP_BWD, HILS_OP_LANDMARK = 0, 1, 2, 3
+HILS_OP_DECODE_Q8, HILS_OP_Q8_APPEND, HILS_OP_Q8_LANDMARK, HILS_OP_CACHE_EVICT = 4, 5, 6, 7
 
 
 class HilsError(RuntimeError):
@@ -60,6 +63,11 @@ def _load():
     lib.hils_bwd.argtypes = [P] + [vp] * 17 + [sz, vp]
     lib.hils_landmark_fwd.argtypes = [P, vp, vp, vp, vp, vp]
     lib.hils_landmark_bwd.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    ci = ctypes.c_int
+    lib.hils_q8_append.argtypes = [P, vp, vp, vp, vp, vp, vp, ci, vp, vp, vp]
+    lib.hils_q8_landmark_fwd.argtypes = [P, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp]
+    lib.hils_decode_q8_fwd.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.hils_cache_evict.argtypes = [P, vp, vp, vp, vp, vp, ci, ci, ci, vp, vp, vp, vp, vp, vp]
     lib.hils_prefill_record_cap.argtypes = [sz]
     lib.hils_prefill_record_cap.restype = sz
     lib.hils_timing_enable.argtypes = [ctypes.c_int]
@@ -67,7 +75,8 @@ def _load():
                                      ctypes.POINTER(ctypes.c_int), ctypes.c_int, ctypes.POINTER(ctypes.c_int)]
     for f in (lib.hils_workspace_size, lib.hils_prefill_fwd, lib.hils_decode_fwd, lib.hils_decode_fwd_noalloc,
               lib.hils_bwd,
-              lib.hils_landmark_fwd, lib.hils_landmark_bwd, lib.hils_timing_enable, lib.hils_timing_read):
+              lib.hils_landmark_fwd, lib.hils_landmark_bwd, lib.hils_q8_append, lib.hils_q8_landmark_fwd,
+              lib.hils_decode_q8_fwd, lib.hils_cache_evict, lib.hils_timing_enable, lib.hils_timing_read):
         f.restype = ctypes.c_int
     return lib
 
@@ -329,6 +338,140 @@ def hils_landmark_bwd(p: Params, lq, k, dlmk, dlmk_bias=None, dlq=None, dk=None,
                                  _ptr(dlq, "dlq", lqs, dt), _ptr(dk, "dk", S["kv"], dt), _ptr(ws, "workspace"), n,
                                  _stream()))
     return dlq, dk
+
+
+# ---- the 8-bit cache: k_pages [P, Hkv, S, d], v_pages [P, Hkv, d, S] and lmk_pages [P, Hl, d] are
+# torch.float8_e4m3fn, kv_scale [P, Hkv, 2] and bias_pages [P, Hl] float32, block_table [B, L/S] int32
+
+
+def _on_device_of(fn):
+    """The call with its first tensor's device current (the kernels run there, on that device's current stream)."""
+    @functools.wraps(fn)
+    def call(p, t, *args, **kw):
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            with torch.cuda.device(t.device):
+                return fn(p, t, *args, **kw)
+        return fn(p, t, *args, **kw)
+    return call
+
+
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, expected {dev}")
+
+
+def hils_window_pieces(window: int) -> int:
+    """Chunks that a window of this many tokens reaches into, at most: the window entries of ``weights``."""
+    return (window + 62) // 64 + 1
+
+
+@_on_device_of
+def hils_q8_append(p: Params, k_new, v_new, k_pages, v_pages, kv_scale, block_table, seqlens=None, newlens=None):
+    """Write new tokens into the 8-bit cache: sequence b's first newlens[b] rows of k_new, v_new
+    [B, Hkv, N, d] go to its last newlens[b] positions (seqlens counts them).  Changes k_pages,
+    v_pages and kv_scale in place and returns them."""
+    dt, n = p.torch_dtype, k_pages.shape[0]
+    new = (p.B, p.Hkv, p.N, p.d)
+    cp = p.c()
+    args = (_ptr(k_new, "k_new", new, dt), _ptr(v_new, "v_new", new, dt),
+            _ptr(k_pages, "k_pages", (n, p.Hkv, p.chunk, p.d), torch.float8_e4m3fn),
+            _ptr(v_pages, "v_pages", (n, p.Hkv, p.d, p.chunk), torch.float8_e4m3fn),
+            _ptr(kv_scale, "kv_scale", (n, p.Hkv, 2), torch.float32),
+            _ptr(block_table, "block_table", (p.B, p.L // p.chunk), torch.int32), n,
+            _ptr(seqlens, "seqlens", (p.B,), torch.int32, False), _ptr(newlens, "newlens", (p.B,), torch.int32, False))
+    _same_device(k_new.device, v_new=v_new, k_pages=k_pages, v_pages=v_pages, kv_scale=kv_scale,
+                 block_table=block_table, seqlens=seqlens, newlens=newlens)
+    _check(LIB.hils_q8_append(ctypes.byref(cp), *args, _stream()))
+    return k_pages, v_pages, kv_scale
+
+
+@_on_device_of
+def hils_q8_landmark_fwd(p: Params, lq, k_pages, kv_scale, block_table, lmk_pages, bias_pages, seqlens=None,
+                         newlens=None):
+    """Landmark rows and biases of the chunks that each sequence's last newlens[b] tokens completed, from
+    the stored keys: lq [B, Hl, (N + S - 1) // S, d] (one query per completed chunk) or [Hl, d] under
+    HILS_FLAG_SHARED_LMK_QUERY.  Changes lmk_pages and bias_pages in place and returns them."""
+    dt, n, Hl = p.torch_dtype, k_pages.shape[0], p.Hl or p.Hq
+    lqs = (Hl, p.d) if p.flags & HILS_FLAG_SHARED_LMK_QUERY else (p.B, Hl, (p.N + p.chunk - 1) // p.chunk, p.d)
+    cp = p.c()
+    args = (_ptr(lq, "lq", lqs, dt), _ptr(k_pages, "k_pages", (n, p.Hkv, p.chunk, p.d), torch.float8_e4m3fn),
+            _ptr(kv_scale, "kv_scale", (n, p.Hkv, 2), torch.float32),
+            _ptr(block_table, "block_table", (p.B, p.L // p.chunk), torch.int32), n,
+            _ptr(seqlens, "seqlens", (p.B,), torch.int32, False), _ptr(newlens, "newlens", (p.B,), torch.int32, False),
+            _ptr(lmk_pages, "lmk_pages", (n, Hl, p.d), torch.float8_e4m3fn),
+            _ptr(bias_pages, "bias_pages", (n, Hl), torch.float32))
+    _same_device(lq.device, k_pages=k_pages, kv_scale=kv_scale, block_table=block_table, seqlens=seqlens,
+                 newlens=newlens, lmk_pages=lmk_pages, bias_pages=bias_pages)
+    _check(LIB.hils_q8_landmark_fwd(ctypes.byref(cp), *args, _stream()))
+    return lmk_pages, bias_pages
+
+
+@_on_device_of
+def hils_decode_q8_fwd(p: Params, q, k_pages, v_pages, kv_scale, lmk_pages, block_table, bias_pages=None, q_route=None,
+                       seqlens=None, out=None, lse=None, idx=None, weights=None, want_weights=True, workspace=None):
+    """Decode forward over the 8-bit cache, N >= 1 new queries per sequence.  Returns (out, lse, idx, weights);
+    weights [B, Hkv, N, K + hils_window_pieces(W)] float32 (None without want_weights): each selected chunk's
+    and window piece's attention weight, summed over the group's heads."""
+    S, dt, f8, n, Hl = _shapes(p), p.torch_dtype, torch.float8_e4m3fn, k_pages.shape[0], p.Hl or p.Hq
+    dev = q.device
+    ws_shape = (p.B, p.Hkv, p.N, p.topk + hils_window_pieces(p.window))
+    if out is None:
+        out = torch.empty(S["q"], dtype=dt, device=dev)
+    if lse is None:
+        lse = torch.empty(S["lse"], dtype=torch.float32, device=dev)
+    if idx is None:
+        if p.flags & HILS_FLAG_GIVEN_IDX:
+            raise ValueError("HILS_FLAG_GIVEN_IDX needs idx")
+        idx = torch.empty(S["idx"], dtype=torch.int32, device=dev)
+    if weights is None and want_weights:
+        weights = torch.empty(ws_shape, dtype=torch.float32, device=dev)
+    ws, nbytes = _workspace(p, HILS_OP_DECODE_Q8, workspace)
+    cp = p.c()
+    args = (_ptr(q, "q", S["q"], dt), _ptr(k_pages, "k_pages", (n, p.Hkv, p.chunk, p.d), f8),
+            _ptr(v_pages, "v_pages", (n, p.Hkv, p.d, p.chunk), f8),
+            _ptr(kv_scale, "kv_scale", (n, p.Hkv, 2), torch.float32), _ptr(lmk_pages, "lmk_pages", (n, Hl, p.d), f8),
+            _ptr(bias_pages, "bias_pages", (n, Hl), torch.float32, False), _ptr(q_route, "q_route", S["q"], dt, False),
+            _ptr(block_table, "block_table", (p.B, p.L // p.chunk), torch.int32), n,
+            _ptr(seqlens, "seqlens", (p.B,), torch.int32, False), _ptr(out, "out", S["q"], dt),
+            _ptr(lse, "lse", S["lse"], torch.float32), _ptr(idx, "idx", S["idx"], torch.int32),
+            _ptr(weights, "weights", ws_shape, torch.float32, False), _ptr(ws, "workspace"), nbytes)
+    _same_device(dev, k_pages=k_pages, v_pages=v_pages, kv_scale=kv_scale, lmk_pages=lmk_pages, bias_pages=bias_pages,
+                 q_route=q_route, block_table=block_table, seqlens=seqlens, out=out, lse=lse, idx=idx,
+                 weights=weights, workspace=ws)
+    _check(LIB.hils_decode_q8_fwd(ctypes.byref(cp), *args, _stream()))
+    return out, lse, idx, weights
+
+
+@_on_device_of
+def hils_cache_evict(p: Params, acc, block_table, seqlens=None, budget=0, sink=0, max_evict=None, weights=None,
+                     idx=None, acc_out=None, table_out=None, seqlens_out=None, freed=None, nfreed=None):
+    """Add a decode call's weights (and idx) to the chunks' totals acc [B, L/S], then cut every sequence to
+    ``budget`` candidate chunks by dropping those with the least totals, never the first ``sink``, at most
+    max_evict (None: any number).  Returns (acc, block_table, seqlens, freed, nfreed), new tensors unless
+    outputs are given (the inputs themselves for a call in place); the pages given up by sequence b are
+    freed[b, :nfreed[b]]."""
+    nc, dev, i32 = p.L // p.chunk, acc.device, torch.int32
+    most = nc if max_evict is None else max_evict
+    ws_shape = (p.B, p.Hkv, p.N, p.topk + hils_window_pieces(p.window))
+    if weights is not None and idx is None:
+        raise ValueError("weights needs idx")
+    acc_out = torch.empty_like(acc) if acc_out is None else acc_out
+    table_out = torch.empty_like(block_table) if table_out is None else table_out
+    seqlens_out = torch.empty(p.B, dtype=i32, device=dev) if seqlens_out is None else seqlens_out
+    freed = torch.empty((p.B, most), dtype=i32, device=dev) if freed is None else freed
+    nfreed = torch.empty(p.B, dtype=i32, device=dev) if nfreed is None else nfreed
+    cp = p.c()
+    args = (_ptr(acc, "acc", (p.B, nc), torch.float32), _ptr(block_table, "block_table", (p.B, nc), i32),
+            _ptr(seqlens, "seqlens", (p.B,), i32, False), _ptr(weights, "weights", ws_shape, torch.float32, False),
+            _ptr(idx, "idx", (p.B, p.Hkv, p.N, p.topk), i32, False) if weights is not None else None, budget, sink, most,
+            _ptr(acc_out, "acc_out", (p.B, nc), torch.float32), _ptr(table_out, "table_out", (p.B, nc), i32),
+            _ptr(seqlens_out, "seqlens_out", (p.B,), i32), _ptr(freed, "freed", (p.B, most), i32),
+            _ptr(nfreed, "nfreed", (p.B,), i32))
+    _same_device(dev, block_table=block_table, seqlens=seqlens, weights=weights, idx=idx, acc_out=acc_out,
+                 table_out=table_out, seqlens_out=seqlens_out, freed=freed, nfreed=nfreed)
+    _check(LIB.hils_cache_evict(ctypes.byref(cp), *args, _stream()))
+    return acc_out, table_out, seqlens_out, freed, nfreed
 
 
 def hils_timing_enable(on: bool = True) -> None:
