@@ -22,7 +22,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["hils_api.cpp", "hils_fwd.hip", "hils_f32.hip", "hils_prefill.hip", "hils_bwd.hip", "hils_bwd_mfma.hip", "hils_decode.hip", "hils_decode_d64.hip", "hils_decode_d128.hip", "hils_landmark.hip", "hils_noalloc.hip",
-           "hils_q8_cache.hip", "hils_q8_decode_d64.hip", "hils_q8_decode_d128.hip", "hils_evict.hip"]
+           "hils_q8_cache.hip", "hils_q8_decode.hip", "hils_q8_decode_bf16_d64.hip", "hils_q8_decode_bf16_d128.hip",
+           "hils_q8_decode_f32_d64.hip", "hils_q8_decode_f32_d128.hip", "hils_evict.hip"]
 
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",

@@ -148,7 +148,7 @@ int hip_status(hipError_t e, const char* what) {
 
 // Waves of a cache-writing launch, four to a workgroup of a one-dimensional grid.
 int check_q8_grid(const hils_params* p, long waves) {
-    if ((waves + 3) / 4 > 0x7fffffffl)
+    if ((waves + 3) / 4 > 0xffffffl)  // 2^32 threads
         return fail(HILS_ERR_UNSUPPORTED, "B=%d Hkv=%d N=%d: more workgroups than one grid holds", p->B, p->Hkv, p->N);
     return HILS_OK;
 }

@@ -7,8 +7,10 @@
 // over them and its length falls by 64 per chunk: chunks are whole, so every later position keeps
 // its place inside its chunk.
 //
-// One workgroup per sequence; a sequence's totals and table are read and written once (16 bytes
-// per chunk) and come from the L2 in between.
+// One workgroup per sequence.  What bounds it is latency: a step's work is a few kilobytes per
+// sequence and a dozen dependent phases.  Up to kMaxHeld chunks a sequence's totals stay in LDS
+// and its table in registers between the phases (k_evict); longer ones are read again from the L2 in
+// each (k_evict_long; 16384 chunks cut to 4096: 46 us, k_evict 14).
 #include "hils_dispatch.hpp"
 #include "hils_internal.hpp"
 
@@ -18,6 +20,7 @@ namespace {
 
 constexpr int kEvictBlock = 1024;
 constexpr int kEvictWaves = kEvictBlock / kWave;
+constexpr int kMaxHeld = 32 * kEvictBlock;  // chunks: totals of 128 KB in LDS
 
 // How many lanes below have x, and how many of the wave.
 __device__ __forceinline__ int below(bool x, int& all) {
@@ -26,7 +29,10 @@ __device__ __forceinline__ int below(bool x, int& all) {
     return popc64(m & ((1ull << __lane_id()) - 1ull));
 }
 
-__global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
+// Order of the totals: -0 as 0, a NaN above every number (such a chunk stays while another can go).
+__device__ __forceinline__ uint32_t total_key(float x) { return x != x ? 0xffffffffu : ordered_key(x + 0.f); }
+
+__global__ __launch_bounds__(kEvictBlock) void k_evict_long(EvictArgs a) {
     __shared__ int s_hist[256];
     __shared__ int s_bin, s_k;
     __shared__ int s_tie[kEvictWaves], s_gone[kEvictWaves];
@@ -77,8 +83,7 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
     __syncthreads();
 
     // ---- the drop-th smallest total of chunks sink .. last - 1, eight bits of its key at a time ----
-    // (a total of -0 counts as 0; a NaN is above every number and stays)
-    auto key_of = [&](int c) { return ordered_key(acc[c] + 0.f); };
+    auto key_of = [&](int c) { return total_key(acc[c]); };
     uint32_t T = 0, mask = 0;
     int k = drop;
     for (int shift = 24; shift >= 0; shift -= 8) {
@@ -129,7 +134,7 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
         const float total = in ? acc[c] : 0.f;
         const int32_t page = in ? table_in[c] : -1;
         const bool free_ = c >= a.sink && c < last;
-        const uint32_t key = ordered_key(total + 0.f);
+        const uint32_t key = total_key(total);
         const bool tie = free_ && key == T;
         int nt, ng;
         int before = below(tie, nt);
@@ -160,10 +165,211 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
     }
 }
 
+// The totals of up to 1024 EPT chunks in LDS.  With nr chunks per thread, wave w owns chunks
+// 64 nr w + 64 r + lane, r < nr.
+template <int EPT>
+__global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
+    constexpr int NW = kEvictWaves, kSteps = 1024;
+    __shared__ float s_tot[EPT * kEvictBlock];
+    __shared__ int s_hist[kSteps];
+    __shared__ uint32_t s_lo[NW], s_hi[NW];
+    __shared__ int s_step, s_below, s_ties[NW], s_gone[NW];
+    const int b = blockIdx.x, tid = threadIdx.x, w = wave_id(), lane = tid % kWave;
+    const int nC = a.L / kChunk, nr = (nC + kEvictBlock - 1) / kEvictBlock, first = w * kWave * nr + lane;
+    const float* acc_in = a.acc + (size_t)b * nC;
+    float* acc = a.acc_out + (size_t)b * nC;
+    const int32_t* table_in = a.table + (size_t)b * nC;
+    int32_t* table = a.table_out + (size_t)b * nC;
+    int len = a.seqlens ? a.seqlens[b] : a.L;
+    len = len < a.N ? a.N : (len > a.L ? a.L : len);
+    int32_t page[EPT];
+#pragma unroll
+    for (int r = 0; r < EPT; ++r) {
+        if (r >= nr) break;
+        const int c = first + r * kWave;
+        s_tot[c] = c < nC ? acc_in[c] : 0.f;
+        page[r] = c < nC ? table_in[c] : -1;
+    }
+    if (a.weights) {
+        // row after row (g, n), so that a total is one sum in one order; a row names a chunk once
+        const int per = a.K + (a.W + 62) / kChunk + 1, total = a.Hkv * a.N * per;
+        for (int e0 = 0; e0 < total; e0 += kEvictBlock) {
+            const int e = e0 + tid, r = e / per, t = e % per;
+            int c = -1;
+            float x = 0.f;
+            if (e < total) {
+                const int pos = len - a.N + r % a.N, ncand = n_candidates(pos, a.W);
+                const size_t rg = (size_t)b * a.Hkv * a.N + r;
+                x = a.weights[rg * per + t];
+                if (t < a.K) {
+                    if (idx_entry_valid(a.idx + rg * a.K, t, ncand)) c = a.idx[rg * a.K + t];
+                } else if (ncand + t - a.K <= pos / kChunk) {
+                    c = ncand + t - a.K;
+                }
+            }
+            const int r1 = min(total - 1, e0 + kEvictBlock - 1) / per;
+            for (int row = e0 / per; row <= r1; ++row) {
+                __syncthreads();
+                if (c >= 0 && r == row) s_tot[c] += x;
+            }
+        }
+    }
+    __syncthreads();  // the totals; and every wave has read what the outputs may replace
+    const int last = n_candidates(len - 1, a.W), able = max(0, last - a.sink);
+    const int drop = min(min(max(0, last - a.budget), able), a.most);
+    if (tid == 0) {
+        a.seqlens_out[b] = len - drop * kChunk;
+        a.nfreed[b] = drop;
+    }
+    int32_t* freed = a.freed + (size_t)b * a.most;  // (not touched if most is 0)
+    for (int t = drop + tid; t < a.most; t += kEvictBlock) freed[t] = -1;
+    if (drop == 0) {
+#pragma unroll
+        for (int r = 0; r < EPT; ++r) {
+            if (r >= nr) break;
+            const int c = first + r * kWave;
+            if (c < nC) {
+                acc[c] = s_tot[c];
+                table[c] = page[r];
+            }
+        }
+        return;
+    }
+    // keys of the chunks that may go (from LDS each time: 32 of them and the pages are too many registers)
+    auto key_of = [&](int r) { return total_key(s_tot[first + r * kWave]); };
+    auto may_go = [&](int r) { return first + r * kWave >= a.sink && first + r * kWave < last; };
+    uint32_t lo = 0xffffffffu, hi = 0;
+#pragma unroll
+    for (int r = 0; r < EPT; ++r) {
+        if (r >= nr) break;
+        if (may_go(r)) {
+            const uint32_t key = key_of(r);
+            lo = min(lo, key);
+            hi = max(hi, key);
+        }
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, kWave));
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, kWave));
+    }
+    if (lane == 0) {
+        s_lo[w] = lo;
+        s_hi[w] = hi;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+        lo = min(lo, s_lo[i]);
+        hi = max(hi, s_hi[i]);
+    }
+    // the drop-th smallest key: histograms of 1024 steps of the range, narrowed to the step it is in
+    int want = drop;  // of the keys within [lo, hi]
+    for (;;) {
+        const int shift = max(0, 22 - __clz((hi - lo) | 1u));  // (hi - lo) >> shift < 1024
+        s_hist[tid] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < EPT; ++r) {
+            if (r >= nr) break;
+            const uint32_t key = key_of(r);
+            if (may_go(r) && key >= lo && key <= hi) atomicAdd(&s_hist[(key - lo) >> shift], 1);
+        }
+        __syncthreads();
+        if (w == 0) {
+            int h[kSteps / kWave], sum = 0;
+#pragma unroll
+            for (int i = 0; i < kSteps / kWave; ++i) {
+                h[i] = s_hist[lane * (kSteps / kWave) + i];
+                sum += h[i];
+            }
+            int incl = sum;
+#pragma unroll
+            for (int o = 1; o < kWave; o <<= 1) {
+                const int y = __shfl_up(incl, o, kWave);
+                if (lane >= o) incl += y;
+            }
+            int at = incl - sum;
+            if (at < want && want <= incl) {
+#pragma unroll
+                for (int i = 0; i < kSteps / kWave; ++i) {
+                    if (at < want && want <= at + h[i]) {
+                        s_step = lane * (kSteps / kWave) + i;
+                        s_below = at;
+                    }
+                    at += h[i];
+                }
+            }
+        }
+        __syncthreads();
+        want -= s_below;
+        lo += (uint32_t)s_step << shift;
+        if (shift == 0) break;
+        hi = min(hi, lo + ((1u << shift) - 1u));
+    }
+    // keys below lo go, and the first `want` ties with it
+    int ties = 0, all;
+#pragma unroll
+    for (int r = 0; r < EPT; ++r) {
+        if (r >= nr) break;
+        below(may_go(r) && key_of(r) == lo, all);
+        ties += all;
+    }
+    if (lane == 0) s_ties[w] = ties;
+    __syncthreads();
+    ties = 0;
+    for (int i = 0; i < w; ++i) ties += s_ties[i];
+    uint32_t go = 0;  // bit r
+    int gone = 0;
+#pragma unroll
+    for (int r = 0; r < EPT; ++r) {
+        if (r >= nr) break;
+        const uint32_t key = key_of(r);
+        const bool tie = may_go(r) && key == lo;
+        const int before = ties + below(tie, all);
+        ties += all;
+        const bool out = may_go(r) && (key < lo || (tie && before < want));
+        go |= (uint32_t)out << r;
+        below(out, all);
+        gone += all;
+    }
+    if (lane == 0) s_gone[w] = gone;
+    __syncthreads();
+    gone = 0;
+    for (int i = 0; i < w; ++i) gone += s_gone[i];
+#pragma unroll
+    for (int r = 0; r < EPT; ++r) {
+        if (r >= nr) break;
+        const int c = first + r * kWave;
+        const bool out = (go >> r) & 1u;
+        const int at = gone + below(out, all);
+        gone += all;
+        if (out) {
+            freed[at] = page[r];
+        } else if (c < nC) {
+            acc[c - at] = s_tot[c];
+            table[c - at] = page[r];
+        }
+    }
+    for (int c = nC - drop + tid; c < nC; c += kEvictBlock) {
+        acc[c] = 0.f;
+        table[c] = -1;
+    }
+}
+
 }  // namespace
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
-    HILS_LAUNCH("k_evict", k_evict, dim3(a.B), dim3(kEvictBlock), 0, s, a);
+    const int nC = a.L / kChunk;
+    const dim3 grid(a.B), block(kEvictBlock);
+    if (nC <= kEvictBlock)
+        HILS_LAUNCH("k_evict", k_evict<1>, grid, block, 0, s, a);
+    else if (nC <= 8 * kEvictBlock)
+        HILS_LAUNCH("k_evict", k_evict<8>, grid, block, 0, s, a);
+    else if (nC <= kMaxHeld)
+        HILS_LAUNCH("k_evict", k_evict<32>, grid, block, 0, s, a);
+    else
+        HILS_LAUNCH("k_evict_long", k_evict_long, grid, block, 0, s, a);
     return hipGetLastError();
 }
 

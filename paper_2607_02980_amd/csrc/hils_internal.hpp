@@ -206,8 +206,10 @@ hipError_t launch_q8_append(const Q8AppendArgs& a, hipStream_t s);
 hipError_t launch_q8_landmark(const Q8LandmarkArgs& a, hipStream_t s);
 size_t q8_decode_workspace_bytes(int B, int N, int Hkv, int G, int d, int L, int K, int W);
 hipError_t launch_q8_decode(const Q8DecodeArgs& a, hipStream_t s);
-hipError_t launch_q8_decode_d64(const Q8DecodeArgs& a, hipStream_t s);
-hipError_t launch_q8_decode_d128(const Q8DecodeArgs& a, hipStream_t s);
+hipError_t launch_q8_decode_bf16_d64(const Q8DecodeArgs& a, hipStream_t s);
+hipError_t launch_q8_decode_bf16_d128(const Q8DecodeArgs& a, hipStream_t s);
+hipError_t launch_q8_decode_f32_d64(const Q8DecodeArgs& a, hipStream_t s);
+hipError_t launch_q8_decode_f32_d128(const Q8DecodeArgs& a, hipStream_t s);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
 hipError_t launch_bwd(const BwdArgs& a, hipStream_t s);
 hipError_t launch_bwd_f32(const BwdArgs& a, hipStream_t s);   // fp32 storage

@@ -156,19 +156,22 @@ __global__ __launch_bounds__(kBlock) void k_q8_append(Q8AppendArgs a, int most) 
 // ---- landmark rows -----------------------------------------------------------------
 //
 // Prop. 3.1 on the stored keys k_j = x_j ks: one wave per (sequence, completed chunk, KV head),
-// the group's landmark heads as MFMA columns: S^T = K Q'^T, the softmax over the lane groups,
-// b' = log l - sum_j p_j s_j (s from its maximum), then sum_j p_j x_j per dim from the wave's
-// copy of K in LDS, P in float32: k' / ks, as e4m3.
-template <typename T, int D, int G>
-struct LmkSmem {
-    uint8_t k[kChunk * D];
-    float p[kChunk][G];
+// the group's GL landmark heads as MFMA columns: S^T = K Q'^T from K rows as they lie in the
+// page, the softmax over the lane groups, b' = log l - sum_j p_j s_j (s from its maximum), and
+// k' / ks = X^T P^T with X^T by transposing reads of the rows, as bf16, in the wave's LDS tile
+// and P in two bf16 terms (2^-17 of it, below e4m3's 2^-4 by far).  Bound by memory: 64 d + GL (d + 4)
+// bytes per wave.  (Products with P on the vector unit, key by key from LDS: 512 chunks of 32
+// heads 18 us, 24 chunks 12 us.)
+template <int D>
+struct LmkTile {
+    static constexpr int ROW = D + 16;  // (transposing reads of padded rows meet two addresses per bank)
+    bf16 x[kChunk * ROW];
 };
-template <typename T, int D, int G>
+template <typename T, int D, int GL>
 __global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int most) {
-    constexpr int DJ = D / 64, LPR = D / 2, TH = kWave / LPR;
-    __shared__ __align__(16) LmkSmem<T, D, G> sm_all[kWaves];
-    LmkSmem<T, D, G>& sm = sm_all[wave_id()];
+    constexpr int DJ = D / 64, DB = D / 16, ROW = LmkTile<D>::ROW;
+    __shared__ __align__(16) LmkTile<D> tiles[kWaves];
+    bf16* tile = tiles[wave_id()].x;
     const int lane = threadIdx.x % kWave, lg = lane / 16, n16 = lane % 16;
     const long unit = (long)blockIdx.x * kWaves + wave_id();
     const int g = (int)(unit % a.Hkv);
@@ -180,31 +183,37 @@ __global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int mo
     if (c >= len / kChunk) return;
     const size_t page = clamp_page(a.block_table[(size_t)b * (a.L / kChunk) + c], a.num_pages);
     const uint8_t* kp = static_cast<const uint8_t*>(a.k_pages) + (page * a.Hkv + g) * kChunk * D;
-    const float ks = a.kv_scale[(page * a.Hkv + g) * 2];
-    const int gl = a.Hl / a.Hkv;  // landmark heads of the group: G or 1
-    // key of row m = 4 a + i of block kb: 16 a + 4 kb + i, so that lane group lg ends with keys 16 lg + 0..15
+    const int hl0 = g * GL;
+    QRow<T, D> q;
+    {
+        const int hl = hl0 + min(n16, GL - 1);
+        const size_t row = a.shared ? hl : ((size_t)b * a.Hl + hl) * most + j;
+        q.load(as<T>(a.lq) + row * D, lg, n16 < GL);
+    }
     uint4 kx[4][DJ];
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
         for (int t = 0; t < DJ; ++t)
-            kx[kb][t] = *reinterpret_cast<const uint4*>(kp + ((n16 / 4) * 16 + kb * 4 + n16 % 4) * D + t * 64 + lg * 16);
-    QRow<T, D> q;
-    {
-        const int hl = g * gl + min(n16, gl - 1);
-        const size_t row = a.shared ? hl : ((size_t)b * a.Hl + hl) * most + j;
-        q.load(as<T>(a.lq) + row * D, lg, n16 < gl);
-    }
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-        for (int t = 0; t < DJ; ++t)
-            *reinterpret_cast<uint4*>(sm.k + ((n16 / 4) * 16 + kb * 4 + n16 % 4) * D + t * 64 + lg * 16) = kx[kb][t];
-    const float c1 = a.scale * ks;
+            kx[kb][t] = *reinterpret_cast<const uint4*>(kp + (kb * 16 + n16) * D + t * 64 + lg * 16);
+    const float c1 = a.scale * a.kv_scale[(page * a.Hkv + g) * 2];
+    // S^T (lane: head n16, keys 16 kb + 4 lg + i)
     float s[16], mx = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
-        const f32x4 st = mfma_row<T, D>(kx[kb], q, zero4());
+        f32x4 st = zero4();
+#pragma unroll
+        for (int t = 0; t < DJ; ++t) {
+            const bf16x8 k0 = bf16x8_of_e4m3(kx[kb][t].x, kx[kb][t].y), k1 = bf16x8_of_e4m3(kx[kb][t].z, kx[kb][t].w);
+            bf16* dst = tile + (kb * 16 + n16) * ROW + t * 64 + lg * 16;
+            *reinterpret_cast<bf16x8*>(dst) = k0;
+            *reinterpret_cast<bf16x8*>(dst + 8) = k1;
+#pragma unroll
+            for (int r = QRow<T, D>::S - 1; r >= 0; --r) {
+                st = mfma16x16x32(k0, q.x[2 * t][r], st);
+                st = mfma16x16x32(k1, q.x[2 * t + 1][r], st);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             s[kb * 4 + i] = st[i] * c1;
@@ -223,38 +232,29 @@ __global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int mo
     l = group4_sum(l);
     ps = group4_sum(ps);
     const float inv = 1.f / l;
-    if (n16 < gl) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sm.p[lg * 16 + i][n16] = s[i] * inv;
-        if (lg == 0) a.bias_pages[page * a.Hl + g * gl + n16] = logf(l) - ps * inv;
-    }
+    if (n16 < GL && lg == 0) a.bias_pages[page * a.Hl + hl0 + n16] = logf(l) - ps * inv;
+    bf16x8 p0[2], p1[2];
+    split_bf16x8<2>(s, p0);
+    split_bf16x8<2>(s + 8, p1);
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int dd = (lane % LPR) * 2, th = lane / LPR;
-    float acc[G][2] = {};
-#pragma unroll 8
-    for (int r = th; r < kChunk; r += TH) {
-        typedef __attribute__((ext_vector_type(2))) float f32x2;
-        const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(*reinterpret_cast<const uint16_t*>(sm.k + r * D + dd), false);
+    // (lane: head n16, dims 16 db + 4 lg + i; a convex combination of codes: above 448 by the
+    // sum's rounding at most, which rounds back to it)
+    f32x4 o[DB];
 #pragma unroll
-        for (int h = 0; h < G; ++h)
-            if (h < gl) {
-                acc[h][0] += sm.p[r][h] * x[0];
-                acc[h][1] += sm.p[r][h] * x[1];
-            }
+    for (int db = 0; db < DB; ++db) {
+        const bf16x8 x0 = tr_operand_perm(tile, ROW, 0, db * 16, lane), x1 = tr_operand_perm(tile, ROW, 32, db * 16, lane);
+        o[db] = mfma16x16x32(x0, p0[1], zero4());
+        o[db] = mfma16x16x32(x1, p1[1], o[db]);
+        o[db] = mfma16x16x32(x0, p0[0], o[db]);
+        o[db] = mfma16x16x32(x1, p1[0], o[db]);
     }
+    if (n16 < GL) {
+        uint8_t* dst = static_cast<uint8_t*>(a.lmk_pages) + (page * a.Hl + hl0 + n16) * D + lg * 4;
 #pragma unroll
-    for (int h = 0; h < G; ++h) {
-        if (h >= gl) break;
-        if constexpr (TH == 2) {
-            acc[h][0] += __shfl_xor(acc[h][0], LPR, kWave);
-            acc[h][1] += __shfl_xor(acc[h][1], LPR, kWave);
-        }
-        // (a convex combination of codes: above 448 by the sum's rounding at most, which rounds back to it)
-        const uint32_t w = f32x4_to_e4m3(acc[h][0], acc[h][1], 0.f, 0.f);
-        if (th == 0)
-            *reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(a.lmk_pages) + (page * a.Hl + g * gl + h) * D + dd) =
-                (uint16_t)w;
+        for (int db = 0; db < DB; ++db)
+            *reinterpret_cast<uint32_t*>(dst + db * 16) =
+                f32x4_to_e4m3(o[db][0] * inv, o[db][1] * inv, o[db][2] * inv, o[db][3] * inv);
     }
 }
 
@@ -280,8 +280,11 @@ struct Q8LandmarkRun {
     static hipError_t run(const Q8LandmarkArgs& a, hipStream_t s) {
         const int most = (a.N + kChunk - 1) / kChunk;  // chunks that N tokens complete, at most
         const long waves = (long)a.B * a.Hkv * most;
-        HILS_LAUNCH("k_q8_landmark", (k_q8_landmark<T, D, G>), dim3((unsigned)((waves + kWaves - 1) / kWaves)),
-                    dim3(kBlock), 0, s, a, most);
+        const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves)), block(kBlock);
+        if (a.Hl == a.Hkv)
+            HILS_LAUNCH("k_q8_landmark", (k_q8_landmark<T, D, 1>), grid, block, 0, s, a, most);
+        else
+            HILS_LAUNCH("k_q8_landmark", (k_q8_landmark<T, D, G>), grid, block, 0, s, a, most);
         return hipGetLastError();
     }
 };

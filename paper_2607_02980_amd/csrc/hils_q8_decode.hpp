@@ -1,9 +1,8 @@
 // HiLS attention decode over the 8-bit cache (layout: hils_q8.hpp), gfx950; compiled once per
-// head dim.  N >= 1 new queries per sequence, each a row (b, g, n) of its own position.
+// storage type and head dim.  N >= 1 new queries per sequence, each a row (b, g, n) of its own position.
 //
-//   A  k_q8_scan     grid (slices, Hkv, B x query groups): s^ of a slice of candidate chunks for
-//                    a KV group's heads on MFMA, A operand the landmark rows as they lie in the
-//                    pages, columns the queries; max over heads, the slice's top-K
+//   A  k_q8_scan     a workgroup per (slice of candidate chunks, KV group, query group): s^ for the
+//                    group's heads, max over heads, the slice's top-K
 //   B  merge         top-K over the slices' survivors, by each wave that needs it
 //   C  k_q8_parts    a wave per part: a selected chunk of one query, or one piece of the window
 //                    for all the queries of a group (16 / G of them, whose (query, head) pairs
@@ -24,7 +23,7 @@ namespace hils {
 
 namespace {
 
-inline DecLayout q8_layout(int B, int N, int Hkv, int G, int d, int L, int K, int W, bool shared) {
+inline DecLayout q8_layout(int B, int N, int Hkv, int G, int d, int L, int K, int W) {
     DecLayout o = {};
     o.nC = L / kChunk;
     o.nlocal = local_pieces_max(W);
@@ -59,18 +58,57 @@ struct __align__(16) Q8ScanSmem {
     int oid[NQ][64], tid[NQ][64];
 };
 
-// Landmark rows of 64 chunks (4 MFMA tiles) of one landmark head against the columns of q.
-template <typename T, int D>
+// Scores of one landmark head's rows (chunks first, first + 64, ... of the slice) for nq queries: the
+// plain products, scales and biases come later.  D / 16 lanes read a row, so that a load covers
+// whole 128-byte lines, non-temporal where a step reads each line once, and the next 64 rows are
+// in flight behind the ones that are multiplied.  (On MFMA, whose operand takes half a row per
+// load and lane group: 65 us against 59, and 87 non-temporal, every line fetched twice; 32
+// sequences of 131K.)
+template <typename T, int D, int NQ, bool STREAM>
+struct ScanRows {
+    static constexpr int LPR = D / 16, RPL = kWave / LPR, NL = 64 / RPL;  // lanes per row, rows per load, loads
+    uint4 x[NL];
+    __device__ __forceinline__ void load(const uint8_t* lmk, const int* page, int r0, int len, int Hl, int hl, int lane) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const uint8_t* src =
+                lmk + ((size_t)page[min(r0 + i * RPL + lane / LPR, len - 1)] * Hl + hl) * D + lane % LPR * 16;
+            x[i] = STREAM ? ld_stream16(src) : *reinterpret_cast<const uint4*>(src);
+        }
+    }
+    // score[q * stride + r0 + row]
+    __device__ __forceinline__ void dot(const float (&q)[NQ][16], float* score, int stride, int r0, int lane) const {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            float y[16];
+            e4m3_to_f32x4(x[i].x, y);
+            e4m3_to_f32x4(x[i].y, y + 4);
+            e4m3_to_f32x4(x[i].z, y + 8);
+            e4m3_to_f32x4(x[i].w, y + 12);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                float part = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) part += y[e] * q[n][e];
+                part = group_sum<LPR>(part);
+                if (lane % LPR == 0) score[n * stride + r0 + i * RPL + lane / LPR] = part;
+            }
+        }
+    }
+};
+
+// Landmarks shared by the group: 64 rows (4 MFMA tiles) against (query, head) columns.  All heads
+// from one read of the row; a wave's VALU would take G products per element.
+template <int D>
 struct LmkBlock {
     uint4 x[4][D / 64];
     __device__ __forceinline__ void load(const uint8_t* lmk, const int* page, int r0, int len, int Hl, int hl, int lg,
-                                         int n16, bool stream) {
+                                         int n16) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const uint8_t* src = lmk + ((size_t)page[min(r0 + t * 16 + n16, len - 1)] * Hl + hl) * D + lg * 16;
 #pragma unroll
-            for (int j = 0; j < D / 64; ++j)
-                x[t][j] = stream ? ld_stream16(src + j * 64) : *reinterpret_cast<const uint4*>(src + j * 64);
+            for (int j = 0; j < D / 64; ++j) x[t][j] = *reinterpret_cast<const uint4*>(src + j * 64);
         }
     }
 };
@@ -79,11 +117,17 @@ template <typename T, int D, int G, int NQ>
 __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout ly, int counters) {
     const FwdArgs& a = qa.f;
     const int ngrp = (a.N + NQ - 1) / NQ;
-    const int b = blockIdx.z / ngrp, n0 = (blockIdx.z % ngrp) * NQ, g = blockIdx.y;
+    // (slice, query group) pairs are dealt to the XCDs (block x runs on XCD x mod 8), a pair's KV
+    // groups one after the other on one: a page's scales of all heads are one line, its
+    // landmarks 4 KB in one place (slices fastest: scan of 32 sequences of 131K 74 us, now 59)
+    const int xcd = blockIdx.x % 8, seq = blockIdx.x / 8, g = seq % a.Hkv, pair = seq / a.Hkv * 8 + xcd;
+    const int slice = pair % ly.nslices, bz = pair / ly.nslices;
+    const int b = bz / ngrp, n0 = (bz % ngrp) * NQ;
+    if (b >= a.B) return;
     const int nq = min(NQ, a.N - n0);
     __shared__ Q8ScanSmem<G, NQ> ss;
     const int tid = threadIdx.x, wave = wave_id(), lane = tid % kWave, lg = lane / 16, n16 = lane % 16;
-    const int c0 = blockIdx.x * ly.slice;
+    const int c0 = slice * ly.slice;
     float* cand_sc = reinterpret_cast<float*>(static_cast<char*>(a.ws) + ly.cand);
     int* cand_id = reinterpret_cast<int*>(cand_sc + (size_t)a.B * a.N * a.Hkv * ly.nslices * a.K);
     auto row_of = [&](int q) { return ((size_t)b * a.Hkv + g) * a.N + n0 + q; };
@@ -91,14 +135,14 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
         return q < nq ? max(0, min(ly.slice, n_candidates(decode_position(a, b, n0 + q), a.W) - c0)) : 0;
     };
     auto clear_counters = [&]() {
-        if (counters && blockIdx.x == 0 && tid < nq) *part_counter<D>(a, ly, row_of(tid), G) = 0;
+        if (counters && slice == 0 && tid < nq) *part_counter<D>(a, ly, row_of(tid), G) = 0;
     };
     int len = 0;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) len = max(len, len_of(q));
     for (int q = 0; q < nq; ++q) {
         if (len_of(q) > 0) continue;
-        const size_t cbase = (row_of(q) * ly.nslices + blockIdx.x) * a.K;
+        const size_t cbase = (row_of(q) * ly.nslices + slice) * a.K;
         for (int t = tid; t < a.K; t += kBlock) {
             cand_sc[cbase + t] = -INFINITY;
             cand_id[cbase + t] = -1;
@@ -128,35 +172,44 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
     }
     const uint8_t* lmk = static_cast<const uint8_t*>(a.lmk);
     const T* qsrc = as<T>(a.q_route ? a.q_route : a.q);
-    const bool stream = a.N <= NQ;
-    // column n16: query n16 of one head, or, the landmarks shared by the group, (query, head)
-    const int gl = shared ? 1 : G;       // landmark heads of the group
-    const int ncol = shared ? nq * G : nq;
-    // units of (landmark head, 64 chunks): wave, wave + 4, ..., the head fastest, so that with
-    // four heads or more a wave keeps its queries
-    const int nblk = (len + 63) / 64, nunits = gl * nblk;
-    if (wave < nunits) {
-        LmkBlock<T, D> cur;
-        QRow<T, D> q;
-        int qh = -1;
-        cur.load(lmk, ss.page, wave / gl * 64, len, a.Hl, shared ? g : g * G + wave % gl, lg, n16, stream);
-        for (int u = wave; u < nunits; u += kBlock / kWave) {
-            const int hh = u % gl, r0 = u / gl * 64;
-            if (hh != qh) {
-                const int col = min(n16, ncol - 1), qq = shared ? col / G : col, h = shared ? col % G : hh;
-                q.load(qsrc + q_row(a, b, g * G + h, n0 + qq) * D, lg, true);
-                qh = hh;
-            }
-            LmkBlock<T, D> nxt;
-            const int un = min(u + kBlock / kWave, nunits - 1);  // (past the end: a block again, discarded)
-            nxt.load(lmk, ss.page, un / gl * 64, len, a.Hl, shared ? g : g * G + un % gl, lg, n16, stream);
+    const int nblk = (len + 63) / 64;
+    if (!shared) {
+        // units of (head, 64 chunks): wave, wave + 4, ..., the head fastest, so that with four
+        // heads or more a wave keeps its queries
+        using Rows = ScanRows<T, D, NQ, NQ == 1>;
+        const int nunits = G * nblk, seg = lane % Rows::LPR;
+        if (wave < nunits) {
+            Rows cur, nxt;
+            float q[NQ][16];
+            int qh = -1;
+            cur.load(lmk, ss.page, wave / G * 64, len, a.Hl, g * G + wave % G, lane);
+            for (int u = wave; u < nunits; u += kBlock / kWave) {
+                const int hh = u % G, un = min(u + kBlock / kWave, nunits - 1);  // (past the end: discarded)
+                if (hh != qh) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const f32x4 s = mfma_row<T, D>(cur.x[t], q, zero4());
-                if (n16 < ncol)
-                    *reinterpret_cast<f32x4*>(&ss.score[shared ? n16 / G : n16][shared ? n16 % G : hh][r0 + t * 16 + lg * 4]) = s;
+                    for (int n = 0; n < NQ; ++n) {
+                        const T* src = qsrc + q_row(a, b, g * G + hh, n0 + min(n, nq - 1)) * D + seg * 16;
+                        load8(src, q[n]);
+                        load8(src + 8, q[n] + 8);
+                    }
+                    qh = hh;
+                }
+                nxt.load(lmk, ss.page, un / G * 64, len, a.Hl, g * G + un % G, lane);
+                cur.dot(q, &ss.score[0][hh][0], G * kSlice, u / G * 64, lane);
+                cur = nxt;
             }
-            cur = nxt;
+        }
+    } else if (wave < nblk) {
+        const int ncol = nq * G, col = min(n16, ncol - 1);
+        QRow<T, D> q;
+        q.load(qsrc + q_row(a, b, g * G + col % G, n0 + col / G) * D, lg, true);
+        LmkBlock<D> x;
+        x.load(lmk, ss.page, wave * 64, len, a.Hl, g, lg, n16);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const f32x4 sc = mfma_row<T, D>(x.x[t], q, zero4());
+            if (n16 < ncol)
+                *reinterpret_cast<f32x4*>(&ss.score[n16 / G][n16 % G][wave * 64 + t * 16 + lg * 4]) = sc;
         }
     }
     __syncthreads();
@@ -186,7 +239,7 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
                 id[r] = ok[r] ? c0 + e : -1;
             }
             const int m = wave_topk_reg<E, kTopkNatural>(sc, id, ok, a.K, ss.oid[q], ss.osc[q], ss.tid[q], ss.tsc[q]);
-            const size_t cbase = (row_of(q) * ly.nslices + blockIdx.x) * a.K;
+            const size_t cbase = (row_of(q) * ly.nslices + slice) * a.K;
             for (int t = lane; t < a.K; t += kWave) {
                 cand_sc[cbase + t] = t < m ? ss.osc[q][t] : -INFINITY;
                 cand_id[cbase + t] = t < m ? ss.oid[q][t] : -1;
@@ -286,18 +339,22 @@ __device__ __forceinline__ void q8_part(const Q8DecodeArgs& qa, const DecLayout&
         uint32_t keep[4];
 #pragma unroll
         for (int w = 0; w < 4; ++w) keep[w] = keys_below(lg * 16 + w * 4, nk);
+        // (every product before the first store, so that the dims' chains of products overlap)
+        f32x4 o[DB];
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
             const bf16x8 v0 = bf16x8_of_e4m3(vx[db].x & keep[0], vx[db].y & keep[1]);
             const bf16x8 v1 = bf16x8_of_e4m3(vx[db].z & keep[2], vx[db].w & keep[3]);
-            f32x4 o = zero4();
+            o[db] = zero4();
 #pragma unroll
             for (int s = PS - 1; s >= 0; --s) {
-                o = mfma16x16x32(v0, p0[s], o);
-                o = mfma16x16x32(v1, p1[s], o);
+                o[db] = mfma16x16x32(v0, p0[s], o[db]);
+                o[db] = mfma16x16x32(v1, p1[s], o[db]);
             }
-            if (store) recs.store4(col.rec + 4 + db * 16 + lg * 4, o * vs);
         }
+        if (store)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) recs.store4(col.rec + 4 + db * 16 + lg * 4, o[db] * vs);
     };
     // the keys of each query (uniform: the same for all)
     auto keys_of = [&](int q) { return __builtin_amdgcn_readlane(col.nk, q * G); };
@@ -314,8 +371,8 @@ __device__ __forceinline__ void q8_part(const Q8DecodeArgs& qa, const DecLayout&
     }
 }
 
-// Fusion of row (b, g, n), records from float offset `off` of recs, by a workgroup of four waves:
-// wave w takes heads w, w + 4, ...  With lambda0 the log mass of the window's pieces, z the scores
+// Fusion of row (b, g, n), records from float offset `off` of recs, by a workgroup of NW waves:
+// wave w takes heads w, w + NW, ...  With lambda0 the log mass of the window's pieces, z the scores
 // of the chunks and L = LSE({z} U {lambda0}): a chunk weighs exp(z - L), a piece its share
 // exp(m + log l - L) of the window; out = sum of weight * o / l.  A part's weights are added
 // over the group's heads.
@@ -324,14 +381,14 @@ struct __align__(16) Q8FuseSmem {
     float w[G][kMaxParts];     // weight / l
     float mass[G][kMaxParts];  // weight
 };
-template <typename T, int D, int G, bool SHARED>
-__device__ void q8_fuse(const Q8DecodeArgs& qa, const DecLayout& ly, Q8FuseSmem<G>& fs, const Recs<SHARED>& recs,
-                        int off, int b, int n, int g) {
+template <typename T, int D, int G, int NW, typename R>
+__device__ void q8_fuse(const Q8DecodeArgs& qa, const DecLayout& ly, Q8FuseSmem<G>& fs, const R& recs, int off, int b,
+                        int n, int g) {
     constexpr int P = kMaxParts / kWave;
     constexpr int RECF = 4 + D, LPP = D / 4, PPL = kWave / LPP, BATCH = 16;
     const FwdArgs& a = qa.f;
     const int lane = threadIdx.x % kWave, d0 = (lane % LPP) * 4, sub = lane / LPP;
-    for (int hh = wave_id(); hh < G; hh += kBlock / kWave) {
+    for (int hh = wave_id(); hh < G; hh += NW) {
         auto part = [&](int j) {
             return recs.load4(off + (min(sub + PPL * j, ly.nparts - 1) * G + hh) * RECF + 4 + d0);
         };
@@ -405,7 +462,7 @@ __device__ void q8_fuse(const Q8DecodeArgs& qa, const DecLayout& ly, Q8FuseSmem<
     if (qa.weights) {
         __syncthreads();
         const size_t rg = ((size_t)b * a.Hkv + g) * a.N + n;
-        for (int pt = threadIdx.x; pt < ly.nparts; pt += kBlock) {
+        for (int pt = threadIdx.x; pt < ly.nparts; pt += NW * kWave) {
             float m = 0.f;
 #pragma unroll
             for (int hh = 0; hh < G; ++hh) m += fs.mass[hh][pt];
@@ -420,7 +477,7 @@ __device__ void q8_fuse(const Q8DecodeArgs& qa, const DecLayout& ly, Q8FuseSmem<
 // merge the scan's survivors themselves (kSoloE: each alone; more: its workgroup, all of one
 // query); 0: idx given.
 template <typename T, int D, int G, int NQP, int E, bool FUSE>
-__global__ __launch_bounds__(kBlock) void k_q8_parts(Q8DecodeArgs qa, DecLayout ly) {
+__global__ __launch_bounds__(kBlock, FUSE || sizeof(T) == 4 ? 1 : 4) void k_q8_parts(Q8DecodeArgs qa, DecLayout ly) {
     constexpr int NW = kBlock / kWave;
     constexpr int kScratch = E > kSoloE ? (int)sizeof(MergeSmem<NW>) : (int)sizeof(MergeSmem<1>) * NW;
     constexpr int kBytes = FUSE && (int)sizeof(Q8FuseSmem<G>) > kScratch ? (int)sizeof(Q8FuseSmem<G>) : kScratch;
@@ -489,7 +546,7 @@ __global__ __launch_bounds__(kBlock) void k_q8_parts(Q8DecodeArgs qa, DecLayout 
     if constexpr (FUSE) {
         if (last_to_arrive(part_counter<D>(a, ly, rg0, G), gridDim.x))
             for (int q = 0; q < nq; ++q)
-                q8_fuse<T, D, G>(qa, ly, *reinterpret_cast<Q8FuseSmem<G>*>(s_raw), recs, q * rowf, b, n0 + q, g);
+                q8_fuse<T, D, G, NW>(qa, ly, *reinterpret_cast<Q8FuseSmem<G>*>(s_raw), recs, q * rowf, b, n0 + q, g);
     }
 }
 
@@ -500,23 +557,498 @@ __global__ __launch_bounds__(kBlock) void k_q8_combine(Q8DecodeArgs qa, DecLayou
     const int g = blockIdx.x, b = blockIdx.y / a.N, n = blockIdx.y % a.N;
     const size_t rg = ((size_t)b * a.Hkv + g) * a.N + n;
     const Recs<false> recs(part_record<D>(a, ly, rg, 0, 0, G), (size_t)ly.nparts * G * (4 + D));
-    q8_fuse<T, D, G>(qa, ly, fs, recs, 0, b, n, g);
+    q8_fuse<T, D, G, kBlock / kWave>(qa, ly, fs, recs, 0, b, n, g);
+}
+
+// The K best of more survivors than a wave takes in one round, by the whole workgroup of row rg:
+// histograms of 1024 steps of the keys' range (keys fall into its steps in order, so everything
+// above the step that holds the K-th is in, everything below it out), narrowed to that step
+// until at most 64 entries are left at or above it, which one wave ranks exactly.  More equal keys than
+// that go the way of the smaller selections.  (2048 survivors: one wave, two rounds of 1024,
+// 1M x 4 step 85 us; now 72.)
+struct __align__(16) Q8BlockMerge {
+    uint32_t lo[kBlock / kWave], hi[kBlock / kWave];
+    int hist[1024];
+    int id[64], oid[64], tid[64];
+    float sc[64], osc[64], tsc[64];
+    int count, step, above;
+};
+template <typename MS>
+__device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, Q8BlockMerge& bm, MS& ms) {
+    constexpr int E = 8;
+    const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave;
+    const float* cand_sc = reinterpret_cast<const float*>(static_cast<const char*>(a.ws) + ly.cand);
+    const int* cand_id = reinterpret_cast<const int*>(cand_sc + (size_t)a.B * a.N * a.Hkv * ly.nslices * a.K);
+    const size_t base = rg * ly.nslices * a.K;
+    const int total = ly.nslices * a.K;
+    // key 0: no entry.  The first kBlock * E survivors stay in registers, the others are read again.
+    uint32_t key0[E];
+    auto key_at = [&](int e) {
+        if (e >= total || cand_id[base + e] < 0) return 0u;
+        const uint32_t k = ordered_key(cand_sc[base + e]);
+        return k ? k : 1u;
+    };
+    uint32_t lo = 0xffffffffu, hi = 0;
+    int n = 0;
+#pragma unroll
+    for (int r = 0; r < E; ++r) key0[r] = key_at(r * kBlock + tid);
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int r = 0; r < E; ++r) f(key0[r], r * kBlock + tid);
+        for (int e = E * kBlock + tid; e - tid < total; e += kBlock) f(key_at(e), e);
+    };
+    each([&](uint32_t k, int) {
+        if (k) {
+            lo = min(lo, k);
+            hi = max(hi, k);
+            ++n;
+        }
+    });
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, kWave));
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, kWave));
+        n += __shfl_xor(n, o, kWave);
+    }
+    if (tid == 0) bm.count = 0;
+    __syncthreads();
+    if (lane == 0) {
+        bm.lo[w] = lo;
+        bm.hi[w] = hi;
+        atomicAdd(&bm.count, n);
+    }
+    __syncthreads();
+    n = bm.count;
+#pragma unroll
+    for (int i = 0; i < kBlock / kWave; ++i) {
+        lo = min(lo, bm.lo[i]);
+        hi = max(hi, bm.hi[i]);
+    }
+    const int m = min(n, a.K);
+    uint32_t from = 1;  // entries with key >= from are left
+    int left = n, want = m;  // of which `want` of the ones within [lo, hi] are among the m best
+    while (left > 64) {
+        const int shift = max(0, 22 - __clz(hi - lo | 1u));  // (hi - lo) >> shift < 1024
+        for (int i = tid; i < 1024; i += kBlock) bm.hist[i] = 0;
+        __syncthreads();
+        each([&](uint32_t k, int) {
+            if (k >= lo && k <= hi) atomicAdd(&bm.hist[(k - lo) >> shift], 1);
+        });
+        __syncthreads();
+        if (w == 0) {  // the step where the count from the top reaches `want`; lane l: steps 1023 - 16 l and down
+            int h[16], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                h[i] = bm.hist[1023 - 16 * lane - i];
+                sum += h[i];
+            }
+            int incl = sum;
+#pragma unroll
+            for (int o = 1; o < kWave; o <<= 1) {
+                const int y = __shfl_up(incl, o, kWave);
+                if (lane >= o) incl += y;
+            }
+            int at = incl - sum;
+            if (at < want && want <= incl) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if (at < want && want <= at + h[i]) {
+                        bm.step = 1023 - 16 * lane - i;
+                        bm.above = at;
+                        bm.count = at + h[i];
+                    }
+                    at += h[i];
+                }
+            }
+        }
+        __syncthreads();
+        left = m - want + bm.count;  // the ones above the range, and the range's down to that step
+        want -= bm.above;
+        lo += (uint32_t)bm.step << shift;
+        from = lo;
+        hi = min(hi, lo + ((1u << shift) - 1u));
+        __syncthreads();
+        if (shift == 0 && left > 64) break;
+    }
+    if (left > 64) {  // ties
+        merge_row<E, kBlock / kWave>(a, ly, rg, ms, w);
+        if (tid < ms.nbest) bm.oid[tid] = ms.bid[tid];
+        __syncthreads();
+        return ms.nbest;
+    }
+    if (tid == 0) bm.count = 0;
+    __syncthreads();
+    each([&](uint32_t k, int e) {
+        if (k >= from) {
+            const int at = atomicAdd(&bm.count, 1);
+            bm.id[at] = cand_id[base + e];
+            bm.sc[at] = cand_sc[base + e];
+        }
+    });
+    __syncthreads();
+    if (w == 0) {
+        const bool ok[1] = {lane < left};
+        const float sc[1] = {ok[0] ? bm.sc[lane] : 0.f};
+        const int id[1] = {ok[0] ? bm.id[lane] : -1};
+        wave_topk_reg<1>(sc, id, ok, a.K, bm.oid, bm.osc, bm.tid, bm.tsc);
+    }
+    __syncthreads();
+    return m;
+}
+
+// One new query per sequence: gridDim.z workgroups of four waves share the parts of a row.  In a
+// workgroup the last wave selects while the others take their share of the window's pieces, then
+// the selected chunks are spread over all four.  A wave adds its parts into one running
+// (maximum, sum, numerator) per head: part t enters with weight exp(z_t - M), z = s^_c for a chunk,
+// whose P is divided by its own sum, and z = m + log l for a piece of the window.  The next part's
+// K, landmark row and V are loaded as soon as the current one is done with their registers (the
+// loads are the same in every iteration, so that the compiler counts the outstanding ones).
+// The waves' results meet in LDS, those of several workgroups in the last of them to arrive.
+// (A wave per part with its record in memory and the fusion in a launch of its own: 1024 rows of
+// 25 parts 99 + 14 us.)
+constexpr int kQ8RowWaves = 4;
+constexpr int kQ8MaxSplit = 8;
+template <typename T>
+__device__ __forceinline__ void q8_store_out(const FwdArgs& a, size_t at, const f32x4& o) {
+    if constexpr (sizeof(T) == 2)
+        store_unaligned(as_mut<bf16>(a.out) + at, make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])));
+    else
+        __builtin_memcpy(as_mut<float>(a.out) + at, &o, 16);
+}
+template <typename T, int D, int G>
+struct Q8RowSmem {
+    float acc[kQ8RowWaves][G][D];
+    float m[kQ8RowWaves][G], z[kQ8RowWaves][G];
+    float part[kMaxParts][G];  // z of each part, log2 units
+    float lse[G];
+    union {
+        MergeSmem<1> ms;
+        MergeSmem<kQ8RowWaves> msb;
+    };
+    int page[64];      // of each slot
+    float ks[64], vs[64];
+};
+template <typename T, int D, int G, int E, bool ROUTE, bool SPLIT>
+__global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs qa, DecLayout ly) {
+    constexpr int NW = kQ8RowWaves, DJ = D / 64, DB = D / 16, PS = sizeof(T) == 2 ? 2 : 3;
+    __shared__ __align__(16) Q8RowSmem<T, D, G> sm;
+    __shared__ Q8BlockMerge bm;
+    const FwdArgs& a = qa.f;
+    const int ns = SPLIT ? gridDim.z : 1, split = SPLIT ? blockIdx.z : 0;
+    const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, w = wave_id(), lane = tid % kWave, lg = lane / 16,
+              n16 = lane % 16;
+    const size_t rg = (size_t)b * a.Hkv + g;
+    const int pos = decode_position(a, b, 0), ncand = n_candidates(pos, a.W);
+    const int hh = min(n16, G - 1), hl = a.Hl == a.Hq ? g * G + hh : g;
+    QRow<T, D> q, qr_;
+    q.load(as<T>(a.q) + q_row(a, b, g * G + hh, 0) * D, lg, n16 < G);
+    if constexpr (ROUTE) qr_.load(as<T>(a.q_route) + q_row(a, b, g * G + hh, 0) * D, lg, n16 < G);
+    const QRow<T, D>& qr = ROUTE ? qr_ : q;
+    f32x4 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db] = zero4();
+    float M = -INFINITY, Z = 0.f;
+
+    struct Regs {
+        uint4 k[4][DJ], l[DJ], v[DB];
+        float bias;
+    } x;
+    // (past a wave's last part `on` is 0 and the lanes of a load read one 16-byte piece; a
+    // multiplication, because the compiler makes a choice a branch, with a wait, around each load)
+    const int koff = ((n16 / 4) * 16 + n16 % 4) * D + lg * 16, voff = n16 * kChunk + lg * 16;
+    auto load_k = [&](size_t page, int on) {
+        const uint8_t* kp = static_cast<const uint8_t*>(a.k) + (page * a.Hkv + g) * kChunk * D;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int j = 0; j < DJ; ++j)
+                x.k[kb][j] = *reinterpret_cast<const uint4*>(kp + koff * on + kb * 4 * D + j * 64);
+    };
+    auto load_l = [&](size_t page, int on) {
+        const uint8_t* lr = static_cast<const uint8_t*>(a.lmk) + (page * a.Hl + hl) * D;
+#pragma unroll
+        for (int j = 0; j < DJ; ++j) x.l[j] = *reinterpret_cast<const uint4*>(lr + lg * 16 * on + j * 64);
+        // (branch-free: without biases a scale is read and not used)
+        x.bias = *(a.bias ? a.bias + page * a.Hl + hl : qa.kv_scale + (page * a.Hkv + g) * 2);
+    };
+    auto load_v = [&](size_t page, int on) {
+        const uint8_t* vp = static_cast<const uint8_t*>(a.v) + (page * a.Hkv + g) * kChunk * D;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            x.v[db] = *reinterpret_cast<const uint4*>(vp + voff * on + db * 16 * kChunk);
+    };
+    // a part's page (-1: nothing there) and scales
+    struct Where {
+        int page;
+        float ks, vs;
+    };
+    auto where = [&](int c) {
+        Where r = {-1, 0.f, 0.f};
+        if (c >= 0) {
+            r.page = page_of(a, ly.nC, b, c);
+            const float* sc = qa.kv_scale + ((size_t)r.page * a.Hkv + g) * 2;
+            r.ks = sc[0];
+            r.vs = sc[1];
+        }
+        return r;
+    };
+
+    // the workgroup's share: window pieces split, split + ns, ... and slots likewise
+    const int npiece = (ly.nlocal - split + ns - 1) / ns, nslot = (a.K - split + ns - 1) / ns;
+    int nsel = 0;
+    if constexpr (E > kSoloE) nsel = q8_merge_block(a, ly, rg, bm, sm.msb);
+    for (int phase = 0; phase < 2; ++phase) {
+        if (phase == 0 && w == NW - 1 && nslot > 0) {
+            int c = -1;  // lane t: the chunk of slot t (K <= 64)
+            if constexpr (E > kSoloE) {
+                c = lane < nsel ? bm.oid[lane] : -1;
+                if (split == 0 && lane < a.K) a.idx[rg * a.K + lane] = c;
+            } else if constexpr (E > 0) {
+                merge_row_wave<E>(a, ly, rg, sm.ms);
+                c = lane < sm.ms.nbest ? sm.ms.bid[lane] : -1;
+                if (split == 0 && lane < a.K) a.idx[rg * a.K + lane] = c;
+            } else {
+                const int32_t* irow = a.idx + rg * a.K;
+                if (lane < a.K && idx_entry_valid(irow, lane, ncand)) c = irow[lane];
+            }
+            const Where r = where(c);
+            sm.page[lane] = r.page;
+            sm.ks[lane] = r.ks;
+            sm.vs[lane] = r.vs;
+        }
+        if (phase == 1) __syncthreads();  // the selection is made
+        const int j0 = phase == 0 && w == NW - 1 ? npiece : w, step = phase == 0 ? NW - 1 : NW;
+        const int nj = phase == 0 ? npiece : nslot;
+        if (j0 >= nj) continue;
+        // lane t: the wave's t-th part (at most 64 pieces or slots, over three or four waves)
+        Where mine = {-1, 0.f, 0.f};
+        {
+            const int j = j0 + lane * step, at = split + j * ns;
+            if (j < nj) {
+                if (phase == 0)
+                    mine = where(ncand + at <= pos / kChunk ? ncand + at : -1);
+                else
+                    mine = {sm.page[at], sm.ks[at], sm.vs[at]};
+            }
+        }
+        {
+            const int page = max(0, __builtin_amdgcn_readlane(mine.page, 0));
+            load_k(page, 1);
+            load_l(page, 1);
+            load_v(page, 1);
+        }
+        for (int j = j0, it = 0; j < nj; j += step, ++it) {
+            const int pg = __builtin_amdgcn_readlane(mine.page, it);
+            const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine.ks), it));
+            const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine.vs), it));
+            const int at = split + j * ns, slot = phase == 0 ? a.K + at : at;
+            const int nk = pg < 0 ? 0 : phase == 0 ? min(kChunk, pos - (ncand + at) * kChunk + 1) : kChunk;
+            const int on = __builtin_amdgcn_readfirstlane((int)(j + step < nj));
+            const int page = max(0, __builtin_amdgcn_readlane(mine.page, it + on));
+            // S^T (lane: column n16, keys 16 lg + 4 kb + i), in log2 units; the next K
+            const float c1 = a.scale * ks * kLog2e;
+            float st[16], mx = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                const f32x4 s4 = mfma_row<T, D>(x.k[kb], q, zero4());
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st[kb * 4 + i] = s4[i] * c1;
+            }
+            load_k(page, on);
+            // s^ of head n16: the diagonal of (landmark rows) x q^, held by lane group n16 / 4
+            const f32x4 d4 = mfma_row<T, D>(x.l, qr, zero4());
+            float dg = d4[0];
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+                if (n16 % 4 == i) dg = d4[i];
+            const float sh = c1 * __shfl(dg, n16 + 16 * (n16 / 4), kWave) + (a.bias ? x.bias * kLog2e : 0.f);
+            load_l(page, on);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                st[i] = lg * 16 + i < nk ? st[i] : -INFINITY;
+                mx = fmaxf(mx, st[i]);
+            }
+            mx = group4_max(mx);
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            float l = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                st[i] = fexp2(st[i] - ref);
+                l += st[i];
+            }
+            l = group4_sum(l);
+            // the part enters the running sums
+            const float z = l == 0.f ? -INFINITY : phase ? sh : mx + __builtin_amdgcn_logf(l);
+            const float Mn = fmaxf(M, z), base = Mn == -INFINITY ? 0.f : Mn;
+            const float corr = fexp2(M - base), zin = fexp2(z - base);
+            const float f = l == 0.f ? 0.f : vs * (phase ? zin / l : fexp2(mx - base));
+            Z = Z * corr + zin;
+            M = Mn;
+            if (n16 < G && lg == 0) sm.part[slot][n16] = z;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] *= corr;
+            // (a part that weighs nothing for any head adds nothing, whatever its values)
+            if (__ballot(f != 0.f) != 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[i] *= f;
+                bf16x8 p0[PS], p1[PS];
+                split_bf16x8<PS>(st, p0);
+                split_bf16x8<PS>(st + 8, p1);
+                uint32_t keep[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) keep[i] = keys_below(lg * 16 + i * 4, nk);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    const bf16x8 v0 = bf16x8_of_e4m3(x.v[db].x & keep[0], x.v[db].y & keep[1]);
+                    const bf16x8 v1 = bf16x8_of_e4m3(x.v[db].z & keep[2], x.v[db].w & keep[3]);
+#pragma unroll
+                    for (int s = PS - 1; s >= 0; --s) {
+                        acc[db] = mfma16x16x32(v0, p0[s], acc[db]);
+                        acc[db] = mfma16x16x32(v1, p1[s], acc[db]);
+                    }
+                }
+            }
+            load_v(page, on);
+        }
+    }
+    // ---- the waves' sums, then the workgroups' ----
+    if (n16 < G) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(&sm.acc[w][n16][db * 16 + lg * 4]) = acc[db];
+        if (lg == 0) {
+            sm.m[w][n16] = M;
+            sm.z[w][n16] = Z;
+        }
+    }
+    __syncthreads();
+    constexpr int RECF = 4 + D;
+    // records {M, Z} and numerators of the row's workgroups, then z of its parts
+    const Recs<true> recs(part_record<D>(a, ly, rg, 0, 0, G), (size_t)ly.nparts * G * RECF);
+    const int zoff = ns * G * RECF;
+    for (int e = tid; e < G * D / 4; e += NW * kWave) {
+        const int h = e / (D / 4), d0 = e % (D / 4) * 4;
+        float m = -INFINITY, z = 0.f;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) m = fmaxf(m, sm.m[i][h]);
+        const float base = m == -INFINITY ? 0.f : m;
+        f32x4 o = zero4();
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            const float c = fexp2(sm.m[i][h] - base);
+            z += c * sm.z[i][h];
+            o += c * *reinterpret_cast<const f32x4*>(&sm.acc[i][h][d0]);
+        }
+        if constexpr (SPLIT) {
+            recs.store4((split * G + h) * RECF + 4 + d0, o);
+            if (d0 == 0) recs.store3((split * G + h) * RECF, m, z, 0.f);
+        } else {
+            q8_store_out<T>(a, q_row(a, b, g * G + h, 0) * D + d0, o * (1.f / z));
+            if (d0 == 0) {
+                sm.lse[h] = m + __builtin_amdgcn_logf(z);
+                a.lse[q_row(a, b, g * G + h, 0)] = (m + __builtin_amdgcn_logf(z)) * (1.f / kLog2e);
+            }
+        }
+    }
+    if constexpr (SPLIT) {
+        auto z_at = [&](int e) { return (zoff + e) * 4; };
+        for (int e = tid; e < ly.nparts * G; e += NW * kWave) {
+            const int pt = e / G;
+            if ((pt < a.K ? pt : pt - a.K) % ns == split)
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint((&sm.part[0][0])[e]), recs.r, z_at(e), 0, Recs<true>::kAux);
+        }
+        if (!last_to_arrive(part_counter<D>(a, ly, rg, G), ns)) return;
+        for (int e = tid; e < G * D / 4; e += NW * kWave) {
+            const int h = e / (D / 4), d0 = e % (D / 4) * 4;
+            f32x4 head[kQ8MaxSplit], num[kQ8MaxSplit];
+#pragma unroll
+            for (int i = 0; i < kQ8MaxSplit; ++i) {
+                const int r = (min(i, ns - 1) * G + h) * RECF;
+                head[i] = recs.load4(r);
+                num[i] = recs.load4(r + 4 + d0);
+            }
+            float m = -INFINITY, z = 0.f;
+#pragma unroll
+            for (int i = 0; i < kQ8MaxSplit; ++i) m = fmaxf(m, head[i][0]);
+            const float base = m == -INFINITY ? 0.f : m;
+            f32x4 o = zero4();
+#pragma unroll
+            for (int i = 0; i < kQ8MaxSplit; ++i)
+                if (i < ns) {
+                    const float c = fexp2(head[i][0] - base);
+                    z += c * head[i][1];
+                    o += c * num[i];
+                }
+            q8_store_out<T>(a, q_row(a, b, g * G + h, 0) * D + d0, o * (1.f / z));
+            if (d0 == 0) {
+                sm.lse[h] = m + __builtin_amdgcn_logf(z);
+                a.lse[q_row(a, b, g * G + h, 0)] = (m + __builtin_amdgcn_logf(z)) * (1.f / kLog2e);
+            }
+        }
+        if (qa.weights)
+            for (int e = tid; e < ly.nparts * G; e += NW * kWave)
+                (&sm.part[0][0])[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(recs.r, z_at(e), 0, Recs<true>::kAux));
+    }
+    if (qa.weights) {
+        __syncthreads();
+        for (int pt = tid; pt < ly.nparts; pt += NW * kWave) {
+            float sum = 0.f;
+#pragma unroll
+            for (int h = 0; h < G; ++h) sum += fexp2(sm.part[pt][h] - sm.lse[h]);
+            qa.weights[rg * ly.nparts + pt] = sum;
+        }
+    }
 }
 
 struct Q8DecRun {
-    template <typename T, int D, int G, int NQS, int NQP>
-    static hipError_t go(const Q8DecodeArgs& qa, hipStream_t s) {
+    template <typename T, int D, int G>
+    static hipError_t run(const Q8DecodeArgs& qa, hipStream_t s) {
         const FwdArgs& a = qa.f;
-        const DecLayout ly = q8_layout(a.B, a.N, a.Hkv, G, D, a.L, a.K, a.W, a.Hl != a.Hq);
-        const int R = a.B * a.N, cus = device_cus();
-        constexpr int NW = kBlock / kWave;
+        const DecLayout ly = q8_layout(a.B, a.N, a.Hkv, G, D, a.L, a.K, a.W);
+        const int R = a.B * a.N, cus = device_cus(), surv = ly.nslices * a.K;
+        auto scan = [&](auto many_tag, int counters) {
+            constexpr int NQ = scan_queries<G>(decltype(many_tag)::value);
+            const int pairs = ly.nslices * a.B * ((a.N + NQ - 1) / NQ);
+            if (!a.given_idx)
+                HILS_LAUNCH("k_q8_scan", (k_q8_scan<T, D, G, NQ>), dim3((pairs + 7) / 8 * 8 * a.Hkv), dim3(kBlock), 0, s,
+                            qa, ly, counters);
+        };
+        if (a.N == 1) {
+            // Two workgroups per CU hold the chip's registers; with fewer rows than that a row
+            // goes over several, down to a part per wave.  (A given selection comes without the
+            // scan that clears the arrival counters: one workgroup per row.)
+            const int ns = a.given_idx ? 1 : std::max(1, std::min({kQ8MaxSplit, (ly.nparts + 3) / 4, 2 * cus / (R * a.Hkv)}));
+            scan(std::false_type{}, ns > 1);
+            const dim3 grid(a.Hkv, a.B, ns), block(kQ8RowWaves * kWave);
+            auto row = [&](auto e_tag, auto route_tag) {
+                constexpr int EE = decltype(e_tag)::value;
+                constexpr bool RR = decltype(route_tag)::value;
+                if constexpr (EE > 0)
+                    if (ns > 1) {
+                        HILS_LAUNCH("k_q8_row", (k_q8_row<T, D, G, EE, RR, true>), grid, block, 0, s, qa, ly);
+                        return;
+                    }
+                HILS_LAUNCH("k_q8_row", (k_q8_row<T, D, G, EE, RR, false>), grid, block, 0, s, qa, ly);
+            };
+            auto by_route = [&](auto e_tag) {
+                if (a.q_route) row(e_tag, std::true_type{});
+                else row(e_tag, std::false_type{});
+            };
+            // (survivors a wave selects from in one round: 64 per unit of E)
+            if (a.given_idx)
+                by_route(std::integral_constant<int, 0>{});
+            else if (surv <= kWave * 4)
+                by_route(std::integral_constant<int, 4>{});
+            else
+                by_route(std::integral_constant<int, 16>{});
+            return hipGetLastError();
+        }
+        constexpr int NW = kBlock / kWave, NQP = MqCfg<G>::NQ;
         const int KP = (a.K + NW - 1) / NW * NW;
+        // up to 8 parts per CU the last workgroup to arrive fuses, as in k_dec_parts_w
         const bool fuse = !a.given_idx && (long)R * a.Hkv * ly.nparts <= 8l * cus;
-        if (!a.given_idx)
-            HILS_LAUNCH("k_q8_scan", (k_q8_scan<T, D, G, NQS>),
-                        dim3(ly.nslices, a.Hkv, a.B * ((a.N + NQS - 1) / NQS)), dim3(kBlock), 0, s, qa, ly, fuse);
+        scan(std::true_type{}, fuse);
         // (queries of a group sit within one chunk's length of each other: one more piece at most)
-        const int units = NQP * KP + ly.nlocal + (NQP > 1 ? 1 : 0);
+        const int units = NQP * KP + ly.nlocal + 1;
         const dim3 grid((units + NW - 1) / NW, a.Hkv, a.B * ((a.N + NQP - 1) / NQP));
         auto parts = [&](auto e_tag) {
             constexpr int EE = decltype(e_tag)::value;
@@ -529,29 +1061,21 @@ struct Q8DecRun {
             HILS_LAUNCH("k_q8_parts", (k_q8_parts<T, D, G, NQP, EE, false>), grid, dim3(kBlock), 0, s, qa, ly);
             HILS_LAUNCH("k_q8_combine", (k_q8_combine<T, D, G>), dim3(a.Hkv, R), dim3(kBlock), 0, s, qa, ly);
         };
-        const int surv = ly.nslices * a.K;
         if (a.given_idx)
             parts(std::integral_constant<int, 0>{});
         else if (surv <= kWave * kSoloE)
             parts(std::integral_constant<int, kSoloE>{});
-        else if (surv <= kBlock * 8)
-            parts(std::integral_constant<int, 8>{});
         else
-            parts(std::integral_constant<int, 16>{});
+            parts(std::integral_constant<int, 8>{});
         return hipGetLastError();
-    }
-    template <typename T, int D, int G>
-    static hipError_t run(const Q8DecodeArgs& qa, hipStream_t s) {
-        if (qa.f.N == 1) return go<T, D, G, 1, 1>(qa, s);
-        return go<T, D, G, scan_queries<G>(true), MqCfg<G>::NQ>(qa, s);
     }
 };
 
-template <int D>
+template <typename T, int D>
 hipError_t dispatch_q8_decode(const Q8DecodeArgs& qa, hipStream_t s) {
     const int G = qa.f.Hq / qa.f.Hkv;
 #define HILS_CASE(GG) \
-    if (G == GG) return qa.f.bf16 ? Q8DecRun::run<bf16, D, GG>(qa, s) : Q8DecRun::run<float, D, GG>(qa, s);
+    if (G == GG) return Q8DecRun::run<T, D, GG>(qa, s);
     HILS_CASE(1) HILS_CASE(2) HILS_CASE(4) HILS_CASE(8)
 #undef HILS_CASE
     return hipErrorInvalidValue;

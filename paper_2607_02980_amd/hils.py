@@ -14,7 +14,6 @@ if ``libhils.so`` is missing or fails to load, importing this module raises.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 from dataclasses import dataclass
 
@@ -341,24 +340,42 @@ def hils_landmark_bwd(p: Params, lq, k, dlmk, dlmk_bias=None, dlq=None, dk=None,
 
 
 # ---- the 8-bit cache: k_pages [P, Hkv, S, d], v_pages [P, Hkv, d, S] and lmk_pages [P, Hl, d] are
-# torch.float8_e4m3fn, kv_scale [P, Hkv, 2] and bias_pages [P, Hl] float32, block_table [B, L/S] int32
+# torch.float8_e4m3fn, kv_scale [P, Hkv, 2] and bias_pages [P, Hl] float32, block_table [B, L/S] int32.
+# A single-token step of a small batch takes the GPU about as long as these checks take the host, so
+# each tensor is looked at once and its address passed as an int.
+
+_F8, _F32, _I32 = torch.float8_e4m3fn, torch.float32, torch.int32
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _on_device_of(fn):
-    """The call with its first tensor's device current (the kernels run there, on that device's current stream)."""
-    @functools.wraps(fn)
-    def call(p, t, *args, **kw):
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
-            with torch.cuda.device(t.device):
-                return fn(p, t, *args, **kw)
-        return fn(p, t, *args, **kw)
-    return call
+def _address(t, name, shape, dtype, dev):
+    """The address of a contiguous tensor of this shape and type on device number dev."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _ptr(t, name, shape, dtype)  # says what is wrong
+    raise ValueError(f"{name} is on {t.device}, expected cuda:{dev}")
 
 
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, expected {dev}")
+def _gpu(t, name):
+    """Number of the device that a call runs on: its first tensor's."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    return t.get_device()
+
+
+def _run(fn, dev, *args):
+    """The C call on device dev (made current for it) and that device's current stream."""
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _raw_stream(dev))
+    if rc:
+        _check(rc)
 
 
 def hils_window_pieces(window: int) -> int:
@@ -366,84 +383,72 @@ def hils_window_pieces(window: int) -> int:
     return (window + 62) // 64 + 1
 
 
-@_on_device_of
 def hils_q8_append(p: Params, k_new, v_new, k_pages, v_pages, kv_scale, block_table, seqlens=None, newlens=None):
     """Write new tokens into the 8-bit cache: sequence b's first newlens[b] rows of k_new, v_new
     [B, Hkv, N, d] go to its last newlens[b] positions (seqlens counts them).  Changes k_pages,
     v_pages and kv_scale in place and returns them."""
-    dt, n = p.torch_dtype, k_pages.shape[0]
-    new = (p.B, p.Hkv, p.N, p.d)
-    cp = p.c()
-    args = (_ptr(k_new, "k_new", new, dt), _ptr(v_new, "v_new", new, dt),
-            _ptr(k_pages, "k_pages", (n, p.Hkv, p.chunk, p.d), torch.float8_e4m3fn),
-            _ptr(v_pages, "v_pages", (n, p.Hkv, p.d, p.chunk), torch.float8_e4m3fn),
-            _ptr(kv_scale, "kv_scale", (n, p.Hkv, 2), torch.float32),
-            _ptr(block_table, "block_table", (p.B, p.L // p.chunk), torch.int32), n,
-            _ptr(seqlens, "seqlens", (p.B,), torch.int32, False), _ptr(newlens, "newlens", (p.B,), torch.int32, False))
-    _same_device(k_new.device, v_new=v_new, k_pages=k_pages, v_pages=v_pages, kv_scale=kv_scale,
-                 block_table=block_table, seqlens=seqlens, newlens=newlens)
-    _check(LIB.hils_q8_append(ctypes.byref(cp), *args, _stream()))
+    dev, dt, B, H, d, S = _gpu(k_new, "k_new"), p.torch_dtype, p.B, p.Hkv, p.d, p.chunk
+    new, n = (B, H, p.N, d), k_pages.shape[0]
+    _run(LIB.hils_q8_append, dev, ctypes.byref(p.c()), _address(k_new, "k_new", new, dt, dev),
+         _address(v_new, "v_new", new, dt, dev), _address(k_pages, "k_pages", (n, H, S, d), _F8, dev),
+         _address(v_pages, "v_pages", (n, H, d, S), _F8, dev), _address(kv_scale, "kv_scale", (n, H, 2), _F32, dev),
+         _address(block_table, "block_table", (B, p.L // S), _I32, dev), n,
+         None if seqlens is None else _address(seqlens, "seqlens", (B,), _I32, dev),
+         None if newlens is None else _address(newlens, "newlens", (B,), _I32, dev))
     return k_pages, v_pages, kv_scale
 
 
-@_on_device_of
 def hils_q8_landmark_fwd(p: Params, lq, k_pages, kv_scale, block_table, lmk_pages, bias_pages, seqlens=None,
                          newlens=None):
     """Landmark rows and biases of the chunks that each sequence's last newlens[b] tokens completed, from
     the stored keys: lq [B, Hl, (N + S - 1) // S, d] (one query per completed chunk) or [Hl, d] under
     HILS_FLAG_SHARED_LMK_QUERY.  Changes lmk_pages and bias_pages in place and returns them."""
-    dt, n, Hl = p.torch_dtype, k_pages.shape[0], p.Hl or p.Hq
-    lqs = (Hl, p.d) if p.flags & HILS_FLAG_SHARED_LMK_QUERY else (p.B, Hl, (p.N + p.chunk - 1) // p.chunk, p.d)
-    cp = p.c()
-    args = (_ptr(lq, "lq", lqs, dt), _ptr(k_pages, "k_pages", (n, p.Hkv, p.chunk, p.d), torch.float8_e4m3fn),
-            _ptr(kv_scale, "kv_scale", (n, p.Hkv, 2), torch.float32),
-            _ptr(block_table, "block_table", (p.B, p.L // p.chunk), torch.int32), n,
-            _ptr(seqlens, "seqlens", (p.B,), torch.int32, False), _ptr(newlens, "newlens", (p.B,), torch.int32, False),
-            _ptr(lmk_pages, "lmk_pages", (n, Hl, p.d), torch.float8_e4m3fn),
-            _ptr(bias_pages, "bias_pages", (n, Hl), torch.float32))
-    _same_device(lq.device, k_pages=k_pages, kv_scale=kv_scale, block_table=block_table, seqlens=seqlens,
-                 newlens=newlens, lmk_pages=lmk_pages, bias_pages=bias_pages)
-    _check(LIB.hils_q8_landmark_fwd(ctypes.byref(cp), *args, _stream()))
+    dev, B, H, Hl, d, S = _gpu(lq, "lq"), p.B, p.Hkv, p.Hl or p.Hq, p.d, p.chunk
+    n, lqs = k_pages.shape[0], (Hl, d) if p.flags & HILS_FLAG_SHARED_LMK_QUERY else (B, Hl, (p.N + S - 1) // S, d)
+    _run(LIB.hils_q8_landmark_fwd, dev, ctypes.byref(p.c()), _address(lq, "lq", lqs, p.torch_dtype, dev),
+         _address(k_pages, "k_pages", (n, H, S, d), _F8, dev), _address(kv_scale, "kv_scale", (n, H, 2), _F32, dev),
+         _address(block_table, "block_table", (B, p.L // S), _I32, dev), n,
+         None if seqlens is None else _address(seqlens, "seqlens", (B,), _I32, dev),
+         None if newlens is None else _address(newlens, "newlens", (B,), _I32, dev),
+         _address(lmk_pages, "lmk_pages", (n, Hl, d), _F8, dev), _address(bias_pages, "bias_pages", (n, Hl), _F32, dev))
     return lmk_pages, bias_pages
 
 
-@_on_device_of
 def hils_decode_q8_fwd(p: Params, q, k_pages, v_pages, kv_scale, lmk_pages, block_table, bias_pages=None, q_route=None,
                        seqlens=None, out=None, lse=None, idx=None, weights=None, want_weights=True, workspace=None):
     """Decode forward over the 8-bit cache, N >= 1 new queries per sequence.  Returns (out, lse, idx, weights);
     weights [B, Hkv, N, K + hils_window_pieces(W)] float32 (None without want_weights): each selected chunk's
     and window piece's attention weight, summed over the group's heads."""
-    S, dt, f8, n, Hl = _shapes(p), p.torch_dtype, torch.float8_e4m3fn, k_pages.shape[0], p.Hl or p.Hq
-    dev = q.device
-    ws_shape = (p.B, p.Hkv, p.N, p.topk + hils_window_pieces(p.window))
+    dev, dt, B, Hq, H, N, d, S = _gpu(q, "q"), p.torch_dtype, p.B, p.Hq, p.Hkv, p.N, p.d, p.chunk
+    n, Hl, qs, K = k_pages.shape[0], p.Hl or p.Hq, (B, Hq, N, d), p.topk
+    on = q.device
     if out is None:
-        out = torch.empty(S["q"], dtype=dt, device=dev)
+        out = torch.empty(qs, dtype=dt, device=on)
     if lse is None:
-        lse = torch.empty(S["lse"], dtype=torch.float32, device=dev)
+        lse = torch.empty((B, Hq, N), dtype=_F32, device=on)
     if idx is None:
         if p.flags & HILS_FLAG_GIVEN_IDX:
             raise ValueError("HILS_FLAG_GIVEN_IDX needs idx")
-        idx = torch.empty(S["idx"], dtype=torch.int32, device=dev)
+        idx = torch.empty((B, H, N, K), dtype=_I32, device=on)
+    wshape = (B, H, N, K + hils_window_pieces(p.window))
     if weights is None and want_weights:
-        weights = torch.empty(ws_shape, dtype=torch.float32, device=dev)
-    ws, nbytes = _workspace(p, HILS_OP_DECODE_Q8, workspace)
-    cp = p.c()
-    args = (_ptr(q, "q", S["q"], dt), _ptr(k_pages, "k_pages", (n, p.Hkv, p.chunk, p.d), f8),
-            _ptr(v_pages, "v_pages", (n, p.Hkv, p.d, p.chunk), f8),
-            _ptr(kv_scale, "kv_scale", (n, p.Hkv, 2), torch.float32), _ptr(lmk_pages, "lmk_pages", (n, Hl, p.d), f8),
-            _ptr(bias_pages, "bias_pages", (n, Hl), torch.float32, False), _ptr(q_route, "q_route", S["q"], dt, False),
-            _ptr(block_table, "block_table", (p.B, p.L // p.chunk), torch.int32), n,
-            _ptr(seqlens, "seqlens", (p.B,), torch.int32, False), _ptr(out, "out", S["q"], dt),
-            _ptr(lse, "lse", S["lse"], torch.float32), _ptr(idx, "idx", S["idx"], torch.int32),
-            _ptr(weights, "weights", ws_shape, torch.float32, False), _ptr(ws, "workspace"), nbytes)
-    _same_device(dev, k_pages=k_pages, v_pages=v_pages, kv_scale=kv_scale, lmk_pages=lmk_pages, bias_pages=bias_pages,
-                 q_route=q_route, block_table=block_table, seqlens=seqlens, out=out, lse=lse, idx=idx,
-                 weights=weights, workspace=ws)
-    _check(LIB.hils_decode_q8_fwd(ctypes.byref(cp), *args, _stream()))
+        weights = torch.empty(wshape, dtype=_F32, device=on)
+    if workspace is None:
+        workspace = torch.empty(max(1, hils_workspace_size(p, HILS_OP_DECODE_Q8)), dtype=torch.uint8, device=on)
+    nbytes = workspace.numel()  # the library says if that is too little
+    _run(LIB.hils_decode_q8_fwd, dev, ctypes.byref(p.c()), _address(q, "q", qs, dt, dev),
+         _address(k_pages, "k_pages", (n, H, S, d), _F8, dev), _address(v_pages, "v_pages", (n, H, d, S), _F8, dev),
+         _address(kv_scale, "kv_scale", (n, H, 2), _F32, dev), _address(lmk_pages, "lmk_pages", (n, Hl, d), _F8, dev),
+         None if bias_pages is None else _address(bias_pages, "bias_pages", (n, Hl), _F32, dev),
+         None if q_route is None else _address(q_route, "q_route", qs, dt, dev),
+         _address(block_table, "block_table", (B, p.L // S), _I32, dev), n,
+         None if seqlens is None else _address(seqlens, "seqlens", (B,), _I32, dev), _address(out, "out", qs, dt, dev),
+         _address(lse, "lse", (B, Hq, N), _F32, dev), _address(idx, "idx", (B, H, N, K), _I32, dev),
+         None if weights is None else _address(weights, "weights", wshape, _F32, dev),
+         _address(workspace, "workspace", (nbytes,), torch.uint8, dev), nbytes)
     return out, lse, idx, weights
 
 
-@_on_device_of
 def hils_cache_evict(p: Params, acc, block_table, seqlens=None, budget=0, sink=0, max_evict=None, weights=None,
                      idx=None, acc_out=None, table_out=None, seqlens_out=None, freed=None, nfreed=None):
     """Add a decode call's weights (and idx) to the chunks' totals acc [B, L/S], then cut every sequence to
@@ -451,26 +456,29 @@ def hils_cache_evict(p: Params, acc, block_table, seqlens=None, budget=0, sink=0
     max_evict (None: any number).  Returns (acc, block_table, seqlens, freed, nfreed), new tensors unless
     outputs are given (the inputs themselves for a call in place); the pages given up by sequence b are
     freed[b, :nfreed[b]]."""
-    nc, dev, i32 = p.L // p.chunk, acc.device, torch.int32
-    most = nc if max_evict is None else max_evict
-    ws_shape = (p.B, p.Hkv, p.N, p.topk + hils_window_pieces(p.window))
     if weights is not None and idx is None:
         raise ValueError("weights needs idx")
-    acc_out = torch.empty_like(acc) if acc_out is None else acc_out
-    table_out = torch.empty_like(block_table) if table_out is None else table_out
-    seqlens_out = torch.empty(p.B, dtype=i32, device=dev) if seqlens_out is None else seqlens_out
-    freed = torch.empty((p.B, most), dtype=i32, device=dev) if freed is None else freed
-    nfreed = torch.empty(p.B, dtype=i32, device=dev) if nfreed is None else nfreed
-    cp = p.c()
-    args = (_ptr(acc, "acc", (p.B, nc), torch.float32), _ptr(block_table, "block_table", (p.B, nc), i32),
-            _ptr(seqlens, "seqlens", (p.B,), i32, False), _ptr(weights, "weights", ws_shape, torch.float32, False),
-            _ptr(idx, "idx", (p.B, p.Hkv, p.N, p.topk), i32, False) if weights is not None else None, budget, sink, most,
-            _ptr(acc_out, "acc_out", (p.B, nc), torch.float32), _ptr(table_out, "table_out", (p.B, nc), i32),
-            _ptr(seqlens_out, "seqlens_out", (p.B,), i32), _ptr(freed, "freed", (p.B, most), i32),
-            _ptr(nfreed, "nfreed", (p.B,), i32))
-    _same_device(dev, block_table=block_table, seqlens=seqlens, weights=weights, idx=idx, acc_out=acc_out,
-                 table_out=table_out, seqlens_out=seqlens_out, freed=freed, nfreed=nfreed)
-    _check(LIB.hils_cache_evict(ctypes.byref(cp), *args, _stream()))
+    dev, B, nc = _gpu(acc, "acc"), p.B, p.L // p.chunk
+    most, on = nc if max_evict is None else max_evict, acc.device
+    if acc_out is None:
+        acc_out = torch.empty_like(acc)
+    if table_out is None:
+        table_out = torch.empty_like(block_table)
+    if seqlens_out is None:
+        seqlens_out = torch.empty(B, dtype=_I32, device=on)
+    if freed is None:
+        freed = torch.empty((B, most), dtype=_I32, device=on)
+    if nfreed is None:
+        nfreed = torch.empty(B, dtype=_I32, device=on)
+    _run(LIB.hils_cache_evict, dev, ctypes.byref(p.c()), _address(acc, "acc", (B, nc), _F32, dev),
+         _address(block_table, "block_table", (B, nc), _I32, dev),
+         None if seqlens is None else _address(seqlens, "seqlens", (B,), _I32, dev),
+         None if weights is None else
+         _address(weights, "weights", (B, p.Hkv, p.N, p.topk + hils_window_pieces(p.window)), _F32, dev),
+         None if weights is None else _address(idx, "idx", (B, p.Hkv, p.N, p.topk), _I32, dev), budget, sink, most,
+         _address(acc_out, "acc_out", (B, nc), _F32, dev), _address(table_out, "table_out", (B, nc), _I32, dev),
+         _address(seqlens_out, "seqlens_out", (B,), _I32, dev), _address(freed, "freed", (B, most), _I32, dev),
+         _address(nfreed, "nfreed", (B,), _I32, dev))
     return acc_out, table_out, seqlens_out, freed, nfreed
 
 

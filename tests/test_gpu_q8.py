@@ -350,6 +350,8 @@ EVICT = {
     "none": (dict(B=2, Hq=2, Hkv=1, N=1, L=64 * 50, d=64, topk=4, window=128), [3200, 1], 1000, 0, None),
     "zero_most": (dict(B=1, Hq=2, Hkv=1, N=1, L=64 * 50, d=64, topk=4, window=128), None, 1, 0, 0),
     "sinks_past_the_end": (dict(B=1, Hq=2, Hkv=1, N=1, L=64 * 9, d=64, topk=4, window=128), [500], 0, 100, None),
+    # more chunks than the totals of which fit in LDS
+    "long": (dict(B=1, Hq=4, Hkv=2, N=2, L=64 * 33001, d=64, topk=16, window=512), None, 9000, 3, None),
     "tiles": (dict(B=2, Hq=4, Hkv=2, N=2, L=64 * 5001, d=64, topk=64, window=4032), [64 * 5001 - 5, 64 * 3500], 1800, 3, None),
 }
 
@@ -410,6 +412,29 @@ def test_evict_special_totals():
     for budget, gone in ((7, [3]), (6, [0, 3]), (5, [0, 1, 3]), (1, [0, 1, 3, 4, 5, 6, 7])):
         got = hils.hils_cache_evict(p, dev(acc), dev(table), budget=budget)
         assert got[3][0, :len(gone)].tolist() == [20 + c for c in gone] and got[4].tolist() == [len(gone)]
+
+
+def test_evict_negative_nan():
+    """A NaN total stays whatever its sign bit."""
+    hils = hils_()
+    p = hils.Params(B=1, Hq=1, Hkv=1, N=1, L=64 * 9, d=64, topk=1, window=64)
+    acc = np.arange(9, dtype=np.float32)[None]
+    acc.view(np.uint32)[0, 4] = 0xffc00000
+    got = hils.hils_cache_evict(p, dev(acc), torch.arange(9, dtype=torch.int32, device="cuda")[None], budget=1)
+    assert got[3][0, :7].tolist() == [0, 1, 2, 3, 5, 6, 7]
+
+
+@pytest.mark.parametrize("n", [1, 3])
+def test_decode_ties_everywhere(n):
+    """Equal scores of every candidate: the lowest chunks are chosen, however many survivors tie."""
+    hils = hils_()
+    p = hils.Params(B=1, Hq=2, Hkv=2, N=n, L=64 * 1500, d=64, topk=60, window=128, scale=0.125)
+    t = world(p, 31)
+    t["lmk"][:] = 0
+    ref = Q.decode(p, t["q"], t["k"], t["v"], t["scale"], t["lmk"], t["table"])
+    got = run_decode(p, t)
+    check_decode(p, got, ref)
+    assert got[2][0, 0, 0].tolist() == list(range(60))
 
 
 def test_a_sequence_lives():
