@@ -20,7 +20,7 @@ namespace {
 
 constexpr int kEvictBlock = 1024;
 constexpr int kEvictWaves = kEvictBlock / kWave;
-constexpr int kMaxHeld = 32 * kEvictBlock;  // chunks: totals of 128 KB in LDS
+constexpr int kMaxHeld = 20 * kEvictBlock;  // chunks (1.3M tokens): totals of 80 KB in LDS
 
 // How many lanes below have x, and how many of the wave.
 __device__ __forceinline__ int below(bool x, int& all) {
@@ -29,8 +29,10 @@ __device__ __forceinline__ int below(bool x, int& all) {
     return popc64(m & ((1ull << __lane_id()) - 1ull));
 }
 
-// Order of the totals: -0 as 0, a NaN above every number (such a chunk stays while another can go).
-__device__ __forceinline__ uint32_t total_key(float x) { return x != x ? 0xffffffffu : ordered_key(x + 0.f); }
+// Order of the totals: -0 as 0, a NaN above every number (such a chunk stays while another can go);
+// below 0xffffffff.  And the total of a number's key.
+__device__ __forceinline__ uint32_t total_key(float x) { return x != x ? 0xfffffffeu : ordered_key(x + 0.f); }
+__device__ __forceinline__ float key_total(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
 __global__ __launch_bounds__(kEvictBlock) void k_evict_long(EvictArgs a) {
     __shared__ int s_hist[256];
@@ -172,8 +174,8 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
     constexpr int NW = kEvictWaves, kSteps = 1024;
     __shared__ float s_tot[EPT * kEvictBlock];
     __shared__ int s_hist[kSteps];
-    __shared__ uint32_t s_lo[NW], s_hi[NW];
-    __shared__ int s_step, s_below, s_ties[NW], s_gone[NW];
+    __shared__ uint32_t s_lo[NW], s_hi[NW], s_list[kWave];
+    __shared__ int s_step, s_below, s_in, s_ties[NW], s_gone[NW];
     const int b = blockIdx.x, tid = threadIdx.x, w = wave_id(), lane = tid % kWave;
     const int nC = a.L / kChunk, nr = (nC + kEvictBlock - 1) / kEvictBlock, first = w * kWave * nr + lane;
     const float* acc_in = a.acc + (size_t)b * nC;
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
     int32_t page[EPT];
 #pragma unroll
     for (int r = 0; r < EPT; ++r) {
-        if (r >= nr) break;
+        if (r >= nr) continue;
         const int c = first + r * kWave;
         s_tot[c] = c < nC ? acc_in[c] : 0.f;
         page[r] = c < nC ? table_in[c] : -1;
@@ -226,7 +228,7 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
     if (drop == 0) {
 #pragma unroll
         for (int r = 0; r < EPT; ++r) {
-            if (r >= nr) break;
+            if (r >= nr) continue;
             const int c = first + r * kWave;
             if (c < nC) {
                 acc[c] = s_tot[c];
@@ -235,46 +237,57 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
         }
         return;
     }
-    // keys of the chunks that may go (from LDS each time: 32 of them and the pages are too many registers)
-    auto key_of = [&](int r) { return total_key(s_tot[first + r * kWave]); };
-    auto may_go = [&](int r) { return first + r * kWave >= a.sink && first + r * kWave < last; };
-    uint32_t lo = 0xffffffffu, hi = 0;
+    // keys of the chunks that may go; kStays for the others
+    constexpr uint32_t kStays = 0xffffffffu;
+    uint32_t key[EPT];
+    uint32_t lo = kStays, hi = 0;
 #pragma unroll
     for (int r = 0; r < EPT; ++r) {
-        if (r >= nr) break;
-        if (may_go(r)) {
-            const uint32_t key = key_of(r);
-            lo = min(lo, key);
-            hi = max(hi, key);
+        const int c = first + r * kWave;
+        const bool may = r < nr && c >= a.sink && c < last;
+        key[r] = may ? total_key(s_tot[c]) : kStays;
+        lo = min(lo, key[r]);
+        hi = max(hi, may ? key[r] : 0u);
+    }
+    // least and greatest key within [from, to]
+    auto range = [&]() {
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) {
+            lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, kWave));
+            hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, kWave));
         }
-    }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, kWave));
-        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, kWave));
-    }
-    if (lane == 0) {
-        s_lo[w] = lo;
-        s_hi[w] = hi;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-        lo = min(lo, s_lo[i]);
-        hi = max(hi, s_hi[i]);
-    }
-    // the drop-th smallest key: histograms of 1024 steps of the range, narrowed to the step it is in
-    int want = drop;  // of the keys within [lo, hi]
-    for (;;) {
-        const int shift = max(0, 22 - __clz((hi - lo) | 1u));  // (hi - lo) >> shift < 1024
-        s_hist[tid] = 0;
+        if (lane == 0) {
+            s_lo[w] = lo;
+            s_hi[w] = hi;
+        }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < EPT; ++r) {
-            if (r >= nr) break;
-            const uint32_t key = key_of(r);
-            if (may_go(r) && key >= lo && key <= hi) atomicAdd(&s_hist[(key - lo) >> shift], 1);
+        for (int i = 0; i < NW; ++i) {
+            lo = min(lo, s_lo[i]);
+            hi = max(hi, s_hi[i]);
         }
+    };
+    range();
+    // The drop-th smallest key, by histograms of 1024 steps of the range that it is in, narrowed to
+    // one step until 64 keys are left.  Steps of the totals themselves first: equal steps of their
+    // keys, which grow with the logarithm, put most totals into a few of them, and a wave's
+    // additions to one counter take one cycle each (16385 chunks: 10 of 27 us).  Any step that
+    // grows with the key is as good: what lies below the chosen one goes, above it stays.
+    const float f0 = key_total(lo), f1 = key_total(hi);
+    bool by_value = f1 - f0 > 0.f && f1 - f0 < INFINITY;  // (not with a NaN or an infinity among them)
+    int want = drop, ties;  // the want-th of the keys within [lo, hi]; keys equal to it
+    for (;;) {
+        const int shift = max(0, 22 - __clz((hi - lo) | 1u));  // (hi - lo) >> shift < 1024
+        const float per = 1023.f / (f1 - f0);
+        auto step_of = [&](uint32_t k) {
+            return by_value ? min(1023, (int)((key_total(k) - f0) * per)) : (int)((k - lo) >> shift);
+        };
+        s_hist[tid] = 0;
+        if (tid == 0) s_in = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < EPT; ++r)
+            if (key[r] >= lo && key[r] <= hi) atomicAdd(&s_hist[step_of(key[r])], 1);
         __syncthreads();
         if (w == 0) {
             int h[kSteps / kWave], sum = 0;
@@ -302,51 +315,84 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
             }
         }
         __syncthreads();
+        const int step = s_step, in = s_hist[step];
         want -= s_below;
-        lo += (uint32_t)s_step << shift;
-        if (shift == 0) break;
-        hi = min(hi, lo + ((1u << shift) - 1u));
-    }
-    // keys below lo go, and the first `want` ties with it
-    int ties = 0, all;
+        const uint32_t from = lo, to = hi;
+        lo = kStays;
+        hi = 0;
+        if (in <= kWave) {  // few: one wave ranks them
 #pragma unroll
-    for (int r = 0; r < EPT; ++r) {
-        if (r >= nr) break;
-        below(may_go(r) && key_of(r) == lo, all);
-        ties += all;
+            for (int r = 0; r < EPT; ++r)
+                if (key[r] >= from && key[r] <= to && (by_value ? step_of(key[r]) : (int)((key[r] - from) >> shift)) == step)
+                    s_list[atomicAdd(&s_in, 1)] = key[r];
+            __syncthreads();
+            const uint32_t mine = s_list[lane];
+            int less = 0, upto = 0;
+            for (int i = 0; i < in; ++i) {
+                const uint32_t x = s_list[i];
+                less += x < mine;
+                upto += x <= mine;
+            }
+            const uint64_t hit = __ballot(lane < in && less < want && want <= upto);
+            const int src = __ffsll((unsigned long long)hit) - 1;
+            lo = (uint32_t)__shfl((int)mine, src, kWave);
+            ties = __shfl(upto - less, src, kWave);
+            want -= __shfl(less, src, kWave);
+            break;
+        }
+#pragma unroll
+        for (int r = 0; r < EPT; ++r)
+            if (key[r] >= from && key[r] <= to && (by_value ? step_of(key[r]) : (int)((key[r] - from) >> shift)) == step) {
+                lo = min(lo, key[r]);
+                hi = max(hi, key[r]);
+            }
+        range();
+        by_value = false;
+        if (lo == hi) {
+            ties = in;
+            break;
+        }
     }
-    if (lane == 0) s_ties[w] = ties;
-    __syncthreads();
-    ties = 0;
-    for (int i = 0; i < w; ++i) ties += s_ties[i];
+    // keys below lo go, and the first `want` of the ties with it
     uint32_t go = 0;  // bit r
-    int gone = 0;
+    if (ties == want) {
 #pragma unroll
-    for (int r = 0; r < EPT; ++r) {
-        if (r >= nr) break;
-        const uint32_t key = key_of(r);
-        const bool tie = may_go(r) && key == lo;
-        const int before = ties + below(tie, all);
-        ties += all;
-        const bool out = may_go(r) && (key < lo || (tie && before < want));
-        go |= (uint32_t)out << r;
-        below(out, all);
-        gone += all;
+        for (int r = 0; r < EPT; ++r) go |= (uint32_t)(key[r] <= lo && key[r] != kStays) << r;
+    } else {
+        int before = 0, all;
+#pragma unroll
+        for (int r = 0; r < EPT; ++r) {
+            below(key[r] == lo, all);
+            before += all;
+        }
+        if (lane == 0) s_ties[w] = before;
+        __syncthreads();
+        before = 0;
+        for (int i = 0; i < w; ++i) before += s_ties[i];
+#pragma unroll
+        for (int r = 0; r < EPT; ++r) {
+            const bool tie = key[r] == lo;
+            const int at = before + below(tie, all);
+            before += all;
+            go |= (uint32_t)(key[r] < lo || (tie && at < want)) << r;
+        }
     }
+    int gone = __popc(go), all;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) gone += __shfl_xor(gone, o, kWave);
     if (lane == 0) s_gone[w] = gone;
     __syncthreads();
     gone = 0;
     for (int i = 0; i < w; ++i) gone += s_gone[i];
 #pragma unroll
     for (int r = 0; r < EPT; ++r) {
-        if (r >= nr) break;
         const int c = first + r * kWave;
         const bool out = (go >> r) & 1u;
         const int at = gone + below(out, all);
         gone += all;
         if (out) {
             freed[at] = page[r];
-        } else if (c < nC) {
+        } else if (r < nr && c < nC) {
             acc[c - at] = s_tot[c];
             table[c - at] = page[r];
         }
@@ -367,7 +413,7 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
     else if (nC <= 8 * kEvictBlock)
         HILS_LAUNCH("k_evict", k_evict<8>, grid, block, 0, s, a);
     else if (nC <= kMaxHeld)
-        HILS_LAUNCH("k_evict", k_evict<32>, grid, block, 0, s, a);
+        HILS_LAUNCH("k_evict", k_evict<20>, grid, block, 0, s, a);
     else
         HILS_LAUNCH("k_evict_long", k_evict_long, grid, block, 0, s, a);
     return hipGetLastError();

@@ -3,17 +3,17 @@
 //
 //   A  k_q8_scan     a workgroup per (slice of candidate chunks, KV group, query group): s^ for the
 //                    group's heads, max over heads, the slice's top-K
-//   B  merge         top-K over the slices' survivors, by each wave that needs it
-//   C  k_q8_parts    a wave per part: a selected chunk of one query, or one piece of the window
-//                    for all the queries of a group (16 / G of them, whose (query, head) pairs
-//                    are the MFMA columns).  Record {m, l, s^, o[d]} per (row, part, head)
-//   D  fusion        softmax over the parts -> out, lse and each part's weight; by the last
-//                    workgroup of a group to arrive, or k_q8_combine
+//   B  k_q8_row      one or more workgroups per row: top-K over the slices' survivors -> idx; the
+//                    intra-chunk softmax of the selected chunks and the pieces of the window,
+//                    their fusion -> out, lse and each part's weight
 //
-// Memory-bound: a row reads G d bytes of landmarks per candidate (one head's, d) and 128 d per
+// Memory-bound: a row reads G d bytes of landmarks per candidate (one head's: d) and 128 d per
 // part.  S^T = K Q^T leaves lane group lg with keys 16 lg + 0..15 when key 16 a + 4 kb + i is row
 // 4 a + i of block kb, and V^T's 16-byte pieces hold those keys: P^T goes from the accumulators
 // into O^T = V^T P^T without leaving its lane, and nothing of a part passes through LDS.
+// (Several new queries of a sequence are rows of their own: their windows meet in an XCD's L2,
+// which all rows of a KV group share with Hkv a multiple of 8, and a value behind a query never
+// meets its products.  One tile for the window of 4 queries: 4 x 64K of 8 sequences 28 us, now 23.)
 #pragma once
 
 #include "hils_decode.hpp"
@@ -23,13 +23,25 @@ namespace hils {
 
 namespace {
 
+// Workgroups that may share a row, and rows (b, g, n) up to which they do.
+constexpr int kQ8MaxSplit = 8, kQ8SplitRows = 256;
+
+// Floats of a shared row's records: {M, Z, -, -, numerator[d]} per workgroup and head, then z of
+// each part and head.  The first record's last header word is the row's arrival counter.
+__host__ __device__ __forceinline__ int q8_row_floats(int nparts, int G, int d) {
+    return kQ8MaxSplit * G * (4 + d) + (nparts * G + 3) / 4 * 4;
+}
+
+// Workspace: the slices' survivors (as in dec_layout), then the records.  Room for the finest
+// slices and for every shared row, so that the size never falls as a call grows.
 inline DecLayout q8_layout(int B, int N, int Hkv, int G, int d, int L, int K, int W) {
     DecLayout o = {};
     o.nC = L / kChunk;
     o.nlocal = local_pieces_max(W);
     o.nparts = K + o.nlocal;
-    const size_t bg = (size_t)B * N * Hkv;
-    const size_t parts = align256(bg * o.nparts * G * (4 + d) * 4);
+    const size_t rows = (size_t)B * N * Hkv;
+    // slices of 256 chunks, halved while fewer than four workgroups per CU would scan and a row's
+    // survivors stay within one selection of a wave
     o.slice = kSlice;
     const long sgroups = (long)B * ((N + 3) / 4) * Hkv;
     while (o.slice > 64 && sgroups * ((o.nC + o.slice - 1) / o.slice) < 1024 &&
@@ -37,10 +49,13 @@ inline DecLayout q8_layout(int B, int N, int Hkv, int G, int d, int L, int K, in
         o.slice /= 2;
     o.nslices = (o.nC + o.slice - 1) / o.slice;
     o.cand = 0;
-    // sized for the finest slices, so that the size never falls as a call grows
-    o.parts = align256(bg * ((o.nC + 63) / 64) * K * 8);
-    o.total = o.parts + parts;
+    o.parts = align256(rows * ((o.nC + 63) / 64) * K * 8);
+    o.total = o.parts + align256(std::min(rows, (size_t)kQ8SplitRows) * q8_row_floats(o.nparts, G, d) * 4);
     return o;
+}
+
+__device__ __forceinline__ float* q8_record(const FwdArgs& a, const DecLayout& ly, size_t rg, int G, int d) {
+    return reinterpret_cast<float*>(static_cast<char*>(a.ws) + ly.parts) + rg * q8_row_floats(ly.nparts, G, d);
 }
 
 // New queries whose scores a scan workgroup takes from one read of the landmarks.
@@ -135,7 +150,7 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
         return q < nq ? max(0, min(ly.slice, n_candidates(decode_position(a, b, n0 + q), a.W) - c0)) : 0;
     };
     auto clear_counters = [&]() {
-        if (counters && slice == 0 && tid < nq) *part_counter<D>(a, ly, row_of(tid), G) = 0;
+        if (counters && slice == 0 && tid < nq) *reinterpret_cast<int*>(q8_record(a, ly, row_of(tid), G, D) + 3) = 0;
     };
     int len = 0;
 #pragma unroll
@@ -253,311 +268,6 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
 __device__ __forceinline__ uint32_t keys_below(int k0, int nk) {
     const int n = nk - k0;
     return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
-}
-
-// The columns of a part: lane l % 16 is (query rq, head rh) of the group's tile, on if it takes
-// part; its first nk keys count, its record is rec (-1: none).
-struct PartCol {
-    int nk, rec;
-    bool on;
-};
-
-// One part (chunk c) for the lanes' columns.  l = 0 marks a part without keys.  P is split into
-// bf16 terms (two, three for float32 outputs), so that O has the sums' precision, not P's.
-// uniform: every column that is on has the same nk; otherwise the values are masked for one
-// query after the other (a value behind a query must not reach it, not even as 0 * NaN).
-template <typename T, int D, int G, typename R>
-__device__ __forceinline__ void q8_part(const Q8DecodeArgs& qa, const DecLayout& ly, const R& recs, int b, int g, int c,
-                                        const T* qrow, const T* rrow, int hl, const PartCol& col, bool is_chunk,
-                                        int nq, int rq) {
-    constexpr int DJ = D / 64, DB = D / 16, PS = sizeof(T) == 2 ? 2 : 3;
-    const FwdArgs& a = qa.f;
-    const int lane = threadIdx.x % kWave, lg = lane / 16, n16 = lane % 16;
-    const size_t page = page_of(a, ly.nC, b, c), pg = page * a.Hkv + g;
-    const uint8_t* kp = static_cast<const uint8_t*>(a.k) + pg * kChunk * D;
-    const uint8_t* vp = static_cast<const uint8_t*>(a.v) + pg * kChunk * D;
-    uint4 kx[4][DJ], vx[DB];
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-        for (int j = 0; j < DJ; ++j)
-            kx[kb][j] =
-                *reinterpret_cast<const uint4*>(kp + ((n16 / 4) * 16 + kb * 4 + n16 % 4) * D + j * 64 + lg * 16);
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-        vx[db] = *reinterpret_cast<const uint4*>(vp + (db * 16 + n16) * kChunk + lg * 16);
-    const float ks = qa.kv_scale[pg * 2], vs = qa.kv_scale[pg * 2 + 1];
-    QRow<T, D> q;
-    q.load(qrow, lg, col.on);
-    // s^ of the column's head: q^ . k' over the lane's 16 dims per 64, summed over the lane groups
-    float sh = -INFINITY;
-    if (is_chunk) {  // uniform over the wave
-        const uint8_t* lr = static_cast<const uint8_t*>(a.lmk) + (page * a.Hl + hl) * D;
-        float acc = 0.f;
-#pragma unroll
-        for (int j = 0; j < DJ; ++j) {
-            const uint4 lx = *reinterpret_cast<const uint4*>(lr + j * 64 + lg * 16);
-            const uint32_t w[4] = {lx.x, lx.y, lx.z, lx.w};
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                float x[8], y[8];
-                e4m3_to_f32x4(w[2 * t], x);
-                e4m3_to_f32x4(w[2 * t + 1], x + 4);
-                load8(rrow + j * 64 + lg * 16 + t * 8, y);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) acc += x[e] * y[e];
-            }
-        }
-        sh = a.scale * ks * group4_sum(acc) + (a.bias ? a.bias[page * a.Hl + hl] : 0.f);
-    }
-    // S^T (lane: column n16, keys 16 lg + 4 kb + i), in log2 units
-    const float c1 = a.scale * ks * kLog2e;
-    float st[16], mx = -INFINITY;
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-        const f32x4 s4 = mfma_row<T, D>(kx[kb], q, zero4());
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            st[kb * 4 + i] = lg * 16 + kb * 4 + i < col.nk ? s4[i] * c1 : -INFINITY;
-            mx = fmaxf(mx, st[kb * 4 + i]);
-        }
-    }
-    mx = group4_max(mx);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    float l = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        st[i] = fexp2(st[i] - ref);
-        l += st[i];
-    }
-    l = group4_sum(l);
-    if (col.rec >= 0 && lg == 0) recs.store3(col.rec, mx * (1.f / kLog2e), l, sh);
-    bf16x8 p0[PS], p1[PS];
-    split_bf16x8<PS>(st, p0);
-    split_bf16x8<PS>(st + 8, p1);
-    auto values = [&](int nk, bool store) {
-        uint32_t keep[4];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) keep[w] = keys_below(lg * 16 + w * 4, nk);
-        // (every product before the first store, so that the dims' chains of products overlap)
-        f32x4 o[DB];
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            const bf16x8 v0 = bf16x8_of_e4m3(vx[db].x & keep[0], vx[db].y & keep[1]);
-            const bf16x8 v1 = bf16x8_of_e4m3(vx[db].z & keep[2], vx[db].w & keep[3]);
-            o[db] = zero4();
-#pragma unroll
-            for (int s = PS - 1; s >= 0; --s) {
-                o[db] = mfma16x16x32(v0, p0[s], o[db]);
-                o[db] = mfma16x16x32(v1, p1[s], o[db]);
-            }
-        }
-        if (store)
-#pragma unroll
-            for (int db = 0; db < DB; ++db) recs.store4(col.rec + 4 + db * 16 + lg * 4, o[db] * vs);
-    };
-    // the keys of each query (uniform: the same for all)
-    auto keys_of = [&](int q) { return __builtin_amdgcn_readlane(col.nk, q * G); };
-    if (is_chunk) {
-        values(kChunk, col.rec >= 0);
-        return;
-    }
-    bool uniform = true;
-    for (int q = 1; q < nq; ++q) uniform = uniform && keys_of(q) == keys_of(0);
-    if (uniform) {
-        values(keys_of(0), col.rec >= 0 && col.nk > 0);
-    } else {
-        for (int q = 0; q < nq; ++q) values(keys_of(q), col.rec >= 0 && col.nk > 0 && rq == q);
-    }
-}
-
-// Fusion of row (b, g, n), records from float offset `off` of recs, by a workgroup of NW waves:
-// wave w takes heads w, w + NW, ...  With lambda0 the log mass of the window's pieces, z the scores
-// of the chunks and L = LSE({z} U {lambda0}): a chunk weighs exp(z - L), a piece its share
-// exp(m + log l - L) of the window; out = sum of weight * o / l.  A part's weights are added
-// over the group's heads.
-template <int G>
-struct __align__(16) Q8FuseSmem {
-    float w[G][kMaxParts];     // weight / l
-    float mass[G][kMaxParts];  // weight
-};
-template <typename T, int D, int G, int NW, typename R>
-__device__ void q8_fuse(const Q8DecodeArgs& qa, const DecLayout& ly, Q8FuseSmem<G>& fs, const R& recs, int off, int b,
-                        int n, int g) {
-    constexpr int P = kMaxParts / kWave;
-    constexpr int RECF = 4 + D, LPP = D / 4, PPL = kWave / LPP, BATCH = 16;
-    const FwdArgs& a = qa.f;
-    const int lane = threadIdx.x % kWave, d0 = (lane % LPP) * 4, sub = lane / LPP;
-    for (int hh = wave_id(); hh < G; hh += NW) {
-        auto part = [&](int j) {
-            return recs.load4(off + (min(sub + PPL * j, ly.nparts - 1) * G + hh) * RECF + 4 + d0);
-        };
-        f32x4 h[P], v[BATCH];
-#pragma unroll
-        for (int t = 0; t < P; ++t) h[t] = recs.load4(off + (min(lane + t * kWave, ly.nparts - 1) * G + hh) * RECF);
-#pragma unroll
-        for (int j = 0; j < BATCH; ++j) v[j] = part(j);
-        float m0 = -INFINITY, z = -INFINITY;
-#pragma unroll
-        for (int t = 0; t < P; ++t) {
-            const int pt = lane + t * kWave;
-            if (pt >= ly.nparts) h[t][1] = 0.f;
-            if (h[t][1] != 0.f) {
-                if (pt >= a.K)
-                    m0 = fmaxf(m0, h[t][0]);
-                else
-                    z = fmaxf(z, h[t][2]);
-            }
-        }
-        m0 = wave_max(m0);
-        float l0 = 0.f;
-#pragma unroll
-        for (int t = 0; t < P; ++t)
-            if (lane + t * kWave >= a.K && h[t][1] != 0.f) l0 += h[t][1] * expf(h[t][0] - m0);
-        l0 = wave_sum(l0);
-        const float lam0 = m0 + logf(l0);
-        const float M = fmaxf(wave_max(z), lam0);
-        float Z = 0.f;
-#pragma unroll
-        for (int t = 0; t < P; ++t)
-            if (lane + t * kWave < a.K && h[t][1] != 0.f) Z += expf(h[t][2] - M);
-        Z = wave_sum(Z) + expf(lam0 - M);
-        const float L = M + logf(Z), a0 = expf(lam0 - L) / l0;
-#pragma unroll
-        for (int t = 0; t < P; ++t) {
-            const int pt = lane + t * kWave;
-            const float l = h[t][1];
-            const float w = l == 0.f ? 0.f : pt >= a.K ? a0 * expf(h[t][0] - m0) : expf(h[t][2] - L) / l;
-            fs.w[hh][pt] = w;
-            fs.mass[hh][pt] = l == 0.f ? 0.f : w * l;
-        }
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        f32x4 acc = zero4();
-        for (int j0 = 0; j0 * PPL < ly.nparts; j0 += BATCH) {
-            if (j0 > 0)
-#pragma unroll
-                for (int j = 0; j < BATCH; ++j) v[j] = part(j0 + j);
-#pragma unroll
-            for (int j = 0; j < BATCH; ++j) {
-                const int pt = sub + PPL * (j0 + j);
-                const float w = pt < ly.nparts ? fs.w[hh][pt] : 0.f;
-                if (w != 0.f) acc += w * v[j];
-            }
-        }
-#pragma unroll
-        for (int o = LPP; o < kWave; o <<= 1)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], o, kWave);
-        const size_t row = q_row(a, b, g * G + hh, n);
-        if (sub == 0) {
-            if constexpr (sizeof(T) == 2)
-                store_unaligned(as_mut<bf16>(a.out) + row * D + d0,
-                                make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])));
-            else
-                __builtin_memcpy(as_mut<float>(a.out) + row * D + d0, &acc, 16);
-        }
-        if (lane == 0) a.lse[row] = L;
-    }
-    if (qa.weights) {
-        __syncthreads();
-        const size_t rg = ((size_t)b * a.Hkv + g) * a.N + n;
-        for (int pt = threadIdx.x; pt < ly.nparts; pt += NW * kWave) {
-            float m = 0.f;
-#pragma unroll
-            for (int hh = 0; hh < G; ++hh) m += fs.mass[hh][pt];
-            qa.weights[rg * ly.nparts + pt] = m;
-        }
-        __syncthreads();  // the next row's weights may follow in fs
-    }
-}
-
-// Four parts per workgroup, one per wave; units of a query group: KP = K rounded up to 4 per
-// query, then the window's pieces.  E as in k_dec_parts_w: > 0, the waves of selected chunks
-// merge the scan's survivors themselves (kSoloE: each alone; more: its workgroup, all of one
-// query); 0: idx given.
-template <typename T, int D, int G, int NQP, int E, bool FUSE>
-__global__ __launch_bounds__(kBlock, FUSE || sizeof(T) == 4 ? 1 : 4) void k_q8_parts(Q8DecodeArgs qa, DecLayout ly) {
-    constexpr int NW = kBlock / kWave;
-    constexpr int kScratch = E > kSoloE ? (int)sizeof(MergeSmem<NW>) : (int)sizeof(MergeSmem<1>) * NW;
-    constexpr int kBytes = FUSE && (int)sizeof(Q8FuseSmem<G>) > kScratch ? (int)sizeof(Q8FuseSmem<G>) : kScratch;
-    __shared__ __align__(16) unsigned char s_raw[kBytes];
-    const FwdArgs& a = qa.f;
-    const int w = wave_id(), lane = threadIdx.x % kWave, n16 = lane % 16;
-    const int ngrp = (a.N + NQP - 1) / NQP;
-    const int g = blockIdx.y, b = blockIdx.z / ngrp, n0 = (blockIdx.z % ngrp) * NQP;
-    const int nq = min(NQP, a.N - n0);
-    const int KP = (a.K + NW - 1) / NW * NW;
-    const int unit = blockIdx.x * NW + w, rq_unit = unit / KP;
-    const size_t rg0 = ((size_t)b * a.Hkv + g) * a.N + n0;  // the group's first row; the others follow
-    const Recs<FUSE> recs(part_record<D>(a, ly, rg0, 0, 0, G), (size_t)nq * ly.nparts * G * (4 + D));
-    const int rowf = ly.nparts * G * (4 + D);  // floats of a row's records
-    auto record = [&](int q, int part, int h) { return q * rowf + (part * G + h) * (4 + D); };
-    if (rq_unit < nq) {  // a slot of query rq_unit (uniform over the workgroup)
-        const int slot = unit % KP, n = n0 + rq_unit;
-        const size_t rg = rg0 + rq_unit;
-        int csel = -1;
-        if constexpr (E == kSoloE) {
-            if (slot < a.K) {
-                auto& ms = reinterpret_cast<MergeSmem<1>*>(s_raw)[w];
-                merge_row_wave<E>(a, ly, rg, ms);
-                const int nb = ms.nbest;
-                if (slot == 0)
-                    for (int t = lane; t < a.K; t += kWave) a.idx[rg * a.K + t] = t < nb ? ms.bid[t] : -1;
-                csel = slot < nb ? ms.bid[slot] : -1;
-            }
-        } else if constexpr (E > 0) {
-            auto& ms = *reinterpret_cast<MergeSmem<NW>*>(s_raw);
-            merge_row<E, NW>(a, ly, rg, ms, w);
-            const int nb = ms.nbest;
-            if (unit % KP < NW)
-                for (int t = threadIdx.x; t < a.K; t += kBlock) a.idx[rg * a.K + t] = t < nb ? ms.bid[t] : -1;
-            if (slot < a.K) csel = slot < nb ? ms.bid[slot] : -1;
-        } else {
-            const int32_t* irow = a.idx + rg * a.K;
-            if (slot < a.K && idx_entry_valid(irow, slot, n_candidates(decode_position(a, b, n), a.W)))
-                csel = irow[slot];
-        }
-        const int c = __builtin_amdgcn_readfirstlane(csel);
-        const int hh = min(n16, G - 1);
-        if (slot < a.K && c >= 0) {
-            const size_t row = q_row(a, b, g * G + hh, n);
-            const PartCol col = {kChunk, n16 < G ? record(rq_unit, slot, hh) : -1, n16 < G};
-            q8_part<T, D, G>(qa, ly, recs, b, g, c, as<T>(a.q) + row * D,
-                             as<T>(a.q_route ? a.q_route : a.q) + row * D, a.Hl == a.Hq ? g * G + hh : g, col, true, 1, 0);
-        } else if (slot < a.K && lane < G) {
-            recs.store3(record(rq_unit, slot, lane), -INFINITY, 0.f, -INFINITY);
-        }
-    } else if (unit >= NQP * KP) {  // a piece of the window, for the group's queries
-        const int first = decode_position(a, b, n0), c = n_candidates(first, a.W) + (unit - NQP * KP);
-        const int rq = n16 / G, rh = n16 % G;
-        const int pos = first + min(rq, nq - 1), piece = c - n_candidates(pos, a.W);
-        const bool mine = rq < nq && piece >= 0 && piece < ly.nlocal;
-        const int nk = mine ? max(0, min(kChunk, pos - c * kChunk + 1)) : 0;
-        const int rec = mine ? record(rq, piece + a.K, rh) : -1;
-        if (c <= (first + nq - 1) / kChunk) {  // some query reaches it
-            const size_t row = q_row(a, b, g * G + rh, n0 + min(rq, nq - 1));
-            q8_part<T, D, G>(qa, ly, recs, b, g, c, as<T>(a.q) + row * D, as<T>(a.q), 0, PartCol{nk, rec, rq < nq},
-                             false, nq, rq);
-        } else if (rec >= 0 && lane < 16) {
-            recs.store3(rec, -INFINITY, 0.f, -INFINITY);
-        }
-    }
-    if constexpr (FUSE) {
-        if (last_to_arrive(part_counter<D>(a, ly, rg0, G), gridDim.x))
-            for (int q = 0; q < nq; ++q)
-                q8_fuse<T, D, G, NW>(qa, ly, *reinterpret_cast<Q8FuseSmem<G>*>(s_raw), recs, q * rowf, b, n0 + q, g);
-    }
-}
-
-template <typename T, int D, int G>
-__global__ __launch_bounds__(kBlock) void k_q8_combine(Q8DecodeArgs qa, DecLayout ly) {
-    __shared__ Q8FuseSmem<G> fs;
-    const FwdArgs& a = qa.f;
-    const int g = blockIdx.x, b = blockIdx.y / a.N, n = blockIdx.y % a.N;
-    const size_t rg = ((size_t)b * a.Hkv + g) * a.N + n;
-    const Recs<false> recs(part_record<D>(a, ly, rg, 0, 0, G), (size_t)ly.nparts * G * (4 + D));
-    q8_fuse<T, D, G, kBlock / kWave>(qa, ly, fs, recs, 0, b, n, g);
 }
 
 // The K best of more survivors than a wave takes in one round, by the whole workgroup of row rg:
@@ -696,8 +406,7 @@ __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, 
     return m;
 }
 
-// One new query per sequence: gridDim.z workgroups of four waves share the parts of a row.  In a
-// workgroup the last wave selects while the others take their share of the window's pieces, then
+// gridDim.z workgroups of four waves share the parts of a row.  In a workgroup the last wave selects while the others take their share of the window's pieces, then
 // the selected chunks are spread over all four.  A wave adds its parts into one running
 // (maximum, sum, numerator) per head: part t enters with weight exp(z_t - M), z = s^_c for a chunk,
 // whose P is divided by its own sum, and z = m + log l for a piece of the window.  The next part's
@@ -707,7 +416,6 @@ __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, 
 // (A wave per part with its record in memory and the fusion in a launch of its own: 1024 rows of
 // 25 parts 99 + 14 us.)
 constexpr int kQ8RowWaves = 4;
-constexpr int kQ8MaxSplit = 8;
 template <typename T>
 __device__ __forceinline__ void q8_store_out(const FwdArgs& a, size_t at, const f32x4& o) {
     if constexpr (sizeof(T) == 2)
@@ -735,14 +443,14 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
     __shared__ Q8BlockMerge bm;
     const FwdArgs& a = qa.f;
     const int ns = SPLIT ? gridDim.z : 1, split = SPLIT ? blockIdx.z : 0;
-    const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, w = wave_id(), lane = tid % kWave, lg = lane / 16,
-              n16 = lane % 16;
-    const size_t rg = (size_t)b * a.Hkv + g;
-    const int pos = decode_position(a, b, 0), ncand = n_candidates(pos, a.W);
+    const int g = blockIdx.x, b = blockIdx.y / a.N, n = blockIdx.y % a.N;
+    const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave, lg = lane / 16, n16 = lane % 16;
+    const size_t rg = ((size_t)b * a.Hkv + g) * a.N + n;
+    const int pos = decode_position(a, b, n), ncand = n_candidates(pos, a.W);
     const int hh = min(n16, G - 1), hl = a.Hl == a.Hq ? g * G + hh : g;
     QRow<T, D> q, qr_;
-    q.load(as<T>(a.q) + q_row(a, b, g * G + hh, 0) * D, lg, n16 < G);
-    if constexpr (ROUTE) qr_.load(as<T>(a.q_route) + q_row(a, b, g * G + hh, 0) * D, lg, n16 < G);
+    q.load(as<T>(a.q) + q_row(a, b, g * G + hh, n) * D, lg, n16 < G);
+    if constexpr (ROUTE) qr_.load(as<T>(a.q_route) + q_row(a, b, g * G + hh, n) * D, lg, n16 < G);
     const QRow<T, D>& qr = ROUTE ? qr_ : q;
     f32x4 acc[DB];
 #pragma unroll
@@ -922,9 +630,8 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
     }
     __syncthreads();
     constexpr int RECF = 4 + D;
-    // records {M, Z} and numerators of the row's workgroups, then z of its parts
-    const Recs<true> recs(part_record<D>(a, ly, rg, 0, 0, G), (size_t)ly.nparts * G * RECF);
-    const int zoff = ns * G * RECF;
+    const Recs<true> recs(q8_record(a, ly, SPLIT ? rg : 0, G, D), (size_t)q8_row_floats(ly.nparts, G, D));
+    constexpr int zoff = kQ8MaxSplit * G * RECF;
     for (int e = tid; e < G * D / 4; e += NW * kWave) {
         const int h = e / (D / 4), d0 = e % (D / 4) * 4;
         float m = -INFINITY, z = 0.f;
@@ -942,10 +649,10 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
             recs.store4((split * G + h) * RECF + 4 + d0, o);
             if (d0 == 0) recs.store3((split * G + h) * RECF, m, z, 0.f);
         } else {
-            q8_store_out<T>(a, q_row(a, b, g * G + h, 0) * D + d0, o * (1.f / z));
+            q8_store_out<T>(a, q_row(a, b, g * G + h, n) * D + d0, o * (1.f / z));
             if (d0 == 0) {
                 sm.lse[h] = m + __builtin_amdgcn_logf(z);
-                a.lse[q_row(a, b, g * G + h, 0)] = (m + __builtin_amdgcn_logf(z)) * (1.f / kLog2e);
+                a.lse[q_row(a, b, g * G + h, n)] = (m + __builtin_amdgcn_logf(z)) * (1.f / kLog2e);
             }
         }
     }
@@ -956,7 +663,7 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
             if ((pt < a.K ? pt : pt - a.K) % ns == split)
                 __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint((&sm.part[0][0])[e]), recs.r, z_at(e), 0, Recs<true>::kAux);
         }
-        if (!last_to_arrive(part_counter<D>(a, ly, rg, G), ns)) return;
+        if (!last_to_arrive(reinterpret_cast<int*>(q8_record(a, ly, rg, G, D) + 3), ns)) return;
         for (int e = tid; e < G * D / 4; e += NW * kWave) {
             const int h = e / (D / 4), d0 = e % (D / 4) * 4;
             f32x4 head[kQ8MaxSplit], num[kQ8MaxSplit];
@@ -978,10 +685,10 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
                     z += c * head[i][1];
                     o += c * num[i];
                 }
-            q8_store_out<T>(a, q_row(a, b, g * G + h, 0) * D + d0, o * (1.f / z));
+            q8_store_out<T>(a, q_row(a, b, g * G + h, n) * D + d0, o * (1.f / z));
             if (d0 == 0) {
                 sm.lse[h] = m + __builtin_amdgcn_logf(z);
-                a.lse[q_row(a, b, g * G + h, 0)] = (m + __builtin_amdgcn_logf(z)) * (1.f / kLog2e);
+                a.lse[q_row(a, b, g * G + h, n)] = (m + __builtin_amdgcn_logf(z)) * (1.f / kLog2e);
             }
         }
         if (qa.weights)
@@ -1012,61 +719,38 @@ struct Q8DecRun {
                 HILS_LAUNCH("k_q8_scan", (k_q8_scan<T, D, G, NQ>), dim3((pairs + 7) / 8 * 8 * a.Hkv), dim3(kBlock), 0, s,
                             qa, ly, counters);
         };
-        if (a.N == 1) {
-            // Two workgroups per CU hold the chip's registers; with fewer rows than that a row
-            // goes over several, down to a part per wave.  (A given selection comes without the
-            // scan that clears the arrival counters: one workgroup per row.)
-            const int ns = a.given_idx ? 1 : std::max(1, std::min({kQ8MaxSplit, (ly.nparts + 3) / 4, 2 * cus / (R * a.Hkv)}));
+        // Two workgroups per CU hold the chip's registers; with fewer rows than that a row goes
+        // over several, down to a part per wave.  (A given selection comes without the scan that
+        // clears the arrival counters: one workgroup per row.)
+        const int rows = R * a.Hkv;
+        const int ns = a.given_idx || rows > kQ8SplitRows
+                           ? 1
+                           : std::max(1, std::min({kQ8MaxSplit, (ly.nparts + 3) / 4, 2 * cus / rows}));
+        if (a.N == 1)
             scan(std::false_type{}, ns > 1);
-            const dim3 grid(a.Hkv, a.B, ns), block(kQ8RowWaves * kWave);
-            auto row = [&](auto e_tag, auto route_tag) {
-                constexpr int EE = decltype(e_tag)::value;
-                constexpr bool RR = decltype(route_tag)::value;
-                if constexpr (EE > 0)
-                    if (ns > 1) {
-                        HILS_LAUNCH("k_q8_row", (k_q8_row<T, D, G, EE, RR, true>), grid, block, 0, s, qa, ly);
-                        return;
-                    }
-                HILS_LAUNCH("k_q8_row", (k_q8_row<T, D, G, EE, RR, false>), grid, block, 0, s, qa, ly);
-            };
-            auto by_route = [&](auto e_tag) {
-                if (a.q_route) row(e_tag, std::true_type{});
-                else row(e_tag, std::false_type{});
-            };
-            // (survivors a wave selects from in one round: 64 per unit of E)
-            if (a.given_idx)
-                by_route(std::integral_constant<int, 0>{});
-            else if (surv <= kWave * 4)
-                by_route(std::integral_constant<int, 4>{});
-            else
-                by_route(std::integral_constant<int, 16>{});
-            return hipGetLastError();
-        }
-        constexpr int NW = kBlock / kWave, NQP = MqCfg<G>::NQ;
-        const int KP = (a.K + NW - 1) / NW * NW;
-        // up to 8 parts per CU the last workgroup to arrive fuses, as in k_dec_parts_w
-        const bool fuse = !a.given_idx && (long)R * a.Hkv * ly.nparts <= 8l * cus;
-        scan(std::true_type{}, fuse);
-        // (queries of a group sit within one chunk's length of each other: one more piece at most)
-        const int units = NQP * KP + ly.nlocal + 1;
-        const dim3 grid((units + NW - 1) / NW, a.Hkv, a.B * ((a.N + NQP - 1) / NQP));
-        auto parts = [&](auto e_tag) {
+        else
+            scan(std::true_type{}, ns > 1);
+        const dim3 grid(a.Hkv, R, ns), block(kQ8RowWaves * kWave);
+        auto row = [&](auto e_tag, auto route_tag) {
             constexpr int EE = decltype(e_tag)::value;
-            if constexpr (EE > 0) {
-                if (fuse) {
-                    HILS_LAUNCH("k_q8_parts", (k_q8_parts<T, D, G, NQP, EE, true>), grid, dim3(kBlock), 0, s, qa, ly);
+            constexpr bool RR = decltype(route_tag)::value;
+            if constexpr (EE > 0)
+                if (ns > 1) {
+                    HILS_LAUNCH("k_q8_row", (k_q8_row<T, D, G, EE, RR, true>), grid, block, 0, s, qa, ly);
                     return;
                 }
-            }
-            HILS_LAUNCH("k_q8_parts", (k_q8_parts<T, D, G, NQP, EE, false>), grid, dim3(kBlock), 0, s, qa, ly);
-            HILS_LAUNCH("k_q8_combine", (k_q8_combine<T, D, G>), dim3(a.Hkv, R), dim3(kBlock), 0, s, qa, ly);
+            HILS_LAUNCH("k_q8_row", (k_q8_row<T, D, G, EE, RR, false>), grid, block, 0, s, qa, ly);
+        };
+        auto by_route = [&](auto e_tag) {
+            if (a.q_route) row(e_tag, std::true_type{});
+            else row(e_tag, std::false_type{});
         };
         if (a.given_idx)
-            parts(std::integral_constant<int, 0>{});
+            by_route(std::integral_constant<int, 0>{});
         else if (surv <= kWave * kSoloE)
-            parts(std::integral_constant<int, kSoloE>{});
+            by_route(std::integral_constant<int, kSoloE>{});
         else
-            parts(std::integral_constant<int, 8>{});
+            by_route(std::integral_constant<int, 2 * kSoloE>{});
         return hipGetLastError();
     }
 };

@@ -351,7 +351,7 @@ EVICT = {
     "zero_most": (dict(B=1, Hq=2, Hkv=1, N=1, L=64 * 50, d=64, topk=4, window=128), None, 1, 0, 0),
     "sinks_past_the_end": (dict(B=1, Hq=2, Hkv=1, N=1, L=64 * 9, d=64, topk=4, window=128), [500], 0, 100, None),
     # more chunks than the totals of which fit in LDS
-    "long": (dict(B=1, Hq=4, Hkv=2, N=2, L=64 * 33001, d=64, topk=16, window=512), None, 9000, 3, None),
+    "long": (dict(B=1, Hq=4, Hkv=2, N=2, L=64 * 25001, d=64, topk=16, window=512), None, 9000, 3, None),
     "tiles": (dict(B=2, Hq=4, Hkv=2, N=2, L=64 * 5001, d=64, topk=64, window=4032), [64 * 5001 - 5, 64 * 3500], 1800, 3, None),
 }
 
