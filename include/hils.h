@@ -303,8 +303,8 @@ int hils_landmark_bwd(const hils_params* p, const void* lq, const void* k, const
  *   bias_pages [num_pages, Hl] f32     landmark bias b'_c
  * and chunk c of sequence b is page block_table[b, c] ([B, L/S] int32, device; an
  * entry outside [0, num_pages) is clamped into it; entries of chunks at or past a
- * sequence's length are not read).  k_pages, v_pages and lmk_pages are 16-byte
- * aligned, kv_scale 8-byte aligned.
+ * sequence's length are not read).  k_pages, v_pages, lmk_pages and the workspace must
+ * be 16-byte aligned, kv_scale 8-byte aligned.
  *
  * hils_q8_append writes new tokens' keys and values: sequence b appends the first
  * newlens[b] rows of k_new and v_new ([B, Hkv, N, d], dtype; newlens [B] int32, NULL: N
@@ -370,12 +370,13 @@ int hils_decode_q8_fwd(const hils_params* p, const void* q, const void* k_pages,
  * -1 and 0), the length falls by S per chunk, so that any decode entry point runs on
  * the result: positions serve the chunk partition only (rotations are the caller's).
  *   acc, acc_out         [B, L/S] f32       block_table, table_out [B, L/S] int32
- *   seqlens, seqlens_out [B] int32 (seqlens NULL: L; values are clamped into [N, L])
+ *   seqlens, seqlens_out [B] int32 (seqlens NULL: L; values are clamped into [0, L]; the
+ *          weights belong to the decode call's positions, which start from at least N tokens)
  *   freed  [B, max_evict] int32: the pages given up, in the order of their chunks, -1
  *          past nfreed[b] (NULL if max_evict is 0)
  *   nfreed [B] int32
  * The outputs may be the inputs themselves (in place), but not overlap them otherwise.
- * Uses B, Hkv, N, L, topk and window of `p`.  Deterministic.
+ * Uses B, Hkv, N, L, topk and window of `p` and ignores the forward flags.  Deterministic.
  */
 int hils_cache_evict(const hils_params* p, const float* acc, const int32_t* block_table, const int32_t* seqlens,
                      const float* weights, const int32_t* idx, int budget, int sink, int max_evict, float* acc_out,

@@ -71,7 +71,12 @@ int check_params(const hils_params* p, int op) {
                      HILS_FLAG_UNION_PACKING))
         return fail(HILS_ERR_INVALID, "unknown flags 0x%x", p->flags);
     const bool q8_cache = op == HILS_OP_Q8_APPEND || op == HILS_OP_Q8_LANDMARK || op == HILS_OP_CACHE_EVICT;
-    if (q8_cache && (p->flags & ~(op == HILS_OP_Q8_LANDMARK ? HILS_FLAG_SHARED_LMK_QUERY : 0u)))
+    // (the eviction takes the decode call's parameters, whose forward flags mean nothing to it)
+    const unsigned q8_flags = op == HILS_OP_Q8_LANDMARK ? HILS_FLAG_SHARED_LMK_QUERY
+                              : op == HILS_OP_CACHE_EVICT
+                                  ? HILS_FLAG_GIVEN_IDX | HILS_FLAG_HEAD_NORM_SELECT | HILS_FLAG_UNION_PACKING
+                                  : 0u;
+    if (q8_cache && (p->flags & ~q8_flags))
         return fail(HILS_ERR_INVALID, "flags 0x%x do not apply to this entry point", p->flags);
     if ((p->flags & HILS_FLAG_HEAD_NORM_SELECT) && op == HILS_OP_LANDMARK)
         return fail(HILS_ERR_INVALID, "HILS_FLAG_HEAD_NORM_SELECT does not apply to the landmark compression");
@@ -146,9 +151,12 @@ int hip_status(hipError_t e, const char* what) {
 #define REQUIRE(ptr) \
     if (!(ptr)) return fail(HILS_ERR_INVALID, "required pointer '%s' is NULL", #ptr)
 
-// Waves of a cache-writing launch, four to a workgroup of a one-dimensional grid.
-int check_q8_grid(const hils_params* p, long waves) {
-    if ((waves + 3) / 4 > 0xffffffl)  // 2^32 threads
+#define REQUIRE_ALIGNED(ptr, n) \
+    if ((uintptr_t)(ptr) % (n)) return fail(HILS_ERR_INVALID, "'%s' is not %d-byte aligned", #ptr, n)
+
+// Workgroups of 256 threads in a one-dimensional grid.
+int check_q8_grid(const hils_params* p, double blocks) {
+    if (blocks > 0xffffff)  // 2^32 threads
         return fail(HILS_ERR_UNSUPPORTED, "B=%d Hkv=%d N=%d: more workgroups than one grid holds", p->B, p->Hkv, p->N);
     return HILS_OK;
 }
@@ -374,8 +382,9 @@ int hils_q8_append(const hils_params* p, const void* k_new, const void* v_new, v
     int rc = check_params(p, HILS_OP_Q8_APPEND);
     if (rc) return rc;
     REQUIRE(k_new); REQUIRE(v_new); REQUIRE(k_pages); REQUIRE(v_pages); REQUIRE(kv_scale); REQUIRE(block_table);
+    REQUIRE_ALIGNED(k_pages, 16); REQUIRE_ALIGNED(v_pages, 16); REQUIRE_ALIGNED(kv_scale, 8);
     if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
-    rc = check_q8_grid(p, 2l * p->B * p->Hkv * ((p->N + 62l) / 64 + 1));
+    rc = check_q8_grid(p, .5 * p->B * p->Hkv * ((p->N + 62l) / 64 + 1));
     if (rc) return rc;
     hils::Q8AppendArgs a;
     a.k_new = k_new; a.v_new = v_new; a.k_pages = k_pages; a.v_pages = v_pages; a.kv_scale = kv_scale;
@@ -391,8 +400,9 @@ int hils_q8_landmark_fwd(const hils_params* p, const void* lq, const void* k_pag
     int rc = check_params(p, HILS_OP_Q8_LANDMARK);
     if (rc) return rc;
     REQUIRE(lq); REQUIRE(k_pages); REQUIRE(kv_scale); REQUIRE(block_table); REQUIRE(lmk_pages); REQUIRE(bias_pages);
+    REQUIRE_ALIGNED(k_pages, 16); REQUIRE_ALIGNED(lmk_pages, 16); REQUIRE_ALIGNED(kv_scale, 8);
     if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
-    rc = check_q8_grid(p, (long)p->B * p->Hkv * ((p->N + 63l) / 64));
+    rc = check_q8_grid(p, .25 * p->B * p->Hkv * ((p->N + 63l) / 64));
     if (rc) return rc;
     hils::Q8LandmarkArgs a;
     a.lq = lq; a.k_pages = k_pages; a.kv_scale = kv_scale; a.lmk_pages = lmk_pages; a.bias_pages = bias_pages;
@@ -411,9 +421,13 @@ int hils_decode_q8_fwd(const hils_params* p, const void* q, const void* k_pages,
     if (rc) return rc;
     REQUIRE(q); REQUIRE(k_pages); REQUIRE(v_pages); REQUIRE(kv_scale); REQUIRE(lmk_pages); REQUIRE(block_table);
     REQUIRE(out); REQUIRE(lse); REQUIRE(idx);
+    REQUIRE_ALIGNED(k_pages, 16); REQUIRE_ALIGNED(v_pages, 16); REQUIRE_ALIGNED(lmk_pages, 16); REQUIRE_ALIGNED(kv_scale, 8);
     if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    rc = check_q8_grid(p, ((p->L / 64 + 255) / 256 + 8.) * p->B * p->N * p->Hkv);  // the scan's
+    if (rc) return rc;
     rc = check_ws(p, HILS_OP_DECODE_Q8, workspace, ws_bytes);
     if (rc) return rc;
+    REQUIRE_ALIGNED(workspace, 16);
     hils::Q8DecodeArgs a;
     a.f = fwd_args(p, q, k_pages, v_pages, lmk_pages, bias_pages, q_route, seqlens, out, lse, idx, workspace, ws_bytes);
     a.f.block_table = block_table;
@@ -433,6 +447,9 @@ int hils_cache_evict(const hils_params* p, const float* acc, const int32_t* bloc
     if (budget < 0 || sink < 0 || max_evict < 0)
         return fail(HILS_ERR_INVALID, "budget, sink and max_evict must be >= 0 (budget=%d sink=%d max_evict=%d)", budget,
                     sink, max_evict);
+    if (weights && ((double)p->Hkv * p->N * (p->topk + (p->window + 62) / 64 + 1) > 0x7fffffff))
+        return fail(HILS_ERR_UNSUPPORTED, "Hkv=%d N=%d topk=%d: more weights per sequence than 2^31", p->Hkv, p->N,
+                    p->topk);
     if (max_evict > 0 && !freed) return fail(HILS_ERR_INVALID, "max_evict=%d, so freed must be non-NULL", max_evict);
     hils::EvictArgs a;
     a.acc = acc; a.table = block_table; a.seqlens = seqlens; a.weights = weights; a.idx = idx;

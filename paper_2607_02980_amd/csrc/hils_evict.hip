@@ -22,6 +22,12 @@ constexpr int kEvictBlock = 1024;
 constexpr int kEvictWaves = kEvictBlock / kWave;
 constexpr int kMaxHeld = 20 * kEvictBlock;  // chunks (1.3M tokens): totals of 80 KB in LDS
 
+// Tokens of sequence b.
+__device__ __forceinline__ int evict_tokens(const EvictArgs& a, int b) {
+    const int len = a.seqlens ? a.seqlens[b] : a.L;
+    return len < 0 ? 0 : (len > a.L ? a.L : len);
+}
+
 // How many lanes below have x, and how many of the wave.
 __device__ __forceinline__ int below(bool x, int& all) {
     const uint64_t m = __ballot(x);
@@ -40,8 +46,7 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict_long(EvictArgs a) {
     __shared__ int s_tie[kEvictWaves], s_gone[kEvictWaves];
     const int b = blockIdx.x, tid = threadIdx.x, w = wave_id(), lane = tid % kWave;
     const int nC = a.L / kChunk;
-    int len = a.seqlens ? a.seqlens[b] : a.L;
-    len = len < a.N ? a.N : (len > a.L ? a.L : len);
+    const int len0 = evict_tokens(a, b), len = max(len0, a.N);  // (len: the decode call's positions)
     const float* acc_in = a.acc + (size_t)b * nC;
     float* acc = a.acc_out + (size_t)b * nC;
     const int32_t* table_in = a.table + (size_t)b * nC;
@@ -70,10 +75,10 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict_long(EvictArgs a) {
             __syncthreads();
         }
     }
-    const int last = n_candidates(len - 1, a.W), able = max(0, last - a.sink);
+    const int last = n_candidates(len0 - 1, a.W), able = max(0, last - a.sink);
     const int drop = min(min(max(0, last - a.budget), able), a.most);
     if (tid == 0) {
-        a.seqlens_out[b] = len - drop * kChunk;
+        a.seqlens_out[b] = len0 - drop * kChunk;
         a.nfreed[b] = drop;
     }
     for (int t = drop + tid; t < a.most; t += kEvictBlock) freed[t] = -1;
@@ -182,8 +187,7 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
     float* acc = a.acc_out + (size_t)b * nC;
     const int32_t* table_in = a.table + (size_t)b * nC;
     int32_t* table = a.table_out + (size_t)b * nC;
-    int len = a.seqlens ? a.seqlens[b] : a.L;
-    len = len < a.N ? a.N : (len > a.L ? a.L : len);
+    const int len0 = evict_tokens(a, b), len = max(len0, a.N);  // (len: the decode call's positions)
     int32_t page[EPT];
 #pragma unroll
     for (int r = 0; r < EPT; ++r) {
@@ -217,10 +221,10 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
         }
     }
     __syncthreads();  // the totals; and every wave has read what the outputs may replace
-    const int last = n_candidates(len - 1, a.W), able = max(0, last - a.sink);
+    const int last = n_candidates(len0 - 1, a.W), able = max(0, last - a.sink);
     const int drop = min(min(max(0, last - a.budget), able), a.most);
     if (tid == 0) {
-        a.seqlens_out[b] = len - drop * kChunk;
+        a.seqlens_out[b] = len0 - drop * kChunk;
         a.nfreed[b] = drop;
     }
     int32_t* freed = a.freed + (size_t)b * a.most;  // (not touched if most is 0)

@@ -167,7 +167,8 @@ def evict(p, acc, table, seqlens, budget, sink, most, weights=None, idx=None):
     acc, table = acc.astype(np.float64), table.copy()
     freed, counts, lens = np.full((p.B, most), -1, np.int32), [], []
     for b in range(p.B):
-        length = p.L if seqlens is None else min(max(int(seqlens[b]), p.N), p.L)
+        tokens_ = p.L if seqlens is None else min(max(int(seqlens[b]), 0), p.L)
+        length = max(tokens_, p.N)  # the decode call's positions
         if weights is not None:
             for g in range(p.Hkv):
                 for n in range(p.N):
@@ -178,7 +179,7 @@ def evict(p, acc, table, seqlens, budget, sink, most, weights=None, idx=None):
                             acc[b, row[t]] += weights[b, g, n, t]
                     for c in range(nc, i // S + 1):
                         acc[b, c] += weights[b, g, n, K + c - nc]
-        last = n_candidates(length - 1, W)
+        last = n_candidates(tokens_ - 1, W)
         able = list(range(sink, last))
         count = min(max(0, last - budget), len(able), most)
         gone = sorted(sorted(able, key=lambda c: (np.isnan(acc[b, c]), acc[b, c], c))[:count])
@@ -187,5 +188,5 @@ def evict(p, acc, table, seqlens, budget, sink, most, weights=None, idx=None):
         acc[b] = np.concatenate([acc[b, kept], np.zeros(count)])
         table[b] = np.concatenate([table[b, kept], np.full(count, -1)])
         counts.append(count)
-        lens.append(length - S * count)
+        lens.append(tokens_ - S * count)
     return acc, table, np.array(lens, np.int32), freed, np.array(counts, np.int32)

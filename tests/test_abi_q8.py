@@ -77,7 +77,7 @@ def test_pages_flags_and_limits():
         assert call(params(), pages=0) == 1 and "num_pages" in hils.hils_last_error()
     for call in (append, evict):
         assert call(params(flags=hils.HILS_FLAG_SHARED_LMK_QUERY)) == 1
-    for call in (append, landmark, evict):
+    for call in (append, landmark):
         assert call(params(flags=hils.HILS_FLAG_GIVEN_IDX)) == 1
     assert decode(params(flags=hils.HILS_FLAG_HEAD_NORM_SELECT)) == 2 and "8-bit" in hils.hils_last_error()
     assert decode(params(flags=hils.HILS_FLAG_SHARED_LMK_QUERY)) == 1
@@ -88,6 +88,17 @@ def test_pages_flags_and_limits():
         assert evict(params(), **kw) == 1 and ">= 0" in hils.hils_last_error()
     assert evict(params(), freed=None) == 1 and "freed" in hils.hils_last_error()
     assert evict(params(), weights=FAKE) == 1 and "idx" in hils.hils_last_error()
+    odd = ctypes.c_void_p(0x1008)
+    for call, names in ((append, ["k", "v"]), (landmark, ["k", "lmk"]), (decode, ["k", "v", "lmk"])):
+        for n in names:
+            assert call(params(), **{n: odd}) == 1 and "16-byte" in hils.hils_last_error()
+    for call in (append, landmark, decode):
+        assert call(params(), scale=ctypes.c_void_p(0x1004)) == 1 and "8-byte" in hils.hils_last_error()
+    # more workgroups than a grid holds, more weights than an int counts
+    assert append(params(B=65535, Hkv=64, Hq=64, N=1 << 20, L=1 << 20)) == 2
+    assert landmark(params(B=65535, Hkv=64, Hq=64, N=1 << 20, L=1 << 20)) == 2
+    assert decode(params(B=65535, Hkv=64, Hq=64, N=1, L=1 << 20)) == 2 and "workgroups" in hils.hils_last_error()
+    assert evict(params(Hkv=65535, Hq=65535, N=1 << 20, L=1 << 20), weights=FAKE, idx=FAKE) == 2
 
 
 def test_workspace_never_falls_as_a_call_grows():

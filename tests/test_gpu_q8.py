@@ -346,6 +346,8 @@ def test_landmark_of_equal_keys_at_the_largest_value():
 EVICT = {
     "steps": (dict(B=3, Hq=8, Hkv=4, N=1, L=64 * 40, d=64, topk=6, window=200), [2560, 700, 64], 10, 1, None),
     "drafts": (dict(B=2, Hq=8, Hkv=2, N=5, L=64 * 40, d=64, topk=6, window=64), [2400, 2001], 3, 4, None),
+    # sequences that hold nothing, or less than the call's new tokens
+    "short_of_drafts": (dict(B=3, Hq=8, Hkv=2, N=200, L=64 * 40, d=64, topk=6, window=64), [0, 150, 2001], 1, 0, None),
     "at_most_7": (dict(B=2, Hq=2, Hkv=1, N=1, L=64 * 50, d=64, topk=4, window=128), [3200, 3000], 0, 2, 7),
     "none": (dict(B=2, Hq=2, Hkv=1, N=1, L=64 * 50, d=64, topk=4, window=128), [3200, 1], 1000, 0, None),
     "zero_most": (dict(B=1, Hq=2, Hkv=1, N=1, L=64 * 50, d=64, topk=4, window=128), None, 1, 0, 0),
