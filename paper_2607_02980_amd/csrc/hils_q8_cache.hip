@@ -33,6 +33,43 @@ __device__ __forceinline__ void load_pair(const T* p, float& x, float& y) {
     }
 }
 
+// W / 2 (or W) neighbouring elements as they lie in memory, in W words.
+template <typename T, int W>
+struct Raw {
+    uint32_t u[W];
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(u[i]);
+        else return __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+    }
+};
+template <typename T>
+using Pair = Raw<T, sizeof(T) / 2>;
+template <typename T>
+using Oct = Raw<T, 2 * sizeof(T)>;
+// (elements that are read once: not kept in the caches; of the alignment of bf16 elements at least)
+template <typename R, typename T>
+__device__ __forceinline__ R load_stream(const T* p) {
+    R r;
+    if constexpr (sizeof(R) == 4) {
+        typedef uint32_t u32 __attribute__((aligned(2)));
+        r.u[0] = __builtin_nontemporal_load(reinterpret_cast<const u32*>(p));
+    } else if constexpr (sizeof(R) == 8) {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+        const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+        r.u[0] = x[0];
+        r.u[1] = x[1];
+    } else {
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(R) / 16; ++i) {
+            const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.u[4 * i + e] = x[e];
+        }
+    }
+    return r;
+}
+
 // ---- new tokens ------------------------------------------------------------------
 //
 // One wave per (sequence, chunk that gets tokens, KV head, K or V).  With a the largest finite
@@ -41,9 +78,11 @@ __device__ __forceinline__ void load_pair(const T* p, float& x, float& y) {
 // y -> e4m3(y * s_old / s): powers of two, so exact unless the result falls below e4m3's
 // normal range.  Infinities, which e4m3 lacks, become NaN, as the conversion makes them.  Bytes of rows at or past the sequence's end are left as they were.
 //
-// A lane holds two neighbouring dims of its rows (d = 64: of half the rows), so that a row is
-// one coalesced load, a chunk's values are in registers between the maximum and the
-// conversion, and V's dim-major row of 64 keys is 64 contiguous bytes of one lane.
+// Bound by memory: 2 (es + 1) d bytes per token and head.  A whole chunk's values stay in
+// registers, as they came, between the maximum and the conversion: of K 8 neighbouring dims per
+// lane and load; of V two dims of all rows (d = 64: of half the rows) per lane, so that a
+// dim-major row of 64 keys is 64 contiguous bytes of one lane.  (65536 tokens of 8 heads, d = 128:
+// 78 us, 5.2 TB/s where a copy of 1 GiB takes 4.8; K by two dims per lane and kept as floats 86.)
 template <typename T, int D>
 __global__ __launch_bounds__(kBlock) void k_q8_append(Q8AppendArgs a, int most) {
     constexpr int LPR = D / 2, TH = kWave / LPR, ROWS = kChunk / TH;  // lanes per row, row groups, rows per lane
@@ -68,38 +107,46 @@ __global__ __launch_bounds__(kBlock) void k_q8_append(Q8AppendArgs a, int most) 
     // row r of the chunk is new token c * 64 + r - start
     const T* src = as<T>(which ? a.v_new : a.k_new) + ((size_t)b * a.Hkv + g) * a.N * D +
                    ((long)c * kChunk - start) * D + dd;
-    if (r0 == 0 && r1 == kChunk) {  // a whole chunk, in registers
-        float x[ROWS][2];
+    if (r0 == 0 && r1 == kChunk) {  // a whole chunk, in registers as it came
         float m = 0.f;
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) load_pair(src + (size_t)(th * ROWS + r) * D, x[r][0], x[r][1]);
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) m = fmaxf(m, fmaxf(finite_abs(x[r][0]), finite_abs(x[r][1])));
-        const float s = scale_for(wave_max(m)), inv = 1.f / s;
-        if (lane == 0) *scale = s;
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            x[r][0] *= inv;
-            x[r][1] *= inv;
-        }
         if (which) {
+            Pair<T> x[ROWS];
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) x[r] = load_stream<Pair<T>>(src + (size_t)(th * ROWS + r) * D);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) m = fmaxf(m, fmaxf(finite_abs(x[r].get(0)), finite_abs(x[r].get(1))));
+            const float s = scale_for(wave_max(m)), inv = 1.f / s;
+            if (lane == 0) *scale = s;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int r = 0; r < ROWS; r += 16) {
                     uint32_t w[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        w[i] = f32x4_to_e4m3(x[r + 4 * i][t], x[r + 4 * i + 1][t], x[r + 4 * i + 2][t],
-                                             x[r + 4 * i + 3][t]);
+                    for (int i = 0; i < 4; ++i) {
+                        const Pair<T>* y = x + r + 4 * i;
+                        w[i] = f32x4_to_e4m3(y[0].get(t) * inv, y[1].get(t) * inv, y[2].get(t) * inv, y[3].get(t) * inv);
+                    }
                     *reinterpret_cast<uint4*>(dst + (dd + t) * kChunk + th * ROWS + r) =
                         make_uint4(w[0], w[1], w[2], w[3]);
                 }
-        } else {
+        } else {  // K: 8 neighbouring dims of a row per lane and load
+            constexpr int LP8 = D / 8, RPL = kWave / LP8, NL = kChunk / RPL;
+            const T* src8 = src - dd + (size_t)(lane / LP8) * D + lane % LP8 * 8;
+            Oct<T> x[NL];
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r)
-                *reinterpret_cast<uint16_t*>(dst + (th * ROWS + r) * D + dd) =
-                    (uint16_t)f32x4_to_e4m3(x[r][0], x[r][1], 0.f, 0.f);
+            for (int i = 0; i < NL; ++i) x[i] = load_stream<Oct<T>>(src8 + (size_t)i * RPL * D);
+#pragma unroll
+            for (int i = 0; i < NL; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_abs(x[i].get(e)));
+            const float s = scale_for(wave_max(m)), inv = 1.f / s;
+            if (lane == 0) *scale = s;
+#pragma unroll
+            for (int i = 0; i < NL; ++i)
+                *reinterpret_cast<uint2*>(dst + (i * RPL + lane / LP8) * D + lane % LP8 * 8) = make_uint2(
+                    f32x4_to_e4m3(x[i].get(0) * inv, x[i].get(1) * inv, x[i].get(2) * inv, x[i].get(3) * inv),
+                    f32x4_to_e4m3(x[i].get(4) * inv, x[i].get(5) * inv, x[i].get(6) * inv, x[i].get(7) * inv));
         }
         return;
     }
