@@ -1,5 +1,7 @@
 // Writing the 8-bit cache (gfx950): new tokens' keys and values, and the landmark rows of the
 // chunks that they complete.  Layout of the cache: hils_q8.hpp.
+#include <type_traits>
+
 #include "hils_dispatch.hpp"
 #include "hils_q8.hpp"
 
@@ -20,19 +22,6 @@ __device__ __forceinline__ float scale_for(float amax) {
     return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 __device__ __forceinline__ float finite_abs(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
-template <typename T>
-__device__ __forceinline__ void load_pair(const T* p, float& x, float& y) {
-    if constexpr (sizeof(T) == 2) {
-        const uint32_t u = *reinterpret_cast<const uint32_t*>(p);
-        x = __uint_as_float(u << 16);
-        y = __uint_as_float(u & 0xffff0000u);
-    } else {
-        const float2 f = *reinterpret_cast<const float2*>(p);
-        x = f.x;
-        y = f.y;
-    }
-}
-
 // W / 2 (or W) neighbouring elements as they lie in memory, in W words.
 template <typename T, int W>
 struct Raw {
@@ -150,54 +139,68 @@ __global__ __launch_bounds__(kBlock) void k_q8_append(Q8AppendArgs a, int most) 
         }
         return;
     }
-    float m = 0.f;
-#pragma unroll 4
-    for (int r = r0 + th; r < r1; r += TH) {
-        float x, y;
-        load_pair(src + (long)r * D, x, y);
-        m = fmaxf(m, fmaxf(finite_abs(x), finite_abs(y)));
-    }
-    float s = scale_for(wave_max(m));
-    if (r0 > 0) {
-        const float old = *scale;
-        s = fmaxf(s, old);
-        if (s != old) {  // the older codes at the new scale
-            const float f = old / s;
-            auto moved = [&](uint32_t w) {
-                float y[4];
-                e4m3_to_f32x4(w, y);
-                return f32x4_to_e4m3(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
-            };
-            if (which) {
-                const int quads = (r0 + 3) / 4;  // dwords of a dim's row with older keys
-                for (int e = lane; e < quads * D; e += kWave) {
-                    uint32_t* w = reinterpret_cast<uint32_t*>(dst + (e % D) * kChunk) + e / D;
-                    const int n = r0 - e / D * 4;
-                    const uint32_t keep = n >= 4 ? 0xffffffffu : (1u << (8 * n)) - 1u, was = *w;
-                    *w = (moved(was) & keep) | (was & ~keep);
+    // Part of a chunk, NB row steps of TH rows at a time (rows past the last one are the last one again).
+    auto partial = [&](auto nb_tag) {
+        constexpr int NB = decltype(nb_tag)::value;
+        Pair<T> x[NB];
+        auto row_at = [&](int base, int i) { return r0 + base + i * TH + th; };
+        auto load = [&](int base) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) x[i] = load_stream<Pair<T>>(src + (long)min(row_at(base, i), r1 - 1) * D);
+        };
+        float m = 0.f;
+        for (int base = 0; base < r1 - r0; base += NB * TH) {
+            load(base);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) m = fmaxf(m, fmaxf(finite_abs(x[i].get(0)), finite_abs(x[i].get(1))));
+        }
+        float s = scale_for(wave_max(m));
+        if (r0 > 0) {
+            const float old = *scale;
+            s = fmaxf(s, old);
+            if (s != old) {  // the older codes at the new scale
+                const float f = old / s;
+                auto moved = [&](uint32_t w) {
+                    float y[4];
+                    e4m3_to_f32x4(w, y);
+                    return f32x4_to_e4m3(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+                };
+                if (which) {
+                    const int quads = (r0 + 3) / 4;  // dwords of a dim's row with older keys
+                    for (int e = lane; e < quads * D; e += kWave) {
+                        uint32_t* w = reinterpret_cast<uint32_t*>(dst + (e % D) * kChunk) + e / D;
+                        const int n = r0 - e / D * 4;
+                        const uint32_t keep = n >= 4 ? 0xffffffffu : (1u << (8 * n)) - 1u, was = *w;
+                        *w = (moved(was) & keep) | (was & ~keep);
+                    }
+                } else {
+                    uint32_t* w = reinterpret_cast<uint32_t*>(dst);
+                    for (int e = lane; e < r0 * D / 4; e += kWave) w[e] = moved(w[e]);
                 }
-            } else {
-                uint32_t* w = reinterpret_cast<uint32_t*>(dst);
-                for (int e = lane; e < r0 * D / 4; e += kWave) w[e] = moved(w[e]);
+                // the new keys' bytes may share a dword with the older ones'
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             }
-            // the new keys' bytes may share a dword with the older ones'
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
-    }
-    if (lane == 0) *scale = s;
-    const float inv = 1.f / s;
-#pragma unroll 4
-    for (int r = r0 + th; r < r1; r += TH) {
-        float x, y;
-        load_pair(src + (long)r * D, x, y);
-        const uint32_t w = f32x4_to_e4m3(x * inv, y * inv, 0.f, 0.f);
-        if (which) {
-            dst[dd * kChunk + r] = (uint8_t)w;
-            dst[(dd + 1) * kChunk + r] = (uint8_t)(w >> 8);
-        } else {
-            *reinterpret_cast<uint16_t*>(dst + r * D + dd) = (uint16_t)w;
+        if (lane == 0) *scale = s;
+        const float inv = 1.f / s;
+        for (int base = 0; base < r1 - r0; base += NB * TH) {
+            if (r1 - r0 > NB * TH) load(base);  // (otherwise they are still there)
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const int r = row_at(base, i);
+                if (r >= r1) continue;
+                const uint32_t w = f32x4_to_e4m3(x[i].get(0) * inv, x[i].get(1) * inv, 0.f, 0.f);
+                if (which) {
+                    dst[dd * kChunk + r] = (uint8_t)w;
+                    dst[(dd + 1) * kChunk + r] = (uint8_t)(w >> 8);
+                } else {
+                    *reinterpret_cast<uint16_t*>(dst + r * D + dd) = (uint16_t)w;
+                }
+            }
         }
-    }
+    };
+    if (r1 - r0 <= TH) partial(std::integral_constant<int, 1>{});  // a decode step's one token
+    else partial(std::integral_constant<int, 16>{});
 }
 
 // ---- landmark rows -----------------------------------------------------------------
