@@ -40,11 +40,12 @@ inline DecLayout q8_layout(int B, int N, int Hkv, int G, int d, int L, int K, in
     o.nlocal = local_pieces_max(W);
     o.nparts = K + o.nlocal;
     const size_t rows = (size_t)B * N * Hkv;
-    // slices of 256 chunks, halved while fewer than four workgroups per CU would scan and a row's
-    // survivors stay within one selection of a wave
+    // slices of 256 chunks, halved while fewer than one workgroup per CU would scan and a row's
+    // survivors stay within one selection of a wave (8 sequences of 64K, the step with 256, 512 and
+    // 1024 workgroups: 24.3, 25.4 and 27.1 us, more survivors to select from each time)
     o.slice = kSlice;
     const long sgroups = (long)B * ((N + 3) / 4) * Hkv;
-    while (o.slice > 64 && sgroups * ((o.nC + o.slice - 1) / o.slice) < 1024 &&
+    while (o.slice > 64 && sgroups * ((o.nC + o.slice - 1) / o.slice) < 256 &&
            (o.nC + o.slice / 2 - 1) / (o.slice / 2) * K <= 4 * kWave)
         o.slice /= 2;
     o.nslices = (o.nC + o.slice - 1) / o.slice;
@@ -73,47 +74,40 @@ struct __align__(16) Q8ScanSmem {
     int oid[NQ][64], tid[NQ][64];
 };
 
-// Scores of one landmark head's rows (chunks first, first + 64, ... of the slice) for nq queries: the
-// plain products, scales and biases come later.  D / 16 lanes read a row, so that a load covers
-// whole 128-byte lines, non-temporal where a step reads each line once, and the next 64 rows are
-// in flight behind the ones that are multiplied.  (On MFMA, whose operand takes half a row per
-// load and lane group: 65 us against 59, and 87 non-temporal, every line fetched twice; 32
-// sequences of 131K.)
-template <typename T, int D, int NQ, bool STREAM>
+// One query, landmarks per head: plain products of 64 rows (scales and biases come later).  D / 16
+// lanes read a row, so that a load covers whole 128-byte lines, non-temporal because a step reads
+// each line once; the next 64 rows are in flight behind the ones that are multiplied.  (As MFMA
+// operands, half a row per load and lane group: 65 us against 59, and 87 non-temporal, every line
+// fetched twice; 32 sequences of 131K.)
+template <typename T, int D>
 struct ScanRows {
     static constexpr int LPR = D / 16, RPL = kWave / LPR, NL = 64 / RPL;  // lanes per row, rows per load, loads
     uint4 x[NL];
     __device__ __forceinline__ void load(const uint8_t* lmk, const int* page, int r0, int len, int Hl, int hl, int lane) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const uint8_t* src =
-                lmk + ((size_t)page[min(r0 + i * RPL + lane / LPR, len - 1)] * Hl + hl) * D + lane % LPR * 16;
-            x[i] = STREAM ? ld_stream16(src) : *reinterpret_cast<const uint4*>(src);
-        }
+        for (int i = 0; i < NL; ++i)
+            x[i] = ld_stream16(lmk + ((size_t)page[min(r0 + i * RPL + lane / LPR, len - 1)] * Hl + hl) * D +
+                               lane % LPR * 16);
     }
-    // score[q * stride + r0 + row]
-    __device__ __forceinline__ void dot(const float (&q)[NQ][16], float* score, int stride, int r0, int lane) const {
+    __device__ __forceinline__ void dot(const float (&q)[16], float* score, int lane) const {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            float y[16];
+            float y[16], part = 0.f;
             e4m3_to_f32x4(x[i].x, y);
             e4m3_to_f32x4(x[i].y, y + 4);
             e4m3_to_f32x4(x[i].z, y + 8);
             e4m3_to_f32x4(x[i].w, y + 12);
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                float part = 0.f;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) part += y[e] * q[n][e];
-                part = group_sum<LPR>(part);
-                if (lane % LPR == 0) score[n * stride + r0 + i * RPL + lane / LPR] = part;
-            }
+            for (int e = 0; e < 16; ++e) part += y[e] * q[e];
+            part = group_sum<LPR>(part);
+            if (lane % LPR == 0) score[i * RPL + lane / LPR] = part;
         }
     }
 };
 
-// Landmarks shared by the group: 64 rows (4 MFMA tiles) against (query, head) columns.  All heads
-// from one read of the row; a wave's VALU would take G products per element.
+// Several queries, or landmarks shared by the group: 64 rows as 4 MFMA tiles against a column per
+// query or (query, head).  (On the vector unit a product per query and element: 4 queries, 8
+// sequences of 64K, 2 us more.)
 template <int D>
 struct LmkBlock {
     uint4 x[4][D / 64];
@@ -187,44 +181,56 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
     }
     const uint8_t* lmk = static_cast<const uint8_t*>(a.lmk);
     const T* qsrc = as<T>(a.q_route ? a.q_route : a.q);
-    const int nblk = (len + 63) / 64;
-    if (!shared) {
-        // units of (head, 64 chunks): wave, wave + 4, ..., the head fastest, so that with four
-        // heads or more a wave keeps its queries
-        using Rows = ScanRows<T, D, NQ, NQ == 1>;
-        const int nunits = G * nblk, seg = lane % Rows::LPR;
+    const int nblk = (len + 63) / 64, gl = shared ? 1 : G;  // blocks of 64 chunks; landmark heads of the group
+    // units of (head, block): wave, wave + 4, ..., the head fastest, so that with four heads or more
+    // a wave keeps its queries
+    const int nunits = gl * nblk;
+    auto head_of = [&](int u) { return shared ? 0 : u % G; };
+    auto row_at = [&](int u) { return (shared ? u : u / G) * 64; };
+    if (NQ == 1 && !shared) {
+        using Rows = ScanRows<T, D>;
+        const int seg = lane % Rows::LPR;
         if (wave < nunits) {
             Rows cur, nxt;
-            float q[NQ][16];
+            float q[16];
             int qh = -1;
-            cur.load(lmk, ss.page, wave / G * 64, len, a.Hl, g * G + wave % G, lane);
+            cur.load(lmk, ss.page, row_at(wave), len, a.Hl, g * G + head_of(wave), lane);
             for (int u = wave; u < nunits; u += kBlock / kWave) {
-                const int hh = u % G, un = min(u + kBlock / kWave, nunits - 1);  // (past the end: discarded)
+                const int hh = head_of(u), un = min(u + kBlock / kWave, nunits - 1);  // (past the end: discarded)
                 if (hh != qh) {
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) {
-                        const T* src = qsrc + q_row(a, b, g * G + hh, n0 + min(n, nq - 1)) * D + seg * 16;
-                        load8(src, q[n]);
-                        load8(src + 8, q[n] + 8);
-                    }
+                    const T* src = qsrc + q_row(a, b, g * G + hh, n0) * D + seg * 16;
+                    load8(src, q);
+                    load8(src + 8, q + 8);
                     qh = hh;
                 }
-                nxt.load(lmk, ss.page, un / G * 64, len, a.Hl, g * G + un % G, lane);
-                cur.dot(q, &ss.score[0][hh][0], G * kSlice, u / G * 64, lane);
+                nxt.load(lmk, ss.page, row_at(un), len, a.Hl, g * G + head_of(un), lane);
+                cur.dot(q, &ss.score[0][hh][row_at(u)], lane);
                 cur = nxt;
             }
         }
-    } else if (wave < nblk) {
-        const int ncol = nq * G, col = min(n16, ncol - 1);
+    } else if (wave < nunits) {
+        // columns: the queries of one head, or, the landmarks shared by the group, (query, head)
+        const int ncol = shared ? nq * G : nq, col = min(n16, ncol - 1);
         QRow<T, D> q;
-        q.load(qsrc + q_row(a, b, g * G + col % G, n0 + col / G) * D, lg, true);
-        LmkBlock<D> x;
-        x.load(lmk, ss.page, wave * 64, len, a.Hl, g, lg, n16);
+        LmkBlock<D> cur, nxt;
+        int qh = -1;
+        cur.load(lmk, ss.page, row_at(wave), len, a.Hl, g * gl + head_of(wave), lg, n16);
+        for (int u = wave; u < nunits; u += kBlock / kWave) {
+            const int hh = head_of(u), un = min(u + kBlock / kWave, nunits - 1);
+            if (hh != qh) {
+                const int qq = shared ? col / G : col, h = shared ? col % G : hh;
+                q.load(qsrc + q_row(a, b, g * G + h, n0 + qq) * D, lg, true);
+                qh = hh;
+            }
+            nxt.load(lmk, ss.page, row_at(un), len, a.Hl, g * gl + head_of(un), lg, n16);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const f32x4 sc = mfma_row<T, D>(x.x[t], q, zero4());
-            if (n16 < ncol)
-                *reinterpret_cast<f32x4*>(&ss.score[n16 / G][n16 % G][wave * 64 + t * 16 + lg * 4]) = sc;
+            for (int t = 0; t < 4; ++t) {
+                const f32x4 sc = mfma_row<T, D>(cur.x[t], q, zero4());
+                if (n16 < ncol)
+                    *reinterpret_cast<f32x4*>(
+                        &ss.score[shared ? n16 / G : n16][shared ? n16 % G : hh][row_at(u) + t * 16 + lg * 4]) = sc;
+            }
+            cur = nxt;
         }
     }
     __syncthreads();
