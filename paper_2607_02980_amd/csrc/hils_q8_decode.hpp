@@ -76,12 +76,14 @@ struct __align__(16) Q8ScanSmem {
 
 // One query, landmarks per head: plain products of 64 rows (scales and biases come later).  D / 16
 // lanes read a row, so that a load covers whole 128-byte lines, non-temporal because a step reads
-// each line once; the next 64 rows are in flight behind the ones that are multiplied.  (As MFMA
-// operands, half a row per load and lane group: 65 us against 59, and 87 non-temporal, every line
-// fetched twice; 32 sequences of 131K.)
+// each line once.  (32 sequences of 131K: 46 us, 6 TB/s; as MFMA operands, half a row per load and
+// lane group, 60, and 83 non-temporal, every line fetched twice; the next 64 rows loaded ahead, 51.)
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 template <typename T, int D>
 struct ScanRows {
     static constexpr int LPR = D / 16, RPL = kWave / LPR, NL = 64 / RPL;  // lanes per row, rows per load, loads
+    static constexpr int S = sizeof(T) == 2 ? 1 : 3;                      // bf16 terms of a query element
+    static_assert(NL == LPR, "a row's lanes end with one row each");
     uint4 x[NL];
     __device__ __forceinline__ void load(const uint8_t* lmk, const int* page, int r0, int len, int Hl, int hl, int lane) {
 #pragma unroll
@@ -89,18 +91,62 @@ struct ScanRows {
             x[i] = ld_stream16(lmk + ((size_t)page[min(r0 + i * RPL + lane / LPR, len - 1)] * Hl + hl) * D +
                                lane % LPR * 16);
     }
-    __device__ __forceinline__ void dot(const float (&q)[16], float* score, int lane) const {
+    // The lane's 16 products are the diagonal of a 4 x 4 block of v_mfma_f32_4x4x4_16b (lane l: row and
+    // column l % 4 of block l / 4), half the vector instructions of multiplying them there; the
+    // sums over a row's lanes halve the rows that a lane still carries each time, down to one.
+    __device__ __forceinline__ void dot(const bf16x4 (&q)[S][4], float* score, int lane) const {
+        float part[NL];
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            float y[16], part = 0.f;
-            e4m3_to_f32x4(x[i].x, y);
-            e4m3_to_f32x4(x[i].y, y + 4);
-            e4m3_to_f32x4(x[i].z, y + 8);
-            e4m3_to_f32x4(x[i].w, y + 12);
+            const bf16x8 lo = bf16x8_of_e4m3(x[i].x, x[i].y), hi = bf16x8_of_e4m3(x[i].z, x[i].w);
+            const bf16x4 a[4] = {bf16x4{lo[0], lo[1], lo[2], lo[3]}, bf16x4{lo[4], lo[5], lo[6], lo[7]},
+                                 bf16x4{hi[0], hi[1], hi[2], hi[3]}, bf16x4{hi[4], hi[5], hi[6], hi[7]}};
+            f32x4 d = zero4();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) part += y[e] * q[e];
-            part = group_sum<LPR>(part);
-            if (lane % LPR == 0) score[i * RPL + lane / LPR] = part;
+            for (int s = S - 1; s >= 0; --s)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    d = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(v4i16, a[t]),
+                                                               __builtin_bit_cast(v4i16, q[s][t]), d, 0, 0, 0);
+            const float e0 = lane & 1 ? d[1] : d[0], e1 = lane & 1 ? d[3] : d[2];
+            part[i] = lane & 2 ? e1 : e0;
+        }
+        int row = lane / LPR;  // of the load that the lane ends with: load number times RPL more
+        if constexpr (NL == 8) {
+            const bool up = lane & 4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float keep = up ? part[i + 4] : part[i], send = up ? part[i] : part[i + 4];
+                part[i] = keep + dpp<0x141>(send);  // the other quad of the 8 lanes, mirrored
+            }
+            row += up ? 4 * RPL : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float keep = lane & 2 ? part[i + 2] : part[i], send = lane & 2 ? part[i] : part[i + 2];
+            part[i] = keep + dpp<0x4E>(send);  // lane ^ 2
+        }
+        const float keep = lane & 1 ? part[1] : part[0], send = lane & 1 ? part[0] : part[1];
+        row += (lane & 2 ? 2 * RPL : 0) + (lane & 1 ? RPL : 0);
+        score[row] = keep + dpp<0xB1>(send);  // lane ^ 1
+    }
+    // the lane's piece of a query
+    static __device__ __forceinline__ void load_q(const T* src, bf16x4 (&q)[S][4]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            bf16x8 y[S];
+            if constexpr (S == 1) {
+                y[0] = ld_bf16x8(src + h * 8);
+            } else {
+                float f[8];
+                load8(src + h * 8, f);
+                split_bf16x8<S>(f, y);
+            }
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                q[s][2 * h] = bf16x4{y[s][0], y[s][1], y[s][2], y[s][3]};
+                q[s][2 * h + 1] = bf16x4{y[s][4], y[s][5], y[s][6], y[s][7]};
+            }
         }
     }
 };
@@ -191,38 +237,33 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
         using Rows = ScanRows<T, D>;
         const int seg = lane % Rows::LPR;
         if (wave < nunits) {
-            Rows cur, nxt;
-            float q[16];
+            Rows cur;
+            bf16x4 q[Rows::S][4];
             int qh = -1;
-            cur.load(lmk, ss.page, row_at(wave), len, a.Hl, g * G + head_of(wave), lane);
             for (int u = wave; u < nunits; u += kBlock / kWave) {
-                const int hh = head_of(u), un = min(u + kBlock / kWave, nunits - 1);  // (past the end: discarded)
+                const int hh = head_of(u);
+                cur.load(lmk, ss.page, row_at(u), len, a.Hl, g * G + hh, lane);
                 if (hh != qh) {
-                    const T* src = qsrc + q_row(a, b, g * G + hh, n0) * D + seg * 16;
-                    load8(src, q);
-                    load8(src + 8, q + 8);
+                    Rows::load_q(qsrc + q_row(a, b, g * G + hh, n0) * D + seg * 16, q);
                     qh = hh;
                 }
-                nxt.load(lmk, ss.page, row_at(un), len, a.Hl, g * G + head_of(un), lane);
                 cur.dot(q, &ss.score[0][hh][row_at(u)], lane);
-                cur = nxt;
             }
         }
     } else if (wave < nunits) {
         // columns: the queries of one head, or, the landmarks shared by the group, (query, head)
         const int ncol = shared ? nq * G : nq, col = min(n16, ncol - 1);
         QRow<T, D> q;
-        LmkBlock<D> cur, nxt;
+        LmkBlock<D> cur;
         int qh = -1;
-        cur.load(lmk, ss.page, row_at(wave), len, a.Hl, g * gl + head_of(wave), lg, n16);
         for (int u = wave; u < nunits; u += kBlock / kWave) {
-            const int hh = head_of(u), un = min(u + kBlock / kWave, nunits - 1);
+            const int hh = head_of(u);
+            cur.load(lmk, ss.page, row_at(u), len, a.Hl, g * gl + hh, lg, n16);
             if (hh != qh) {
                 const int qq = shared ? col / G : col, h = shared ? col % G : hh;
                 q.load(qsrc + q_row(a, b, g * G + h, n0 + qq) * D, lg, true);
                 qh = hh;
             }
-            nxt.load(lmk, ss.page, row_at(un), len, a.Hl, g * gl + head_of(un), lg, n16);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const f32x4 sc = mfma_row<T, D>(cur.x[t], q, zero4());
@@ -230,7 +271,6 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
                     *reinterpret_cast<f32x4*>(
                         &ss.score[shared ? n16 / G : n16][shared ? n16 % G : hh][row_at(u) + t * 16 + lg * 4]) = sc;
             }
-            cur = nxt;
         }
     }
     __syncthreads();
@@ -415,9 +455,11 @@ __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, 
 // gridDim.z workgroups of four waves share the parts of a row.  In a workgroup the last wave selects while the others take their share of the window's pieces, then
 // the selected chunks are spread over all four.  A wave adds its parts into one running
 // (maximum, sum, numerator) per head: part t enters with weight exp(z_t - M), z = s^_c for a chunk,
-// whose P is divided by its own sum, and z = m + log l for a piece of the window.  The next part's
-// K, landmark row and V are loaded as soon as the current one is done with their registers (the
-// loads are the same in every iteration, so that the compiler counts the outstanding ones).
+// whose P is divided by its own sum, and z = m + log l for a piece of the window.  With a row to
+// itself a workgroup has many parts per wave, and the next one's K, landmark row and V are loaded as
+// soon as the current one is done with their registers (the loads are the same in every
+// iteration, so that the compiler counts the outstanding ones); with few there is nothing to load
+// ahead (1024 rows 79 us, without 83; 32 rows of a step the other way round, 19.9 and 18.3).
 // The waves' results meet in LDS, those of several workgroups in the last of them to arrive.
 // (A wave per part with its record in memory and the fusion in a launch of its own: 1024 rows of
 // 25 parts 99 + 14 us.)
@@ -445,6 +487,7 @@ struct Q8RowSmem {
 template <typename T, int D, int G, int E, bool ROUTE, bool SPLIT>
 __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs qa, DecLayout ly) {
     constexpr int NW = kQ8RowWaves, DJ = D / 64, DB = D / 16, PS = sizeof(T) == 2 ? 2 : 3;
+    constexpr bool kAhead = !SPLIT;
     __shared__ __align__(16) Q8RowSmem<T, D, G> sm;
     __shared__ Q8BlockMerge bm;
     const FwdArgs& a = qa.f;
@@ -545,7 +588,7 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
                     mine = {sm.page[at], sm.ks[at], sm.vs[at]};
             }
         }
-        {
+        if constexpr (kAhead) {
             const int page = max(0, __builtin_amdgcn_readlane(mine.page, 0));
             load_k(page, 1);
             load_l(page, 1);
@@ -557,8 +600,13 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
             const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine.vs), it));
             const int at = split + j * ns, slot = phase == 0 ? a.K + at : at;
             const int nk = pg < 0 ? 0 : phase == 0 ? min(kChunk, pos - (ncand + at) * kChunk + 1) : kChunk;
-            const int on = __builtin_amdgcn_readfirstlane((int)(j + step < nj));
-            const int page = max(0, __builtin_amdgcn_readlane(mine.page, it + on));
+            const int on = kAhead ? __builtin_amdgcn_readfirstlane((int)(j + step < nj)) : 1;
+            const int page = max(0, kAhead ? __builtin_amdgcn_readlane(mine.page, it + on) : pg);
+            if constexpr (!kAhead) {
+                load_k(page, 1);
+                load_l(page, 1);
+                load_v(page, 1);
+            }
             // S^T (lane: column n16, keys 16 lg + 4 kb + i), in log2 units; the next K
             const float c1 = a.scale * ks * kLog2e;
             float st[16], mx = -INFINITY;
@@ -568,7 +616,7 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) st[kb * 4 + i] = s4[i] * c1;
             }
-            load_k(page, on);
+            if constexpr (kAhead) load_k(page, on);
             // s^ of head n16: the diagonal of (landmark rows) x q^, held by lane group n16 / 4
             const f32x4 d4 = mfma_row<T, D>(x.l, qr, zero4());
             float dg = d4[0];
@@ -576,7 +624,7 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
             for (int i = 1; i < 4; ++i)
                 if (n16 % 4 == i) dg = d4[i];
             const float sh = c1 * __shfl(dg, n16 + 16 * (n16 / 4), kWave) + (a.bias ? x.bias * kLog2e : 0.f);
-            load_l(page, on);
+            if constexpr (kAhead) load_l(page, on);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 st[i] = lg * 16 + i < nk ? st[i] : -INFINITY;
@@ -622,7 +670,7 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
                     }
                 }
             }
-            load_v(page, on);
+            if constexpr (kAhead) load_v(page, on);
         }
     }
     // ---- the waves' sums, then the workgroups' ----
