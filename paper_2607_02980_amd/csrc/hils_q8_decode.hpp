@@ -24,7 +24,7 @@ namespace hils {
 namespace {
 
 // Workgroups that may share a row, and rows (b, g, n) up to which they do.
-constexpr int kQ8MaxSplit = 8, kQ8SplitRows = 256;
+constexpr int kQ8MaxSplit = 8, kQ8SplitRows = 128;
 
 // Floats of a shared row's records: {M, Z, -, -, numerator[d]} per workgroup and head, then z of
 // each part and head.  The first record's last header word is the row's arrival counter.
@@ -459,7 +459,7 @@ __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, 
 // itself a workgroup has many parts per wave, and the next one's K, landmark row and V are loaded as
 // soon as the current one is done with their registers (the loads are the same in every
 // iteration, so that the compiler counts the outstanding ones); with few there is nothing to load
-// ahead (1024 rows 79 us, without 83; 32 rows of a step the other way round, 19.9 and 18.3).
+// ahead (1024 rows 79 us, without 83; a step of 32 rows the other way round, 19.9 and 18.3).
 // The waves' results meet in LDS, those of several workgroups in the last of them to arrive.
 // (A wave per part with its record in memory and the fusion in a launch of its own: 1024 rows of
 // 25 parts 99 + 14 us.)
@@ -773,13 +773,14 @@ struct Q8DecRun {
                 HILS_LAUNCH("k_q8_scan", (k_q8_scan<T, D, G, NQ>), dim3((pairs + 7) / 8 * 8 * a.Hkv), dim3(kBlock), 0, s,
                             qa, ly, counters);
         };
-        // Two workgroups per CU hold the chip's registers; with fewer rows than that a row goes
-        // over several, down to a part per wave.  (A given selection comes without the scan that
-        // clears the arrival counters: one workgroup per row.)
+        // Above 128 rows a workgroup each; up to 128 four or more each, one per CU (256 rows: 1 workgroup
+        // per row 67.1 us a step, 2 70.9; 160 rows 30.3 and 31.3; 128 rows: 4 23.1, 2 24.9, 6 27.5; 64 rows:
+        // 4 22.9, 7 23.7).  (A given selection comes without the scan that clears the arrival
+        // counters: one workgroup per row.)
         const int rows = R * a.Hkv;
         const int ns = a.given_idx || rows > kQ8SplitRows
                            ? 1
-                           : std::max(1, std::min({kQ8MaxSplit, (ly.nparts + 3) / 4, 2 * cus / rows}));
+                           : std::max(1, std::min({kQ8MaxSplit, (ly.nparts + 3) / 4, std::max(4, cus / rows)}));
         if (a.N == 1)
             scan(std::false_type{}, ns > 1);
         else
