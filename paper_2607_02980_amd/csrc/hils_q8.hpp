@@ -57,6 +57,14 @@ __device__ __forceinline__ void split_bf16x8(const float* x, bf16x8 (&o)[S]) {
         }
 }
 
+// Eight consecutive elements of a caller's array, aligned as its elements are.
+__device__ __forceinline__ bf16x8 load8_unaligned(const bf16* p) {
+    bf16x8 r;
+    __builtin_memcpy(&r, p, sizeof r);
+    return r;
+}
+__device__ __forceinline__ void load8_unaligned(const float* p, float* o) { __builtin_memcpy(o, p, 8 * sizeof(float)); }
+
 // A row of D query elements as MFMA operands against 16-byte loads of an e4m3 row: the lane
 // group lg holds dims 64 j + 16 lg + 0..15 of the row, so operand ks = 2 j + t takes dims
 // 64 j + 16 lg + 8 t + 0..7 (the contraction may run over the dims in any order).
@@ -69,11 +77,11 @@ struct QRow {
         for (int ks = 0; ks < KS; ++ks) {
             const T* src = row + (ks / 2) * 64 + lg * 16 + (ks % 2) * 8;
             if constexpr (sizeof(T) == 2) {
-                const bf16x8 y = ld_bf16x8(src);
+                const bf16x8 y = load8_unaligned(src);
                 x[ks][0] = valid ? y : as_bf16x8(make_uint4(0, 0, 0, 0));
             } else {
                 float y[8];
-                load8(src, y);
+                load8_unaligned(src, y);
 #pragma unroll
                 for (int t = 0; t < 8; ++t) y[t] = valid ? y[t] : 0.f;
                 split_bf16x8<S>(y, x[ks]);

@@ -136,10 +136,10 @@ struct ScanRows {
         for (int h = 0; h < 2; ++h) {
             bf16x8 y[S];
             if constexpr (S == 1) {
-                y[0] = ld_bf16x8(src + h * 8);
+                y[0] = load8_unaligned(src + h * 8);
             } else {
                 float f[8];
-                load8(src + h * 8, f);
+                load8_unaligned(src + h * 8, f);
                 split_bf16x8<S>(f, y);
             }
 #pragma unroll

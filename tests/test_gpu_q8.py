@@ -439,6 +439,85 @@ def test_decode_ties_everywhere(n):
     assert got[2][0, 0, 0].tolist() == list(range(60))
 
 
+def odd(t):
+    """The same values one element past an allocation's start."""
+    return torch.cat([t.new_zeros(1), t.reshape(-1)])[1:].view(t.shape)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 3])
+def test_views_at_odd_offsets(dtype, n):
+    """Queries, new rows, outputs and small arrays need no more than their elements' alignment."""
+    hils = hils_()
+    p = hils.Params(B=2, Hq=8, Hkv=2, N=n, L=1024, d=64, topk=5, window=100, scale=0.125, dtype=dtype)
+    t, dt, i32 = world(p, 41), p.torch_dtype, torch.int32
+    lens = odd(dev(np.int32([1024, 600])))
+    q, qr = dev(t["q"], dt), dev(t["q_route"], dt)
+    pools = lambda: (f8(t["k"]), f8(t["v"]), dev(t["scale"]))  # noqa: E731
+    k, v, sc = pools()
+    args = (f8(t["lmk"]), odd(dev(t["table"])))
+    want = hils.hils_decode_q8_fwd(p, q, k, v, sc, *args, bias_pages=odd(dev(t["bias"])), q_route=qr, seqlens=lens)
+    outs = [odd(torch.empty_like(x)) for x in want]
+    got = hils.hils_decode_q8_fwd(p, odd(q), k, v, sc, *args, bias_pages=odd(dev(t["bias"])), q_route=odd(qr), seqlens=lens,
+                                  out=outs[0], lse=outs[1], idx=outs[2], weights=outs[3])
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    new = dev(rounded(np.random.default_rng(1).standard_normal((2, 2, 70 * n, 64)).astype(np.float32), dtype), dt)
+    pa = hils.Params(B=2, Hq=8, Hkv=2, N=70 * n, L=1024, d=64, topk=5, window=100, dtype=dtype)
+    a, b = pools(), pools()
+    hils.hils_q8_append(pa, new, new, *a, dev(t["table"]), lens)
+    hils.hils_q8_append(pa, odd(new), odd(new), *b, odd(dev(t["table"])), lens)
+    assert all(np.array_equal(codes(x), codes(y)) for x, y in zip(a[:2], b[:2])) and torch.equal(a[2], b[2])
+    lq = dev(rounded(np.random.default_rng(2).standard_normal((2, 8, (70 * n + 63) // 64, 64)).astype(np.float32), dtype), dt)
+    la, lb = [(f8(t["lmk"]), dev(t["bias"])) for _ in range(2)]
+    hils.hils_q8_landmark_fwd(pa, lq, a[0], a[2], dev(t["table"]), *la, lens)
+    hils.hils_q8_landmark_fwd(pa, odd(lq), a[0], a[2], dev(t["table"]), lb[0], lb[1], lens)
+    assert np.array_equal(codes(la[0]), codes(lb[0])) and torch.equal(la[1], lb[1])
+
+
+def test_pools_past_4_gib():
+    """Pages whose bytes lie past 2^32: a small cache at the end of large pools."""
+    hils = hils_()
+    p = hils.Params(B=2, Hq=4, Hkv=1, N=1, L=512, d=128, topk=3, window=64, scale=0.125)
+    t = world(p, 43)
+    n, P = len(t["k"]), 600000
+    k, v = (torch.zeros((P, 1) + s, dtype=torch.uint8, device="cuda").view(F8) for s in ((64, 128), (128, 64)))
+    lm, sc, table = torch.zeros((P, 4, 128), dtype=torch.uint8, device="cuda").view(F8), torch.ones((P, 1, 2), device="cuda"), t["table"] + P - n
+    for big, small in ((k, t["k"]), (v, t["v"]), (lm, t["lmk"])):
+        big.view(torch.uint8)[P - n:] = dev(small)
+    sc[P - n:] = dev(t["scale"])
+    ref = Q.decode(p, t["q"], t["k"], t["v"], t["scale"], t["lmk"], t["table"])
+    check_decode(p, hils.hils_decode_q8_fwd(p, dev(t["q"], p.torch_dtype), k, v, sc, lm, dev(table)), ref)
+    new = rounded(np.random.default_rng(1).standard_normal((2, 1, 1, 128)).astype(np.float32), "bf16")
+    want = Q.append(p, new, new, t["k"], t["v"], t["scale"], t["table"], [400, 512])
+    hils.hils_q8_append(p, dev(new, p.torch_dtype), dev(new, p.torch_dtype), k, v, sc, dev(table), dev(np.int32([400, 512])))
+    assert same_codes(codes(k[P - n:]), want[0]) and same_codes(codes(v[P - n:]), want[1])
+    assert np.array_equal(sc[P - n:].cpu().numpy(), want[2]) and not codes(k[:P - n]).any()
+
+
+def test_refusals_of_tensors():
+    """What the binding says of tensors that a call cannot take."""
+    hils = hils_()
+    p = hils.Params(B=2, Hq=4, Hkv=2, N=2, L=256, d=64, topk=2, window=64)
+    t = world(p, 5)
+    good = dict(q=dev(t["q"], torch.bfloat16), k_pages=f8(t["k"]), v_pages=f8(t["v"]), kv_scale=dev(t["scale"]),
+                lmk_pages=f8(t["lmk"]), block_table=dev(t["table"]))
+    hils.hils_decode_q8_fwd(p, **good)
+    for name, bad, what in (("q", good["q"].float(), "dtype"), ("q", good["q"].transpose(1, 2), "contiguous"),
+                            ("k_pages", good["v_pages"][:, :, :32], "contiguous"), ("v_pages", good["k_pages"].view(torch.uint8), "dtype"),
+                            ("kv_scale", good["kv_scale"][..., 0].contiguous(), "shape"), ("block_table", good["block_table"].long(), "dtype"),
+                            ("lmk_pages", good["lmk_pages"].cpu(), "GPU tensor"), ("q", good["q"].cpu(), "GPU tensor")):
+        with pytest.raises(ValueError, match=what):
+            hils.hils_decode_q8_fwd(p, **{**good, name: bad})
+    with pytest.raises(hils.HilsError, match="workspace"):
+        hils.hils_decode_q8_fwd(p, **good, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError, match="needs idx"):
+        hils.hils_decode_q8_fwd(hils.Params(B=2, Hq=4, Hkv=2, N=2, L=256, d=64, topk=2, window=64, flags=hils.HILS_FLAG_GIVEN_IDX), **good)
+    with pytest.raises(ValueError, match="shape"):
+        hils.hils_cache_evict(p, torch.zeros((2, 5), device="cuda"), good["block_table"])
+    with pytest.raises(hils.HilsError, match=">= 0"):
+        hils.hils_cache_evict(p, torch.zeros((2, 4), device="cuda"), good["block_table"], budget=-1)
+
+
 def test_a_sequence_lives():
     """A prompt in two pieces, decode steps with drafts, eviction, more steps: every output against the
     oracle's own cache, on another stream, the steps captured into a graph and replayed between eager work."""
