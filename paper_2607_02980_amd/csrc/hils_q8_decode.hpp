@@ -13,7 +13,7 @@
 // into O^T = V^T P^T without leaving its lane, and nothing of a part passes through LDS.
 // (Several new queries of a sequence are rows of their own: their windows meet in an XCD's L2,
 // which all rows of a KV group share with Hkv a multiple of 8, and a value behind a query never
-// meets its products.  One tile for the window of 4 queries: 4 x 64K of 8 sequences 28 us, now 23.)
+// meets its products.  One tile for the window of 4 queries, 8 sequences of 64K: parts and fusion 25 us, now 20.)
 #pragma once
 
 #include "hils_decode.hpp"
@@ -76,8 +76,9 @@ struct __align__(16) Q8ScanSmem {
 
 // One query, landmarks per head: plain products of 64 rows (scales and biases come later).  D / 16
 // lanes read a row, so that a load covers whole 128-byte lines, non-temporal because a step reads
-// each line once.  (32 sequences of 131K: 46 us, 6 TB/s; as MFMA operands, half a row per load and
-// lane group, 60, and 83 non-temporal, every line fetched twice; the next 64 rows loaded ahead, 51.)
+// each line once.  (32 sequences of 131K: 48 us, 5.6 TB/s of landmarks; as MFMA operands, half a
+// row per load and lane group, 62, and 83 non-temporal, every line fetched twice; the next 64 rows
+// loaded ahead, 54.)
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 template <typename T, int D>
 struct ScanRows {
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
     const int ngrp = (a.N + NQ - 1) / NQ;
     // (slice, query group) pairs are dealt to the XCDs (block x runs on XCD x mod 8), a pair's KV
     // groups one after the other on one: a page's scales of all heads are one line, its
-    // landmarks 4 KB in one place (slices fastest: scan of 32 sequences of 131K 74 us, now 59)
+    // landmarks 4 KB in one place (slices fastest: scan of 32 sequences of 131K 74 us against 59)
     const int xcd = blockIdx.x % 8, seq = blockIdx.x / 8, g = seq % a.Hkv, pair = seq / a.Hkv * 8 + xcd;
     const int slice = pair % ly.nslices, bz = pair / ly.nslices;
     const int b = bz / ngrp, n0 = (bz % ngrp) * NQ;
@@ -321,7 +322,7 @@ __device__ __forceinline__ uint32_t keys_below(int k0, int nk) {
 // above the step that holds the K-th is in, everything below it out), narrowed to that step
 // until at most 64 entries are left at or above it, which one wave ranks exactly.  More equal keys than
 // that go the way of the smaller selections.  (2048 survivors: one wave, two rounds of 1024,
-// 1M x 4 step 85 us; now 72.)
+// 1M x 4 step 85 us, with the histograms 75.)
 struct __align__(16) Q8BlockMerge {
     uint32_t lo[kBlock / kWave], hi[kBlock / kWave];
     int hist[1024];
@@ -462,7 +463,7 @@ __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, 
 // ahead (1024 rows 79 us, without 83; a step of 32 rows the other way round, 19.9 and 18.3).
 // The waves' results meet in LDS, those of several workgroups in the last of them to arrive.
 // (A wave per part with its record in memory and the fusion in a launch of its own: 1024 rows of
-// 25 parts 99 + 14 us.)
+// 25 parts 95 + 10 us, now 76.)
 constexpr int kQ8RowWaves = 4;
 template <typename T>
 __device__ __forceinline__ void q8_store_out(const FwdArgs& a, size_t at, const f32x4& o) {
