@@ -5,7 +5,7 @@
 namespace hils {
 
 size_t q8_decode_workspace_bytes(int B, int N, int Hkv, int G, int d, int L, int K, int W) {
-    return q8_layout(B, N, Hkv, G, d, L, K, W).total;
+    return q8_layout(B, N, Hkv, G, d, L, K, W, false).total;  // (the same with shared landmarks)
 }
 
 hipError_t launch_q8_decode(const Q8DecodeArgs& a, hipStream_t s) {

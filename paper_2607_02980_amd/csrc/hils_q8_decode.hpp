@@ -34,18 +34,20 @@ __host__ __device__ __forceinline__ int q8_row_floats(int nparts, int G, int d) 
 
 // Workspace: the slices' survivors (as in dec_layout), then the records.  Room for the finest
 // slices and for every shared row, so that the size never falls as a call grows.
-inline DecLayout q8_layout(int B, int N, int Hkv, int G, int d, int L, int K, int W) {
+inline DecLayout q8_layout(int B, int N, int Hkv, int G, int d, int L, int K, int W, bool shared) {
     DecLayout o = {};
     o.nC = L / kChunk;
     o.nlocal = local_pieces_max(W);
     o.nparts = K + o.nlocal;
     const size_t rows = (size_t)B * N * Hkv;
-    // slices of 256 chunks, halved while fewer than one workgroup per CU would scan and a row's
-    // survivors stay within one selection of a wave (8 sequences of 64K, the step with 256, 512 and
-    // 1024 workgroups: 24.3, 25.4 and 27.1 us, more survivors to select from each time)
+    // slices of 256 chunks, halved while fewer than four workgroups per CU would scan (two where the
+    // group shares its landmarks and a slice is a quarter of the bytes) and a row's survivors stay
+    // within one selection of a wave (steps with 256, 512, 1024 and 2048 workgroups: 8 sequences of
+    // 64K 23.0, 22.3, 21.8 and 21.7 us, 16 of 64K and 4 new tokens 59.3, 59.2, 58.1 and 56.7, 48 of
+    // 30K 58.7, 58.5, 56.2 and 58.2; 24 of 60K, shared landmarks, 30.8, 29.8, 31.3 and 33.4)
     o.slice = kSlice;
-    const long sgroups = (long)B * ((N + 3) / 4) * Hkv;
-    while (o.slice > 64 && sgroups * ((o.nC + o.slice - 1) / o.slice) < 256 &&
+    const long sgroups = (long)B * ((N + 3) / 4) * Hkv, full = shared ? 512 : 1024;
+    while (o.slice > 64 && sgroups * ((o.nC + o.slice - 1) / o.slice) < full &&
            (o.nC + o.slice / 2 - 1) / (o.slice / 2) * K <= 4 * kWave)
         o.slice /= 2;
     o.nslices = (o.nC + o.slice - 1) / o.slice;
@@ -765,7 +767,7 @@ struct Q8DecRun {
     template <typename T, int D, int G>
     static hipError_t run(const Q8DecodeArgs& qa, hipStream_t s) {
         const FwdArgs& a = qa.f;
-        const DecLayout ly = q8_layout(a.B, a.N, a.Hkv, G, D, a.L, a.K, a.W);
+        const DecLayout ly = q8_layout(a.B, a.N, a.Hkv, G, D, a.L, a.K, a.W, a.Hl != a.Hq);
         const int R = a.B * a.N, cus = device_cus(), surv = ly.nslices * a.K;
         auto scan = [&](auto many_tag, int counters) {
             constexpr int NQ = scan_queries<G>(decltype(many_tag)::value);
