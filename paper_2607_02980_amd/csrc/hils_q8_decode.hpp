@@ -330,7 +330,7 @@ struct __align__(16) Q8BlockMerge {
     int hist[1024];
     int id[64], oid[64], tid[64];
     float sc[64], osc[64], tsc[64];
-    int count, step, above;
+    int count, kept, step, above;
 };
 template <typename MS>
 __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, Q8BlockMerge& bm, MS& ms) {
@@ -369,7 +369,7 @@ __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, 
         hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, kWave));
         n += __shfl_xor(n, o, kWave);
     }
-    if (tid == 0) bm.count = 0;
+    if (tid == 0) bm.count = bm.kept = 0;
     __syncthreads();
     if (lane == 0) {
         bm.lo[w] = lo;
@@ -435,11 +435,9 @@ __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, 
         __syncthreads();
         return ms.nbest;
     }
-    if (tid == 0) bm.count = 0;
-    __syncthreads();
     each([&](uint32_t k, int e) {
-        if (k >= from) {
-            const int at = atomicAdd(&bm.count, 1);
+        if (k >= from) {  // (counted apart: a wave may be here before another has read the first count)
+            const int at = atomicAdd(&bm.kept, 1);
             bm.id[at] = cand_id[base + e];
             bm.sc[at] = cand_sc[base + e];
         }

@@ -427,6 +427,24 @@ def test_evict_negative_nan():
 
 
 @pytest.mark.parametrize("n", [1, 3])
+def test_decode_short_sequences_in_a_large_cache(n):
+    """Slices enough for the whole workgroup's selection, but no more than 64 survivors in any row: it
+    has nothing to narrow down.  The pages past the sequences' ends are one page of NaN."""
+    hils = hils_()
+    kw = dict(B=12, Hq=16, Hkv=8, N=n, d=64, topk=64, window=128, scale=0.125)
+    lens = [130 + 150 * b for b in range(12)]
+    small, p = hils.Params(L=2048, **kw), hils.Params(L=64 * 1500, **kw)
+    t = world(small, 91 + n)
+    bury(t, small, lens)
+    ref = Q.decode(small, t["q"], t["k"], t["v"], t["scale"], t["lmk"], t["table"], seqlens=np.int32(lens))
+    unused = (set(range(len(t["k"]))) - set(t["table"].ravel().tolist())).pop()
+    table = np.full((p.B, p.L // 64), unused, np.int32)
+    table[:, :32] = t["table"]
+    t["table"] = table
+    check_decode(p, run_decode(p, t, lens), ref)
+
+
+@pytest.mark.parametrize("n", [1, 3])
 def test_decode_ties_everywhere(n):
     """Equal scores of every candidate: the lowest chunks are chosen, however many survivors tie."""
     hils = hils_()
