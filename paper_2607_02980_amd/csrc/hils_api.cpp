@@ -447,7 +447,7 @@ int hils_cache_evict(const hils_params* p, const float* acc, const int32_t* bloc
     if (budget < 0 || sink < 0 || max_evict < 0)
         return fail(HILS_ERR_INVALID, "budget, sink and max_evict must be >= 0 (budget=%d sink=%d max_evict=%d)", budget,
                     sink, max_evict);
-    if (weights && ((double)p->Hkv * p->N * (p->topk + (p->window + 62) / 64 + 1) > 0x7fffffff))
+    if (weights && ((double)p->Hkv * p->N * (p->topk + (p->window + 62) / 64 + 1) > 0x7ffffbff))  // (and a step of 1024)
         return fail(HILS_ERR_UNSUPPORTED, "Hkv=%d N=%d topk=%d: more weights per sequence than 2^31", p->Hkv, p->N,
                     p->topk);
     if (max_evict > 0 && !freed) return fail(HILS_ERR_INVALID, "max_evict=%d, so freed must be non-NULL", max_evict);
