@@ -301,10 +301,11 @@ int hils_landmark_bwd(const hils_params* p, const void* lq, const void* k, const
  *   lmk_pages [num_pages, Hl, d]       landmark k'_c of the page's chunk, x stands for
  *                                      x * kv_scale[page, g, 0], g the head's KV group
  *   bias_pages [num_pages, Hl] f32     landmark bias b'_c
- * and chunk c of sequence b is page block_table[b, c] ([B, L/S] int32, device; an
- * entry outside [0, num_pages) is clamped into it; entries of chunks at or past a
- * sequence's length are not read).  k_pages, v_pages, lmk_pages and the workspace must
- * be 16-byte aligned, kv_scale 8-byte aligned.
+ * and chunk c of sequence b is page block_table[b, c] ([B, L/S] int32, device; reads
+ * clamp an entry outside [0, num_pages) into it, and what would be written to such a
+ * page is dropped; entries of chunks at or past a sequence's length are not read).
+ * k_pages, v_pages, lmk_pages and the workspace must be 16-byte aligned, kv_scale
+ * 8-byte aligned.
  *
  * hils_q8_append writes new tokens' keys and values: sequence b appends the first
  * newlens[b] rows of k_new and v_new ([B, Hkv, N, d], dtype; newlens [B] int32, NULL: N

@@ -105,10 +105,6 @@ __device__ __forceinline__ f32x4 mfma_row(const uint4 (&a)[D / 64], const QRow<T
     return acc;
 }
 
-__device__ __forceinline__ int clamp_page(int p, int num_pages) {
-    return p < 0 ? 0 : (p >= num_pages ? num_pages - 1 : p);
-}
-
 // Tokens of sequence b and how many of them are new (at most N of the last ones).
 template <typename A>
 __device__ __forceinline__ int q8_tokens(const A& a, int b, int& fresh) {

@@ -65,7 +65,9 @@ __device__ __forceinline__ R load_stream(const T* p) {
 // magnitude among the chunk's new rows, s = scale_for(a), or the scale the chunk has if it
 // holds older tokens and that one is larger; new x -> e4m3(x / s).  Where s grew, older codes
 // y -> e4m3(y * s_old / s): powers of two, so exact unless the result falls below e4m3's
-// normal range.  Infinities, which e4m3 lacks, become NaN, as the conversion makes them.  Bytes of rows at or past the sequence's end are left as they were.
+// normal range.  Infinities, which e4m3 lacks, become NaN, as the conversion makes them.  Bytes of
+// rows at or past the sequence's end are left as they were; tokens of a chunk without a page
+// (a table entry outside the pool) are dropped.
 //
 // Bound by memory: 2 (es + 1) d bytes per token and head.  A whole chunk's values stay in
 // registers, as they came, between the maximum and the conversion: of K 8 neighbouring dims per
@@ -89,7 +91,9 @@ __global__ __launch_bounds__(kBlock) void k_q8_append(Q8AppendArgs a, int most) 
     const int c = start / kChunk + j;
     const int r0 = j == 0 ? start % kChunk : 0, r1 = min(kChunk, len - c * kChunk);  // the chunk's new rows
     if (fresh == 0 || r1 <= r0) return;
-    const size_t page = clamp_page(a.block_table[(size_t)b * (a.L / kChunk) + c], a.num_pages);
+    const int entry = a.block_table[(size_t)b * (a.L / kChunk) + c];
+    if (entry < 0 || entry >= a.num_pages) return;  // (no page: another sequence's stays as it is)
+    const size_t page = entry;
     const size_t pg = page * a.Hkv + g;
     uint8_t* dst = static_cast<uint8_t*>(which ? a.v_pages : a.k_pages) + pg * kChunk * D;
     float* scale = a.kv_scale + pg * 2 + which;
@@ -231,7 +235,9 @@ __global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int mo
     const int len = q8_tokens(a, b, fresh);
     const int c = (len - fresh) / kChunk + j;
     if (c >= len / kChunk) return;
-    const size_t page = clamp_page(a.block_table[(size_t)b * (a.L / kChunk) + c], a.num_pages);
+    const int entry = a.block_table[(size_t)b * (a.L / kChunk) + c];
+    if (entry < 0 || entry >= a.num_pages) return;  // (no page: another sequence's stays as it is)
+    const size_t page = entry;
     const uint8_t* kp = static_cast<const uint8_t*>(a.k_pages) + (page * a.Hkv + g) * kChunk * D;
     const int hl0 = g * GL;
     QRow<T, D> q;

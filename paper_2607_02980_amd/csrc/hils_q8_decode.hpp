@@ -453,8 +453,9 @@ __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, 
     return m;
 }
 
-// gridDim.z workgroups of four waves share the parts of a row.  In a workgroup the last wave selects while the others take their share of the window's pieces, then
-// the selected chunks are spread over all four.  A wave adds its parts into one running
+// gridDim.z workgroups of four waves share the parts of a row.  In a workgroup the last wave selects
+// while the others take their share of the window's pieces, then the selected chunks are spread
+// over all four.  A wave adds its parts into one running
 // (maximum, sum, numerator) per head: part t enters with weight exp(z_t - M), z = s^_c for a chunk,
 // whose P is divided by its own sum, and z = m + log l for a piece of the window.  With a row to
 // itself a workgroup has many parts per wave, and the next one's K, landmark row and V are loaded as

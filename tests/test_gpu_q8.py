@@ -297,6 +297,31 @@ def test_append_extreme_values(dtype, n, start):
     assert same_codes(got[0], ref[0]) and same_codes(got[1], ref[1])
 
 
+def test_writes_without_a_page_are_dropped():
+    """Table entries outside the pool: nothing is written for those chunks, to no page; the others as ever."""
+    hils = hils_()
+    p = hils.Params(B=3, Hq=2, Hkv=2, N=200, L=256, d=64, topk=1, window=64, flags=0)
+    new, pools, scale, table = append_inputs(p, 21)
+    lens, counts = [256, 201, 64], [200, 200, 64]
+    lone = table.copy()  # the same call with pages of their own for the chunks without one
+    n = len(pools[0])
+    for i, (b, c, bad) in enumerate(((0, 1, -1), (0, 3, n), (1, 0, -2 ** 31), (1, 3, 2 ** 31 - 1))):
+        table[b, c], lone[b, c] = bad, n + i
+    wide = [np.concatenate([x, np.zeros((4,) + x.shape[1:], x.dtype)]) for x in (*pools, scale)]
+    ref = Q.append(p, *new, *wide, lone, lens, counts)
+    got = run_append(p, new, pools, scale, table, lens, counts)
+    assert np.array_equal(got[2], ref[2][:n])
+    assert same_codes(got[0], ref[0][:n]) and same_codes(got[1], ref[1][:n])
+    lmk, bias = np.full((n, 2, 64), 0x5a, np.uint8), np.full((n, 2), 7, np.float32)
+    tl, tb = f8(lmk), dev(bias)
+    lq = torch.zeros((3, 2, 4, 64), dtype=torch.bfloat16, device="cuda")
+    hils.hils_q8_landmark_fwd(p, lq, f8(got[0]), dev(got[2]), dev(table), tl, tb, dev(np.int32(lens)), dev(np.int32(counts)))
+    written = [table[b, c] for b, c in ((0, 0), (0, 2), (1, 1), (1, 2), (2, 0))]
+    keep = [i for i in range(n) if i not in written]
+    assert (codes(tl)[keep] == 0x5a).all() and (tb.cpu().numpy()[keep] == 7).all()
+    assert (np.abs(tb.cpu().numpy()[written] - np.log(64)) < 1e-4).all()
+
+
 LANDMARK = {
     "step": (dict(B=4, Hq=8, Hkv=2, N=1, L=256, d=128), [64, 63, 256, 129], None, False),
     "prompt": (dict(B=2, Hq=8, Hkv=1, N=300, L=512, d=64), [300, 500], [300, 130], False),
