@@ -213,9 +213,10 @@ __global__ __launch_bounds__(kBlock) void k_q8_append(Q8AppendArgs a, int most) 
 // the group's GL landmark heads as MFMA columns: S^T = K Q'^T from K rows as they lie in the
 // page, the softmax over the lane groups, b' = log l - sum_j p_j s_j (s from its maximum), and
 // k' / ks = X^T P^T with X^T by transposing reads of the rows, as bf16, in the wave's LDS tile
-// and P in two bf16 terms (2^-17 of it, below e4m3's 2^-4 by far).  Bound by memory: 64 d + GL (d + 4)
-// bytes per wave.  (Products with P on the vector unit, key by key from LDS: 512 chunks of 32
-// heads 18 us, 24 chunks 12 us.)
+// and P in three bf16 terms, which hold its float32 (two, 2^-17 of it, show where a row's sum
+// cancels, and take 11.5 us of the 12.2 for 512 chunks of 32 heads).  Bound by memory:
+// 64 d + GL (d + 4) bytes per wave.  (Products with P on the vector unit, key by key from LDS: 512
+// chunks of 32 heads 18 us, 24 chunks 12 us.)
 template <int D>
 struct LmkTile {
     static constexpr int ROW = D + 16;  // (transposing reads of padded rows meet two addresses per bank)
@@ -289,9 +290,9 @@ __global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int mo
     ps = group4_sum(ps);
     const float inv = 1.f / l;
     if (n16 < GL && lg == 0) a.bias_pages[page * a.Hl + hl0 + n16] = logf(l) - ps * inv;
-    bf16x8 p0[2], p1[2];
-    split_bf16x8<2>(s, p0);
-    split_bf16x8<2>(s + 8, p1);
+    bf16x8 p0[3], p1[3];
+    split_bf16x8<3>(s, p0);
+    split_bf16x8<3>(s + 8, p1);
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     // (lane: head n16, dims 16 db + 4 lg + i; a convex combination of codes: above 448 by the
@@ -300,10 +301,12 @@ __global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int mo
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
         const bf16x8 x0 = tr_operand_perm(tile, ROW, 0, db * 16, lane), x1 = tr_operand_perm(tile, ROW, 32, db * 16, lane);
-        o[db] = mfma16x16x32(x0, p0[1], zero4());
-        o[db] = mfma16x16x32(x1, p1[1], o[db]);
-        o[db] = mfma16x16x32(x0, p0[0], o[db]);
-        o[db] = mfma16x16x32(x1, p1[0], o[db]);
+        o[db] = zero4();
+#pragma unroll
+        for (int t = 2; t >= 0; --t) {
+            o[db] = mfma16x16x32(x0, p0[t], o[db]);
+            o[db] = mfma16x16x32(x1, p1[t], o[db]);
+        }
     }
     if (n16 < GL) {
         uint8_t* dst = static_cast<uint8_t*>(a.lmk_pages) + (page * a.Hl + hl0 + n16) * D + lg * 4;
