@@ -42,7 +42,7 @@ __device__ __forceinline__ bf16x8 bf16x8_of_e4m3(uint32_t lo, uint32_t hi) {
 }
 
 // x as the sum of S bf16 values, largest first: S = 3 holds a float32 to its last bit
-// (3 x 8 significant bits), S = 2 to 2^-17 of it.
+// (3 x 8 significant bits).
 template <int S>
 __device__ __forceinline__ void split_bf16x8(const float* x, bf16x8 (&o)[S]) {
     float r[8];

@@ -61,3 +61,30 @@ def test_landmark_rows(d, dtype):
     for page, (rows, _) in ref.items():
         assert np.abs(rows[:, 1:]).max() < 2.0 ** -6
         assert np.abs(got[page] - rows)[:, 1:].max() <= 2.0 ** -10 + TOL
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [8, 24])  # 64 rows, which workgroups share, and 192, a workgroup each
+@pytest.mark.parametrize("d", [64, 128])
+def test_decode(d, B, dtype):
+    hils = T.hils_()
+    p = hils.Params(B=B, Hq=8, Hkv=8, N=1, L=1024, d=d, topk=16, window=512, scale=0.125, dtype=dtype)
+    r = np.random.default_rng(d + B)
+    P, q = B * 16, np.zeros((B, 8, 1, d), np.float32)
+    table = r.permutation(P).reshape(B, 16).astype(np.int32)
+    q[..., 0] = queries(r, (B, 8, 1))
+    k, v = np.zeros((P, 8, 64, d), np.uint8), np.zeros((P, 8, d, 64), np.uint8)
+    k[:, :, ::2, 0], k[:, :, 1::2, 0] = Q.encode(128), Q.encode(120)
+    for b in range(B):
+        for h in range(8):
+            for c in range(16):
+                x = codes_that_cancel(r, 0.125 * 2.0 ** -7 * 8 * q[b, h, 0, 0], d)
+                x[:, 0] = x[:, 1]
+                v[table[b, c], h] = Q.encode(x.T)
+    scale, lmk = np.full((P, 8, 2), 2.0 ** -7, np.float32), np.zeros((P, 8, d), np.uint8)
+    ref = Q.decode(p, q, k, v, scale, lmk, table)
+    out, lse, idx, wt = hils.hils_decode_q8_fwd(p, T.dev(q, p.torch_dtype), T.f8(k), T.f8(v), T.dev(scale), T.f8(lmk), T.dev(table))
+    torch.cuda.synchronize()
+    assert np.array_equal(idx.cpu().numpy(), ref[2]) and np.abs(ref[0]).max() < 0.01 * 2.0 ** -7 * 1.01
+    off = np.abs(T.host(out) - ref[0])
+    assert (off <= TOL * 2.0 ** -7 + (2.0 ** -8 * np.abs(ref[0]) if dtype == "bf16" else 0)).all()
