@@ -11,6 +11,8 @@
 // sequence and a dozen dependent phases.  Up to kMaxHeld chunks a sequence's totals stay in LDS
 // and its table in registers between the phases (k_evict); longer ones are read again from the L2 in
 // each (k_evict_long; 16384 chunks cut to 4096: 46 us, k_evict 14).
+#include <climits>
+
 #include "hils_dispatch.hpp"
 #include "hils_internal.hpp"
 
@@ -40,9 +42,17 @@ __device__ __forceinline__ int below(bool x, int& all) {
 __device__ __forceinline__ uint32_t total_key(float x) { return x != x ? 0xfffffffeu : ordered_key(x + 0.f); }
 __device__ __forceinline__ float key_total(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
+// Whether slot t of a selection row does not follow on the one before it.  A row without such a slot
+// ascends and then is padded, so it names a chunk once; a given one may name a chunk again behind
+// another entry ([5, -1, 5]: both slots count, as they do in decode), and its weights are then added
+// one slot after the other, not by two threads at a time.
+__device__ __forceinline__ bool out_of_order(const int32_t* row, int t) {
+    return t > 0 && row[t] >= 0 && row[t] <= (row[t - 1] < 0 ? INT_MAX : row[t - 1]);
+}
+
 __global__ __launch_bounds__(kEvictBlock) void k_evict_long(EvictArgs a) {
     __shared__ int s_hist[256];
-    __shared__ int s_bin, s_k;
+    __shared__ int s_bin, s_k, s_odd;
     __shared__ int s_tie[kEvictWaves], s_gone[kEvictWaves];
     const int b = blockIdx.x, tid = threadIdx.x, w = wave_id(), lane = tid % kWave;
     const int nC = a.L / kChunk;
@@ -54,25 +64,31 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict_long(EvictArgs a) {
     int32_t* freed = a.freed ? a.freed + (size_t)b * a.most : nullptr;
 
     // ---- the totals ----
+    if (tid == 0) s_odd = 0;
     if (acc != acc_in)
         for (int c = tid; c < nC; c += kEvictBlock) acc[c] = acc_in[c];
     __syncthreads();  // (also: every wave has read the length that seqlens_out may replace)
     if (a.weights) {
         const int pieces = (a.W + 62) / kChunk + 1, per = a.K + pieces;
-        // row after row, so that a total is one sum in one order; a row names a chunk once
+        // row after row, so that a total is one sum in one order; a thread per weight of a row (at most
+        // 64 slots and 64 pieces)
         for (int r = 0; r < a.Hkv * a.N; ++r) {
-            const int g = r / a.N, n = r % a.N, pos = len - a.N + n, ncand = n_candidates(pos, a.W);
+            const int g = r / a.N, n = r % a.N, pos = len - a.N + n, ncand = n_candidates(pos, a.W), t = tid;
             const size_t rg = ((size_t)b * a.Hkv + g) * a.N + n;
-            for (int t = tid; t < per; t += kEvictBlock) {
-                int c = -1;
-                if (t < a.K) {
-                    if (idx_entry_valid(a.idx + rg * a.K, t, ncand)) c = a.idx[rg * a.K + t];
-                } else if (ncand + t - a.K <= pos / kChunk) {
-                    c = ncand + t - a.K;
-                }
-                if (c >= 0) acc[c] += a.weights[rg * per + t];
+            const int32_t* row = a.idx + rg * a.K;
+            int c = -1;
+            if (t < a.K) {
+                if (idx_entry_valid(row, t, ncand)) c = row[t];
+                if (out_of_order(row, t)) s_odd = 1;
+            } else if (t < per && ncand + t - a.K <= pos / kChunk) {
+                c = ncand + t - a.K;
             }
             __syncthreads();
+            const int steps = s_odd ? a.K : 1;  // (from the first such row on)
+            for (int u = 0; u < steps; ++u) {
+                if (c >= 0 && (steps == 1 || (t < a.K ? t : 0) == u)) acc[c] += a.weights[rg * per + t];
+                __syncthreads();
+            }
         }
     }
     const int last = n_candidates(len0 - 1, a.W), able = max(0, last - a.sink);
@@ -180,7 +196,7 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
     __shared__ float s_tot[EPT * kEvictBlock];
     __shared__ int s_hist[kSteps];
     __shared__ uint32_t s_lo[NW], s_hi[NW], s_list[kWave];
-    __shared__ int s_step, s_below, s_in, s_ties[NW], s_gone[NW];
+    __shared__ int s_step, s_below, s_in, s_ties[NW], s_gone[NW], s_odd[2][NW];
     const int b = blockIdx.x, tid = threadIdx.x, w = wave_id(), lane = tid % kWave;
     const int nC = a.L / kChunk, nr = (nC + kEvictBlock - 1) / kEvictBlock, first = w * kWave * nr + lane;
     const float* acc_in = a.acc + (size_t)b * nC;
@@ -197,26 +213,44 @@ __global__ __launch_bounds__(kEvictBlock) void k_evict(EvictArgs a) {
         page[r] = c < nC ? table_in[c] : -1;
     }
     if (a.weights) {
-        // row after row (g, n), so that a total is one sum in one order; a row names a chunk once
+        // row after row (g, n), so that a total is one sum in one order
         const int per = a.K + (a.W + 62) / kChunk + 1, total = a.Hkv * a.N * per;
         for (int e0 = 0; e0 < total; e0 += kEvictBlock) {
             const int e = e0 + tid, r = e / per, t = e % per;
             int c = -1;
             float x = 0.f;
+            bool odd = false;
             if (e < total) {
                 const int pos = len - a.N + r % a.N, ncand = n_candidates(pos, a.W);
                 const size_t rg = (size_t)b * a.Hkv * a.N + r;
+                const int32_t* row = a.idx + rg * a.K;
                 x = a.weights[rg * per + t];
                 if (t < a.K) {
-                    if (idx_entry_valid(a.idx + rg * a.K, t, ncand)) c = a.idx[rg * a.K + t];
+                    if (idx_entry_valid(row, t, ncand)) c = row[t];
+                    odd = out_of_order(row, t);
                 } else if (ncand + t - a.K <= pos / kChunk) {
                     c = ncand + t - a.K;
                 }
             }
-            const int r1 = min(total - 1, e0 + kEvictBlock - 1) / per;
-            for (int row = e0 / per; row <= r1; ++row) {
-                __syncthreads();
-                if (c >= 0 && r == row) s_tot[c] += x;
+            const int r0 = e0 / per, r1 = min(total - 1, e0 + kEvictBlock - 1) / per;
+            int* odds = s_odd[(e0 / kEvictBlock) & 1];  // (the last round's may still be being read)
+            odd = __ballot(odd) != 0;
+            if (lane == 0) odds[w] = odd;
+            __syncthreads();
+            odd = false;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) odd |= odds[i] != 0;
+            if (!odd) {
+                for (int row = r0; row <= r1; ++row) {
+                    if (c >= 0 && r == row) s_tot[c] += x;
+                    if (row < r1) __syncthreads();
+                }
+            } else {
+                for (int row = r0; row <= r1; ++row)
+                    for (int u = 0; u < a.K; ++u) {
+                        if (c >= 0 && r == row && (t < a.K ? t : 0) == u) s_tot[c] += x;
+                        __syncthreads();
+                    }
             }
         }
     }

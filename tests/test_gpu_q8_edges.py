@@ -1,0 +1,53 @@
+"""The 8-bit cache on the GPU: selections, values and arguments at the edge of what the entry points take,
+against the float64 oracle (tests/q8_oracle.py) with the tolerances of tests/test_gpu_q8.py."""
+import numpy as np
+import pytest
+import torch
+
+from tests import q8_oracle as Q
+from tests import test_gpu_q8 as T
+
+pytestmark = pytest.mark.gpu
+
+
+def same(got, ref):
+    for x, y in zip(got, ref):
+        assert np.array_equal(x.cpu().numpy().astype(np.float64), np.asarray(y, np.float64))
+
+
+@pytest.mark.parametrize("L", [64 * 40, 64 * 25001])  # totals in LDS, and too many for it
+def test_evict_adds_every_slot_of_a_chunk_named_twice(L):
+    """Given selections that come back to a chunk: its slots are added one after the other, wherever the rows fall."""
+    hils = T.hils_()
+    p = hils.Params(B=1, Hq=4, Hkv=4, N=16, L=L, d=64, topk=64, window=64)  # 64 rows of 66 weights: over four rounds
+    acc, table, wt, idx = T.evict_inputs(p, 3, None, 3)
+    r = np.random.default_rng(5)
+    top = min(30, Q.n_candidates(L - 16, 64))
+    idx[:] = r.integers(-2, top, idx.shape)  # few chunks, many slots
+    idx[0, 0, 0] = -1
+    idx[0, 0, 0, :5] = 5, -1, 5, 2, 5
+    idx[0, 1, 3, :6] = 1 << 30, 7, 2, 3, 7, -5
+    idx[0, 3, 15] = 9
+    rows = idx.reshape(-1, 64)
+    twice = sum(len(v) > len(set(v)) for v in ([c for t, c in enumerate(x) if c >= 0 and (t == 0 or c > x[t - 1])] for x in rows))
+    assert twice > 50
+    budget = Q.n_candidates(L - 1, 64) - 12
+    ref = Q.evict(p, acc, table, None, budget, 2, L // 64, wt, idx)
+    same(hils.hils_cache_evict(p, T.dev(acc), T.dev(table), budget=budget, sink=2, weights=T.dev(wt), idx=T.dev(idx)), ref)
+
+
+def test_a_given_selection_that_repeats_a_chunk_is_evicted_by_all_its_weight():
+    """Decode attends a chunk named twice twice; eviction counts what decode reports, all of it."""
+    hils = T.hils_()
+    p = hils.Params(B=2, Hq=8, Hkv=2, N=2, L=1024, d=64, topk=5, window=128, scale=0.125, flags=hils.HILS_FLAG_GIVEN_IDX)
+    t = T.world(p, 6)
+    given = np.tile(np.int32([5, -1, 5, 2, 5]), (2, 2, 2, 1))
+    got = T.run_decode(p, t, idx=T.dev(given))
+    T.check_decode(p, got, Q.decode(p, t["q"], t["k"], t["v"], t["scale"], t["lmk"], t["table"], given=given))
+    acc = torch.zeros((2, 16), device="cuda")
+    res = hils.hils_cache_evict(p, acc, T.dev(t["table"]), budget=100, weights=got[3], idx=got[2])
+    w = T.host(got[3])
+    assert (w[..., [0, 2, 4]] > 0).all() and (w[..., [1, 3]] == 0).all()
+    # (sums of 4 rows of float32 weights of at most 4: roundings of 2^-24 of 16)
+    assert np.abs(T.host(res[0])[:, 5] - w[..., [0, 2, 4]].sum((1, 2, 3))).max() <= 12 * 16 * 2.0 ** -24
+    assert np.abs(T.host(res[0]).sum(1) - w.sum((1, 2, 3))).max() <= 64 * 16 * 2.0 ** -24
