@@ -645,16 +645,17 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
             const float z = l == 0.f ? -INFINITY : phase ? sh : mx + __builtin_amdgcn_logf(l);
             const float Mn = fmaxf(M, z), base = Mn == -INFINITY ? 0.f : Mn;
             const float corr = fexp2(M - base), zin = fexp2(z - base);
-            const float f = l == 0.f ? 0.f : vs * (phase ? zin / l : fexp2(mx - base));
+            const float f = zin == 0.f ? 0.f : vs * (phase ? zin / l : fexp2(mx - base));
             Z = Z * corr + zin;
             M = Mn;
             if (n16 < G && lg == 0) sm.part[slot][n16] = z;
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] *= corr;
-            // (a part that weighs nothing for any head adds nothing, whatever its values)
-            if (__ballot(f != 0.f) != 0) {
+            // (a part masked for every head, z = -inf, adds nothing, whatever its keys and values; one
+            // masked for some heads adds nothing to them whatever its keys)
+            if (__ballot(n16 < G && f != 0.f) != 0) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) st[i] *= f;
+                for (int i = 0; i < 16; ++i) st[i] = f == 0.f ? 0.f : st[i] * f;
                 // (P's float32 in three bf16 terms; two, 2^-17 of it, show where values cancel: 131K x 32
                 // 69.0 us and now 70.0, 8 x 64K with 4 new tokens 33.9 and 34.9)
                 bf16x8 p0[3], p1[3];

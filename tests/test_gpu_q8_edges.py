@@ -51,3 +51,27 @@ def test_a_given_selection_that_repeats_a_chunk_is_evicted_by_all_its_weight():
     # (sums of 4 rows of float32 weights of at most 4: roundings of 2^-24 of 16)
     assert np.abs(T.host(res[0])[:, 5] - w[..., [0, 2, 4]].sum((1, 2, 3))).max() <= 12 * 16 * 2.0 ** -24
     assert np.abs(T.host(res[0]).sum(1) - w.sum((1, 2, 3))).max() <= 64 * 16 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,B", [(64, 2), (128, 70)])  # shared rows, a workgroup each
+def test_decode_nan_in_masked_chunks(d, B, dtype):
+    """A chunk with a bias of -inf that is chosen because candidates are few weighs nothing, whatever it holds:
+    masked for all heads with NaN keys and values, masked for one head with NaN keys."""
+    hils = T.hils_()
+    p = hils.Params(B=B, Hq=8, Hkv=2, N=1, L=512, d=d, topk=8, window=64, scale=0.125, dtype=dtype)
+    t = T.world(p, 17)
+    for b in range(B):
+        t["bias"][t["table"][b, 1]] = -np.inf
+        t["bias"][t["table"][b, 3], 2] = -np.inf  # head 2, of group 0
+    clean = T.run_decode(p, t, bias=True)
+    T.check_decode(p, clean, Q.decode(p, t["q"], t["k"], t["v"], t["scale"], t["lmk"], t["table"], bias=t["bias"]))
+    for b in range(B):
+        t["k"][t["table"][b, 1], :, 9], t["v"][t["table"][b, 1], :, :, 9] = 0x7f, 0xff
+        t["k"][t["table"][b, 3], 0, 5] = 0x7f
+    got = T.run_decode(p, t, bias=True)
+    keep = [0, 1, 3]  # the heads of group 0 that attend chunk 3
+    others = [2, 4, 5, 6, 7]
+    assert torch.equal(got[0][:, others], clean[0][:, others])
+    assert all(torch.equal(x, y) for x, y in zip(got[1:], clean[1:]))
+    assert torch.isnan(got[0][:, keep]).all()
