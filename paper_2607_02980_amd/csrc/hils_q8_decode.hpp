@@ -284,7 +284,7 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
             float m = -INFINITY;
 #pragma unroll
             for (int h = 0; h < G; ++h) m = fmaxf(m, c * ss.score[q][h][tid] + bias[h]);
-            ss.sig[q][tid] = m;
+            ss.sig[q][tid] = m + 0.f;  // (-0 as 0: equal scores rank by index)
         }
     }
     __syncthreads();

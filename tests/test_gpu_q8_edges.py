@@ -75,3 +75,19 @@ def test_decode_nan_in_masked_chunks(d, B, dtype):
     assert torch.equal(got[0][:, others], clean[0][:, others])
     assert all(torch.equal(x, y) for x, y in zip(got[1:], clean[1:]))
     assert torch.isnan(got[0][:, keep]).all()
+
+
+@pytest.mark.parametrize("n", [1, 3])
+@pytest.mark.parametrize("shared", [False, True])
+def test_decode_zero_scores_of_either_sign_tie(n, shared):
+    """Scores of 0 and -0 (products of -0 with biases of either sign) are equal: the lowest chunks are chosen."""
+    hils = T.hils_()
+    p = hils.Params(B=2, Hq=8, Hkv=2, Hl=2 if shared else 8, N=n, L=64 * 300, d=64, topk=9, window=64, scale=-0.125)
+    t = T.world(p, 23)
+    t["lmk"][:] = 0
+    t["bias"][:] = -0.0
+    t["bias"][t["table"][:, 1::2]] = 0.0
+    ref = Q.decode(p, t["q"], t["k"], t["v"], t["scale"], t["lmk"], t["table"], bias=t["bias"])
+    got = T.run_decode(p, t, bias=True)
+    assert got[2][0, 0, 0].tolist() == list(range(9))
+    T.check_decode(p, got, ref)
