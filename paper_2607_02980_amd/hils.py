@@ -367,6 +367,13 @@ def _gpu(t, name):
     return t.get_device()
 
 
+def _pages(t, name):
+    """Pages of a pool."""
+    if not isinstance(t, torch.Tensor) or t.dim() == 0:
+        raise ValueError(f"{name} must be a GPU tensor")
+    return t.shape[0]
+
+
 def _run(fn, dev, *args):
     """The C call on device dev (made current for it) and that device's current stream."""
     if dev == torch.cuda.current_device():
@@ -388,7 +395,7 @@ def hils_q8_append(p: Params, k_new, v_new, k_pages, v_pages, kv_scale, block_ta
     [B, Hkv, N, d] go to its last newlens[b] positions (seqlens counts them).  Changes k_pages,
     v_pages and kv_scale in place and returns them."""
     dev, dt, B, H, d, S = _gpu(k_new, "k_new"), p.torch_dtype, p.B, p.Hkv, p.d, p.chunk
-    new, n = (B, H, p.N, d), k_pages.shape[0]
+    new, n = (B, H, p.N, d), _pages(k_pages, "k_pages")
     _run(LIB.hils_q8_append, dev, ctypes.byref(p.c()), _address(k_new, "k_new", new, dt, dev),
          _address(v_new, "v_new", new, dt, dev), _address(k_pages, "k_pages", (n, H, S, d), _F8, dev),
          _address(v_pages, "v_pages", (n, H, d, S), _F8, dev), _address(kv_scale, "kv_scale", (n, H, 2), _F32, dev),
@@ -404,7 +411,7 @@ def hils_q8_landmark_fwd(p: Params, lq, k_pages, kv_scale, block_table, lmk_page
     the stored keys: lq [B, Hl, (N + S - 1) // S, d] (one query per completed chunk) or [Hl, d] under
     HILS_FLAG_SHARED_LMK_QUERY.  Changes lmk_pages and bias_pages in place and returns them."""
     dev, B, H, Hl, d, S = _gpu(lq, "lq"), p.B, p.Hkv, p.Hl or p.Hq, p.d, p.chunk
-    n, lqs = k_pages.shape[0], (Hl, d) if p.flags & HILS_FLAG_SHARED_LMK_QUERY else (B, Hl, (p.N + S - 1) // S, d)
+    n, lqs = _pages(k_pages, "k_pages"), (Hl, d) if p.flags & HILS_FLAG_SHARED_LMK_QUERY else (B, Hl, (p.N + S - 1) // S, d)
     _run(LIB.hils_q8_landmark_fwd, dev, ctypes.byref(p.c()), _address(lq, "lq", lqs, p.torch_dtype, dev),
          _address(k_pages, "k_pages", (n, H, S, d), _F8, dev), _address(kv_scale, "kv_scale", (n, H, 2), _F32, dev),
          _address(block_table, "block_table", (B, p.L // S), _I32, dev), n,
@@ -420,7 +427,7 @@ def hils_decode_q8_fwd(p: Params, q, k_pages, v_pages, kv_scale, lmk_pages, bloc
     weights [B, Hkv, N, K + hils_window_pieces(W)] float32 (None without want_weights): each selected chunk's
     and window piece's attention weight, summed over the group's heads."""
     dev, dt, B, Hq, H, N, d, S = _gpu(q, "q"), p.torch_dtype, p.B, p.Hq, p.Hkv, p.N, p.d, p.chunk
-    n, Hl, qs, K = k_pages.shape[0], p.Hl or p.Hq, (B, Hq, N, d), p.topk
+    n, Hl, qs, K = _pages(k_pages, "k_pages"), p.Hl or p.Hq, (B, Hq, N, d), p.topk
     on = q.device
     if out is None:
         out = torch.empty(qs, dtype=dt, device=on)
@@ -435,7 +442,7 @@ def hils_decode_q8_fwd(p: Params, q, k_pages, v_pages, kv_scale, lmk_pages, bloc
         weights = torch.empty(wshape, dtype=_F32, device=on)
     if workspace is None:
         workspace = torch.empty(max(1, hils_workspace_size(p, HILS_OP_DECODE_Q8)), dtype=torch.uint8, device=on)
-    nbytes = workspace.numel()  # the library says if that is too little
+    nbytes = workspace.numel() if isinstance(workspace, torch.Tensor) else 0  # the library says if that is too little
     _run(LIB.hils_decode_q8_fwd, dev, ctypes.byref(p.c()), _address(q, "q", qs, dt, dev),
          _address(k_pages, "k_pages", (n, H, S, d), _F8, dev), _address(v_pages, "v_pages", (n, H, d, S), _F8, dev),
          _address(kv_scale, "kv_scale", (n, H, 2), _F32, dev), _address(lmk_pages, "lmk_pages", (n, Hl, d), _F8, dev),
@@ -461,9 +468,9 @@ def hils_cache_evict(p: Params, acc, block_table, seqlens=None, budget=0, sink=0
     dev, B, nc = _gpu(acc, "acc"), p.B, p.L // p.chunk
     most, on = nc if max_evict is None else max_evict, acc.device
     if acc_out is None:
-        acc_out = torch.empty_like(acc)
+        acc_out = torch.empty((B, nc), dtype=_F32, device=on)
     if table_out is None:
-        table_out = torch.empty_like(block_table)
+        table_out = torch.empty((B, nc), dtype=_I32, device=on)
     if seqlens_out is None:
         seqlens_out = torch.empty(B, dtype=_I32, device=on)
     if freed is None:
