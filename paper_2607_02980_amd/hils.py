@@ -14,6 +14,7 @@ if ``libhils.so`` is missing or fails to load, importing this module raises.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from dataclasses import dataclass
 
@@ -374,6 +375,14 @@ def _pages(t, name):
     return t.shape[0]
 
 
+def _int(x, name):
+    """A whole number that the C call takes as an int (ctypes would drop its higher bits)."""
+    x = operator.index(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name}={x} does not fit in 32 bits")
+    return x
+
+
 def _run(fn, dev, *args):
     """The C call on device dev (made current for it) and that device's current stream."""
     if dev == torch.cuda.current_device():
@@ -465,8 +474,9 @@ def hils_cache_evict(p: Params, acc, block_table, seqlens=None, budget=0, sink=0
     freed[b, :nfreed[b]]."""
     if weights is not None and idx is None:
         raise ValueError("weights needs idx")
-    dev, B, nc = _gpu(acc, "acc"), p.B, p.L // p.chunk
-    most, on = nc if max_evict is None else max_evict, acc.device
+    budget, sink, nc = _int(budget, "budget"), _int(sink, "sink"), p.L // p.chunk
+    most = nc if max_evict is None else _int(max_evict, "max_evict")
+    dev, B, on = _gpu(acc, "acc"), p.B, acc.device
     if acc_out is None:
         acc_out = torch.empty((B, nc), dtype=_F32, device=on)
     if table_out is None:

@@ -39,3 +39,11 @@ def test_a_block_table_that_is_no_gpu_tensor(monkeypatch, bad):
     only(monkeypatch, "block_table")
     with pytest.raises(ValueError, match="block_table"):
         hils.hils_cache_evict(P, ACC, bad)
+
+
+@pytest.mark.parametrize("name", ["budget", "sink", "max_evict"])
+@pytest.mark.parametrize("value", [1 << 31, 1 << 32, (1 << 32) + 5, -(1 << 31) - 1])
+def test_numbers_past_32_bits_are_refused(name, value):
+    """(ctypes drops the higher bits: a budget of 2^32 would be one of 0, and cut every sequence.)"""
+    with pytest.raises(ValueError, match=f"{name}=.*32 bits"):
+        hils.hils_cache_evict(P, ACC, TABLE, **{name: value})
