@@ -54,7 +54,9 @@ def append(p, k_new, v_new, k, v, scale, table, seqlens=None, newlens=None):
             lo, hi = max(start, c * S), min(length, c * S + S)
             if hi <= lo:
                 continue
-            page = min(max(int(table[b, c]), 0), len(k) - 1)
+            page = int(table[b, c])
+            if not 0 <= page < len(k):
+                continue  # no page: dropped
             r0, r1 = lo - c * S, hi - c * S
             for which, new, pool in ((0, k_new, k), (1, v_new, v.transpose(0, 1, 3, 2))):
                 for g in range(p.Hkv):
@@ -78,7 +80,9 @@ def landmark(p, lq, k, scale, table, seqlens=None, newlens=None, shared=False):
         length, fresh = tokens(p, seqlens, newlens, b)
         first = (length - fresh) // S
         for j, c in enumerate(range(first, length // S)):
-            page = min(max(int(table[b, c]), 0), len(k) - 1)
+            page = int(table[b, c])
+            if not 0 <= page < len(k):
+                continue  # no page: dropped
             rows, biases = [], []
             for hl in range(Hl):
                 g = hl // (Hl // p.Hkv)

@@ -91,3 +91,37 @@ def test_decode_zero_scores_of_either_sign_tie(n, shared):
     got = T.run_decode(p, t, bias=True)
     assert got[2][0, 0, 0].tolist() == list(range(9))
     T.check_decode(p, got, ref)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_writes_of_chunks_without_a_page(dtype):
+    """One table for the kernels and the oracle: chunks whose entry is outside the pool are dropped."""
+    hils = T.hils_()
+    p = hils.Params(B=3, Hq=4, Hkv=2, N=200, L=256, d=64, topk=1, window=64, dtype=dtype)
+    new, pools, scale, table = T.append_inputs(p, 22)
+    lens, counts = [256, 201, 64], [200, 200, 64]
+    for b, c, bad in ((0, 1, -1), (0, 3, len(pools[0])), (1, 0, -2 ** 31), (1, 3, 2 ** 31 - 1)):
+        table[b, c] = bad
+    ref = Q.append(p, *new, *pools, scale, table, lens, counts)
+    got = T.run_append(p, new, pools, scale, table, lens, counts)
+    assert np.array_equal(got[2], ref[2]) and T.same_codes(got[0], ref[0]) and T.same_codes(got[1], ref[1])
+    n = len(pools[0])
+    lq = rounded_lq(p, 3)
+    lm, bias = T.f8(np.full((n, 4, 64), 0x5a, np.uint8)), torch.full((n, 4), 7.0, device="cuda")
+    i32 = [T.dev(np.int32(x)) for x in (lens, counts)]
+    hils.hils_q8_landmark_fwd(p, T.dev(lq, p.torch_dtype), T.f8(ref[0]), T.dev(ref[2]), T.dev(table), lm, bias, *i32)
+    rows = Q.landmark(p, lq, ref[0], ref[2], table, lens, counts)
+    assert sorted(rows) == sorted(table[b, c] for b, c in ((0, 0), (0, 2), (1, 1), (1, 2), (2, 0)))
+    for page in range(n):
+        if page in rows:
+            off = np.abs(Q.VALUE[T.codes(lm)[page]] - rows[page][0])
+            assert (off <= np.maximum(2.0 ** -4 * np.abs(rows[page][0]), 2.0 ** -10) + 1e-4 * 448).all()
+            assert np.abs(bias[page].cpu().numpy() - rows[page][1]).max() <= 1e-4
+        else:
+            assert (T.codes(lm)[page] == 0x5a).all() and (bias[page] == 7).all()
+
+
+def rounded_lq(p, seed):
+    """Landmark queries of a call's completed chunks, small enough for logits up to 10."""
+    x = np.random.default_rng(seed).standard_normal((p.B, p.Hl or p.Hq, (p.N + 63) // 64, p.d)).astype(np.float32)
+    return T.rounded(x / 64, p.dtype)
