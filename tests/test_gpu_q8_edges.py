@@ -125,3 +125,62 @@ def rounded_lq(p, seed):
     """Landmark queries of a call's completed chunks, small enough for logits up to 10."""
     x = np.random.default_rng(seed).standard_normal((p.B, p.Hl or p.Hq, (p.N + 63) // 64, p.d)).astype(np.float32)
     return T.rounded(x / 64, p.dtype)
+
+
+TOTALS = {
+    "subnormal": lambda r, n: r.integers(0, 5, n) * 1e-45,
+    "one_subnormal_apart": lambda r, n: 1.0 + r.integers(0, 2, n) * 2.0 ** -23,
+    "whole_range": lambda r, n: r.choice([-3e38, 3e38, 0.0, -0.0, 1e-40, -1e-40, 5.0], n),
+    "infinities": lambda r, n: r.choice([np.inf, -np.inf, 1.0, 2.0, np.nan], n),
+    "two_scales": lambda r, n: np.where(r.random(n) < 0.5, r.random(n) * 1e-6, 1e6 * r.random(n)),
+    "negative": lambda r, n: -np.exp(r.standard_normal(n) * 10),
+    "mostly_equal": lambda r, n: np.where(r.random(n) < 0.99, 7.0, r.standard_normal(n)),
+}
+
+
+@pytest.mark.parametrize("name", TOTALS)
+@pytest.mark.parametrize("nC", [70, 1025, 8193, 20481])
+def test_evict_totals_of_every_kind(nC, name):
+    """Any drop count, over totals whose range, spacing or ties defeat equal steps."""
+    hils = T.hils_()
+    p = hils.Params(B=3, Hq=1, Hkv=1, N=1, L=64 * nC, d=64, topk=1, window=64)
+    r = np.random.default_rng(nC)
+    acc = np.stack([TOTALS[name](r, nC) for _ in range(3)]).astype(np.float32)
+    table = np.stack([r.permutation(nC) for _ in range(3)]).astype(np.int32)
+    lens = [64 * nC, 64 * nC - 900, 64 * (nC // 2)]
+    for budget in (0, nC // 3, nC - 3):
+        got = hils.hils_cache_evict(p, T.dev(acc), T.dev(table), T.dev(np.int32(lens)), budget=budget, sink=2)
+        got = [x.cpu().numpy() for x in got]
+        for b, length in enumerate(lens):
+            able = np.arange(2, Q.n_candidates(length - 1, 64))
+            count = min(max(0, len(able) + 2 - budget), len(able))
+            order = np.lexsort((able, np.nan_to_num(acc[b, able], posinf=np.inf, neginf=-np.inf), np.isnan(acc[b, able])))
+            gone = np.sort(able[order[:count]])
+            kept = np.delete(np.arange(nC), gone)
+            assert got[4][b] == count and got[2][b] == length - 64 * count
+            assert np.array_equal(got[3][b], np.r_[table[b, gone], np.full(nC - count, -1)])
+            assert np.array_equal(got[1][b], np.r_[table[b, kept], np.full(count, -1)])
+            assert np.array_equal(got[0][b], np.r_[acc[b, kept], np.zeros(count, np.float32)], equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_streams_at_once(dtype):
+    """Calls of two streams over the same pages, each with a workspace of its own: the bits of calls by themselves."""
+    hils = T.hils_()
+    ps = [hils.Params(B=b, Hq=16, Hkv=4, N=n, L=4096, d=128, topk=16, window=512, scale=0.125, dtype=dtype) for b, n in ((3, 1), (2, 4))]
+    t = T.world(ps[0], 51)
+    pools = T.f8(t["k"]), T.f8(t["v"]), T.dev(t["scale"]), T.f8(t["lmk"])
+    r = np.random.default_rng(1)
+    qs = [T.dev(r.standard_normal((p.B, 16, p.N, 128)).astype(np.float32), p.torch_dtype) for p in ps]
+    tables = [T.dev(t["table"][:p.B]) for p in ps]
+    wss = [torch.empty(hils.hils_workspace_size(p, hils.HILS_OP_DECODE_Q8), dtype=torch.uint8, device="cuda") for p in ps]
+    want = [hils.hils_decode_q8_fwd(p, q, *pools, tb, workspace=w) for p, q, tb, w in zip(ps, qs, tables, wss)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in ps], [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(hils.hils_decode_q8_fwd(ps[i], qs[i], *pools, tables[i], workspace=wss[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, y) for g in got[i] for x, y in zip(g, want[i]))
