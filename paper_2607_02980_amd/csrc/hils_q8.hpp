@@ -9,8 +9,9 @@
 //   lmk_pages [P, Hl, d]      e4m3 in units of the page's K scale: k'_c is a convex combination
 //                             of the chunk's keys, so it fits in their range
 //   bias_pages [P, Hl]        f32
-// e4m3 values are exact in bf16 (4 significant bits), so products run on the bf16 MFMA with
-// the other operand at full precision; the scales multiply float32 results.
+// e4m3 values are exact in bf16 and float16 (4 significant bits, 2^-9 to 448), so products run on
+// the 16-bit MFMAs with the other operand, queries or weights, as several terms of that type; the
+// scales multiply float32 results.
 #pragma once
 
 #include "hils_device.hpp"
@@ -55,6 +56,42 @@ __device__ __forceinline__ void split_bf16x8(const float* x, bf16x8 (&o)[S]) {
             o[s][t] = static_cast<__bf16>(r[t]);
             r[t] -= (float)o[s][t];
         }
+}
+
+// Softmax weights (0 <= w <= 1) as operands: 4096 w as the sum of two float16 values, to 2^-23 of it, a
+// float32's last bit, and to 2^-37 of 1 (below 2^-26 the terms are subnormal).  Two terms of bf16 hold
+// 2^-17 of w, which shows where a sum cancels; three hold it whole for half as many products again.
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+constexpr float kWeightUnit = 1.f / 4096;
+__device__ __forceinline__ f16x8 f16x8_of_e4m3(uint32_t lo, uint32_t hi) {
+    typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false);
+    const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
+    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false);
+    const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
+    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+struct WeightOperand {
+    f16x8 t[2];
+    __device__ __forceinline__ explicit WeightOperand(const float* w) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float x = w[i] * (1.f / kWeightUnit);
+            t[0][i] = static_cast<_Float16>(x);
+            t[1][i] = static_cast<_Float16>(x - (float)t[0][i]);
+        }
+    }
+};
+// The sum of two products x w of e4m3 values and weights, in units of kWeightUnit, the smaller terms first.
+__device__ __forceinline__ f32x4 mfma_weights(const f16x8& x0, const WeightOperand& w0, const f16x8& x1,
+                                              const WeightOperand& w1) {
+    f32x4 o = zero4();
+#pragma unroll
+    for (int t = 1; t >= 0; --t) {
+        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(x0, w0.t[t], o, 0, 0, 0);
+        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(x1, w1.t[t], o, 0, 0, 0);
+    }
+    return o;
 }
 
 // Eight consecutive elements of a caller's array, aligned as its elements are.

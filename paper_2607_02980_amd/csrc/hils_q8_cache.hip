@@ -212,21 +212,20 @@ __global__ __launch_bounds__(kBlock) void k_q8_append(Q8AppendArgs a, int most) 
 // Prop. 3.1 on the stored keys k_j = x_j ks: one wave per (sequence, completed chunk, KV head),
 // the group's GL landmark heads as MFMA columns: S^T = K Q'^T from K rows as they lie in the
 // page, the softmax over the lane groups, b' = log l - sum_j p_j s_j (s from its maximum), and
-// k' / ks = X^T P^T with X^T by transposing reads of the rows, as bf16, in the wave's LDS tile
-// and P in three bf16 terms, which hold its float32 (two, 2^-17 of it, show where a row's sum
-// cancels, and take 11.5 us of the 12.2 for 512 chunks of 32 heads).  Bound by memory:
-// 64 d + GL (d + 4) bytes per wave.  (Products with P on the vector unit, key by key from LDS: 512
+// k' / ks = X^T P^T with X^T by transposing reads of the rows, as float16, in the wave's LDS tile
+// and P in two float16 terms (512 chunks of 32 heads 12.0 us; in two bf16 terms, 2^-17 of it, 11.5,
+// in three 12.2).  Bound by memory: 64 d + GL (d + 4) bytes per wave.  (Products with P on the vector unit, key by key from LDS: 512
 // chunks of 32 heads 18 us, 24 chunks 12 us.)
 template <int D>
 struct LmkTile {
     static constexpr int ROW = D + 16;  // (transposing reads of padded rows meet two addresses per bank)
-    bf16 x[kChunk * ROW];
+    _Float16 x[kChunk * ROW];
 };
 template <typename T, int D, int GL>
 __global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int most) {
     constexpr int DJ = D / 64, DB = D / 16, ROW = LmkTile<D>::ROW;
     __shared__ __align__(16) LmkTile<D> tiles[kWaves];
-    bf16* tile = tiles[wave_id()].x;
+    _Float16* tile = tiles[wave_id()].x;
     const int lane = threadIdx.x % kWave, lg = lane / 16, n16 = lane % 16;
     const long unit = (long)blockIdx.x * kWaves + wave_id();
     const int g = (int)(unit % a.Hkv);
@@ -262,9 +261,9 @@ __global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int mo
 #pragma unroll
         for (int t = 0; t < DJ; ++t) {
             const bf16x8 k0 = bf16x8_of_e4m3(kx[kb][t].x, kx[kb][t].y), k1 = bf16x8_of_e4m3(kx[kb][t].z, kx[kb][t].w);
-            bf16* dst = tile + (kb * 16 + n16) * ROW + t * 64 + lg * 16;
-            *reinterpret_cast<bf16x8*>(dst) = k0;
-            *reinterpret_cast<bf16x8*>(dst + 8) = k1;
+            _Float16* dst = tile + (kb * 16 + n16) * ROW + t * 64 + lg * 16;
+            *reinterpret_cast<f16x8*>(dst) = f16x8_of_e4m3(kx[kb][t].x, kx[kb][t].y);
+            *reinterpret_cast<f16x8*>(dst + 8) = f16x8_of_e4m3(kx[kb][t].z, kx[kb][t].w);
 #pragma unroll
             for (int r = QRow<T, D>::S - 1; r >= 0; --r) {
                 st = mfma16x16x32(k0, q.x[2 * t][r], st);
@@ -290,9 +289,7 @@ __global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int mo
     ps = group4_sum(ps);
     const float inv = 1.f / l;
     if (n16 < GL && lg == 0) a.bias_pages[page * a.Hl + hl0 + n16] = logf(l) - ps * inv;
-    bf16x8 p0[3], p1[3];
-    split_bf16x8<3>(s, p0);
-    split_bf16x8<3>(s + 8, p1);
+    const WeightOperand p0(s), p1(s + 8);
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     // (lane: head n16, dims 16 db + 4 lg + i; a convex combination of codes: above 448 by the
@@ -300,13 +297,9 @@ __global__ __launch_bounds__(kBlock) void k_q8_landmark(Q8LandmarkArgs a, int mo
     f32x4 o[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-        const bf16x8 x0 = tr_operand_perm(tile, ROW, 0, db * 16, lane), x1 = tr_operand_perm(tile, ROW, 32, db * 16, lane);
-        o[db] = zero4();
-#pragma unroll
-        for (int t = 2; t >= 0; --t) {
-            o[db] = mfma16x16x32(x0, p0[t], o[db]);
-            o[db] = mfma16x16x32(x1, p1[t], o[db]);
-        }
+        const f16x8 x0 = __builtin_bit_cast(f16x8, tr_operand_perm(tile, ROW, 0, db * 16, lane));
+        const f16x8 x1 = __builtin_bit_cast(f16x8, tr_operand_perm(tile, ROW, 32, db * 16, lane));
+        o[db] = mfma_weights(x0, p0, x1, p1) * kWeightUnit;
     }
     if (n16 < GL) {
         uint8_t* dst = static_cast<uint8_t*>(a.lmk_pages) + (page * a.Hl + hl0 + n16) * D + lg * 4;

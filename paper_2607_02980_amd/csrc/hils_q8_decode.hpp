@@ -313,6 +313,10 @@ __global__ __launch_bounds__(kBlock) void k_q8_scan(Q8DecodeArgs qa, DecLayout l
     clear_counters();
 }
 
+// a b, 0 if b is 0, whatever a is.
+extern "C" __device__ float hils_mul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
+__device__ __forceinline__ float mul_0(float a, float b) { return hils_mul_legacy(a, b); }
+
 // Bytes of a dword of keys k0 .. k0 + 3 that lie below nk.
 __device__ __forceinline__ uint32_t keys_below(int k0, int nk) {
     const int n = nk - k0;
@@ -645,35 +649,28 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
             const float z = l == 0.f ? -INFINITY : phase ? sh : mx + __builtin_amdgcn_logf(l);
             const float Mn = fmaxf(M, z), base = Mn == -INFINITY ? 0.f : Mn;
             const float corr = fexp2(M - base), zin = fexp2(z - base);
-            const float f = zin == 0.f ? 0.f : vs * (phase ? zin / l : fexp2(mx - base));
+            const float f = zin == 0.f ? 0.f : vs * kWeightUnit * (phase ? zin / l : fexp2(mx - base));
             Z = Z * corr + zin;
             M = Mn;
             if (n16 < G && lg == 0) sm.part[slot][n16] = z;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) acc[db] *= corr;
             // (a part masked for every head, z = -inf, adds nothing, whatever its keys and values; one
             // masked for some heads adds nothing to them whatever its keys)
             if (__ballot(n16 < G && f != 0.f) != 0) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) st[i] = f == 0.f ? 0.f : st[i] * f;
-                // (P's float32 in three bf16 terms; two, 2^-17 of it, show where values cancel: 131K x 32
-                // 69.0 us and now 70.0, 8 x 64K with 4 new tokens 33.9 and 34.9)
-                bf16x8 p0[3], p1[3];
-                split_bf16x8<3>(st, p0);
-                split_bf16x8<3>(st + 8, p1);
+                const WeightOperand p0(st), p1(st + 8);
                 uint32_t keep[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) keep[i] = keys_below(lg * 16 + i * 4, nk);
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
-                    const bf16x8 v0 = bf16x8_of_e4m3(x.v[db].x & keep[0], x.v[db].y & keep[1]);
-                    const bf16x8 v1 = bf16x8_of_e4m3(x.v[db].z & keep[2], x.v[db].w & keep[3]);
+                    const f16x8 v0 = f16x8_of_e4m3(x.v[db].x & keep[0], x.v[db].y & keep[1]);
+                    const f16x8 v1 = f16x8_of_e4m3(x.v[db].z & keep[2], x.v[db].w & keep[3]);
+                    const f32x4 o = mfma_weights(v0, p0, v1, p1);
 #pragma unroll
-                    for (int s = 2; s >= 0; --s) {
-                        acc[db] = mfma16x16x32(v0, p0[s], acc[db]);
-                        acc[db] = mfma16x16x32(v1, p1[s], acc[db]);
-                    }
+                    for (int i = 0; i < 4; ++i) acc[db][i] = acc[db][i] * corr + mul_0(o[i], f);
                 }
+            } else {
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] *= corr;
             }
             if constexpr (kAhead) load_v(page, on);
         }

@@ -5,7 +5,7 @@ every weight is 1 / l or e / l (e = exp(-delta), l = 32 (1 + e)), and the codes 
 smaller at the first half, -384 at the second, cancel but for a remainder v of at most 0.01.  A weight held in
 16 significant bits shifts the sum by up to 2^-18 of 192 (7e-4), whatever is left of it.  In float32, in units
 of the scale:
-  * e is off by 2^-23 (the logits are exact): 192 * 2^-23 = 2.3e-5;
+  * e is off by 2^-23 (the logits are exact), and its operand by as much: 2 * 192 * 2^-23 = 4.6e-5;
   * 64 additions of partial sums of at most 2300, rounded at 2^-24 and divided by l > 62: 1.4e-4;
   * divisions by l and the fusion's factors: 2^-21 of v, nothing.
   So 2e-4, and half a step of the output: 2^-10 for e4m3 codes below 2^-6, 2^-8 of the value for bf16."""
