@@ -75,10 +75,15 @@ struct WeightOperand {
     f16x8 t[2];
     __device__ __forceinline__ explicit WeightOperand(const float* w) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float x = w[i] * (1.f / kWeightUnit);
-            t[0][i] = static_cast<_Float16>(x);
-            t[1][i] = static_cast<_Float16>(x - (float)t[0][i]);
+        for (int i = 0; i < 8; i += 2) {
+            typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+            const float x0 = w[i] * (1.f / kWeightUnit), x1 = w[i + 1] * (1.f / kWeightUnit);
+            f16x2 h = {static_cast<_Float16>(x0), static_cast<_Float16>(x1)};
+            asm("" : "+v"(h));  // (one conversion of both, not another of each for the difference)
+            t[0][i] = h[0];
+            t[0][i + 1] = h[1];
+            t[1][i] = static_cast<_Float16>(x0 - (float)h[0]);
+            t[1][i + 1] = static_cast<_Float16>(x1 - (float)h[1]);
         }
     }
 };

@@ -213,8 +213,8 @@ __global__ __launch_bounds__(kBlock) void k_q8_append(Q8AppendArgs a, int most) 
 // the group's GL landmark heads as MFMA columns: S^T = K Q'^T from K rows as they lie in the
 // page, the softmax over the lane groups, b' = log l - sum_j p_j s_j (s from its maximum), and
 // k' / ks = X^T P^T with X^T by transposing reads of the rows, as float16, in the wave's LDS tile
-// and P in two float16 terms (512 chunks of 32 heads 12.0 us; in two bf16 terms, 2^-17 of it, 11.5,
-// in three 12.2).  Bound by memory: 64 d + GL (d + 4) bytes per wave.  (Products with P on the vector unit, key by key from LDS: 512
+// and P in two float16 terms (512 chunks of 32 heads 12.3 us; in two bf16 terms, 2^-17 of it, 11.8,
+// in three 12.5).  Bound by memory: 64 d + GL (d + 4) bytes per wave.  (Products with P on the vector unit, key by key from LDS: 512
 // chunks of 32 heads 18 us, 24 chunks 12 us.)
 template <int D>
 struct LmkTile {
