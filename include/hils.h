@@ -344,7 +344,8 @@ int hils_q8_landmark_fwd(const hils_params* p, const void* lq, const void* k_pag
 /*
  * Decode forward over the 8-bit cache: hils_decode_paged_fwd (arguments, positions,
  * limits) on the values that the pages stand for; q, q_route and out are of `dtype`
- * (float32 or bf16), products and sums in float32.  bias_pages NULL: b' = 0.
+ * (float32 or bf16), products and sums in float32 (softmax weights to 2^-23 of
+ * themselves and 2^-37 of their part's largest).  bias_pages NULL: b' = 0.
  *   weights  [B, Hkv, N, K + P] f32, P = (window + 62) / 64 + 1, written unless NULL: the
  *            attention weight of each part of a row, summed over the group's heads: of
  *            the selected chunks (slot k as in idx; 0 for -1 entries) and of the window's
@@ -363,15 +364,18 @@ int hils_decode_q8_fwd(const hils_params* p, const void* q, const void* k_pages,
                        int32_t* idx, float* weights, void* workspace, size_t ws_bytes, void* stream);
 
 /*
- * Eviction from a paged cache (bf16, fp32 or 8-bit) by accumulated attention weight.
- * With weights and idx of a decode call (same p; NULL weights: nothing to add), every
- * chunk's total first takes what it received: acc[b, c] += sum over KV groups and new
- * queries, in that order.  Then a sequence with more than `budget` candidate chunks
- * (|C_i| of the last position, len - 1) loses the excess, at most max_evict: the chunks
- * with the least totals among sink .. |C_i| - 1, ties to the lower index (NaN totals
- * stay).  The rows of block_table and acc close up over them (their last entries become
+ * Eviction from a paged cache by accumulated attention weight.  With weights and idx
+ * of a hils_decode_q8_fwd call (same p; NULL weights: nothing to add), every chunk's
+ * total first takes what it received: acc[b, c] += sum over KV groups and new queries, in
+ * that order, a row's slots in theirs (those of a given selection count as they did
+ * there: a chunk named twice, twice).  Then a sequence with more than `budget` candidate
+ * chunks (|C_i| of the last position, len - 1) loses the excess, at most max_evict: the
+ * chunks with the least totals among sink .. |C_i| - 1, ties to the lower index (NaN
+ * totals stay).  The rows of block_table and acc close up over them (their last entries become
  * -1 and 0), the length falls by S per chunk, so that any decode entry point runs on
  * the result: positions serve the chunk partition only (rotations are the caller's).
+ * Pages are not touched and may be of any type; but no other decode entry point reports
+ * weights: over a bf16 or fp32 cache the totals are the caller's own.
  *   acc, acc_out         [B, L/S] f32       block_table, table_out [B, L/S] int32
  *   seqlens, seqlens_out [B] int32 (seqlens NULL: L; values are clamped into [0, L]; the
  *          weights belong to the decode call's positions, which start from at least N tokens)

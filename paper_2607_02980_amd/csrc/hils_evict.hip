@@ -8,9 +8,11 @@
 // its place inside its chunk.
 //
 // One workgroup per sequence.  What bounds it is latency: a step's work is a few kilobytes per
-// sequence and a dozen dependent phases.  Up to kMaxHeld chunks a sequence's totals stay in LDS
-// and its table in registers between the phases (k_evict); longer ones are read again from the L2 in
-// each (k_evict_long; 16384 chunks cut to 4096: 46 us, k_evict 14).
+// sequence, a dozen dependent phases, and before them a thread's loads, each waited for before the
+// next.  Up to kMaxHeld chunks a sequence's totals stay in LDS and its table in registers between the
+// phases (k_evict; above 8192 chunks 18 registers of it spill); longer ones are read again from the
+// L2 in each (k_evict_long).  Four sequences cut to 4096 chunks: of 16384 21 us, of 20480 22, of
+// 20481 63; eight of 8191 12.5.
 #include <climits>
 
 #include "hils_dispatch.hpp"

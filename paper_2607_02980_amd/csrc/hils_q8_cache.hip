@@ -73,7 +73,7 @@ __device__ __forceinline__ R load_stream(const T* p) {
 // registers, as they came, between the maximum and the conversion: of K 8 neighbouring dims per
 // lane and load; of V two dims of all rows (d = 64: of half the rows) per lane, so that a
 // dim-major row of 64 keys is 64 contiguous bytes of one lane.  (65536 tokens of 8 heads, d = 128:
-// 78 us, 5.2 TB/s where a copy of 1 GiB takes 4.8; K by two dims per lane and kept as floats 86.)
+// 75 to 80 us, 5.0 to 5.4 TB/s where a copy of 1 GiB takes 4.8; K by two dims per lane and kept as floats 86.)
 template <typename T, int D>
 __global__ __launch_bounds__(kBlock) void k_q8_append(Q8AppendArgs a, int most) {
     constexpr int LPR = D / 2, TH = kWave / LPR, ROWS = kChunk / TH;  // lanes per row, row groups, rows per lane

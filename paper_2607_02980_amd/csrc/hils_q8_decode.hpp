@@ -13,7 +13,7 @@
 // into O^T = V^T P^T without leaving its lane, and nothing of a part passes through LDS.
 // (Several new queries of a sequence are rows of their own: their windows meet in an XCD's L2,
 // which all rows of a KV group share with Hkv a multiple of 8, and a value behind a query never
-// meets its products.  One tile for the window of 4 queries, 8 sequences of 64K: parts and fusion 25 us, now 20.)
+// meets its products.  One tile for the window of 4 queries, 8 sequences of 64K: parts and fusion 25 us, now 21.)
 #pragma once
 
 #include "hils_decode.hpp"
@@ -464,11 +464,12 @@ __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, 
 // whose P is divided by its own sum, and z = m + log l for a piece of the window.  With a row to
 // itself a workgroup has many parts per wave, and the next one's K, landmark row and V are loaded as
 // soon as the current one is done with their registers (the loads are the same in every
-// iteration, so that the compiler counts the outstanding ones); with few there is nothing to load
-// ahead (1024 rows 79 us, without 83; a step of 32 rows the other way round, 19.9 and 18.3).
+// iteration, so that the compiler counts the outstanding ones; float32 with routing queries, d = 128,
+// spills 12 to 52 bytes a lane for it); with few there is nothing to load ahead (1024 rows 79 us,
+// without 83; a step of 32 rows the other way round, 19.9 and 18.3).
 // The waves' results meet in LDS, those of several workgroups in the last of them to arrive.
 // (A wave per part with its record in memory and the fusion in a launch of its own: 1024 rows of
-// 25 parts 95 + 10 us, now 76.)
+// 25 parts 95 + 10 us, now 79.)
 constexpr int kQ8RowWaves = 4;
 template <typename T>
 __device__ __forceinline__ void q8_store_out(const FwdArgs& a, size_t at, const f32x4& o) {
@@ -775,10 +776,10 @@ struct Q8DecRun {
                 HILS_LAUNCH("k_q8_scan", (k_q8_scan<T, D, G, NQ>), dim3((pairs + 7) / 8 * 8 * a.Hkv), dim3(kBlock), 0, s,
                             qa, ly, counters);
         };
-        // Above 128 rows a workgroup each; up to 128 four or more each, one per CU (256 rows: 1 workgroup
-        // per row 67.1 us a step, 2 70.9; 160 rows 30.3 and 31.3; 128 rows: 4 23.1, 2 24.9, 6 27.5; 64 rows:
-        // 4 22.9, 7 23.7).  (A given selection comes without the scan that clears the arrival
-        // counters: one workgroup per row.)
+        // Above 128 rows a workgroup each; up to 128 four or more each, one per CU but no more than one
+        // per four parts (256 rows: 1 workgroup per row 67.1 us a step, 2 70.9; 160 rows 30.3 and 31.3; 128
+        // rows: 4 23.1, 2 24.9, 6 27.5; 64 rows: 4 22.9, 7 23.7).  (A given selection comes without the scan
+        // that clears the arrival counters: one workgroup per row.)
         const int rows = R * a.Hkv;
         const int ns = a.given_idx || rows > kQ8SplitRows
                            ? 1
