@@ -88,3 +88,27 @@ def test_decode(d, B, dtype):
     assert np.array_equal(idx.cpu().numpy(), ref[2]) and np.abs(ref[0]).max() < 0.01 * 2.0 ** -7 * 1.01
     off = np.abs(T.host(out) - ref[0])
     assert (off <= TOL * 2.0 ** -7 + (2.0 ** -8 * np.abs(ref[0]) if dtype == "bf16" else 0)).all()
+
+
+@pytest.mark.parametrize("B", [2, 24])
+@pytest.mark.parametrize("d", [64, 128])
+def test_small_weights_beside_a_large_one(d, B):
+    """A key of weight near 1 whose values are 0, as a sequence's first token often has, and 63 of 2^-12 to 2^-17.
+
+    Relative to the outputs, which these alone make up: logits (exact) in units of log2, up to 17, rounded at 2^-23
+    twice: 2 * 17 * 0.7 * 2^-24 = 1.4e-6; exp 2^-23; operands 2^-23, or 2^-37 of a weight of 2^-17: 1e-6; a sum of 63
+    positive terms 63 * 2^-24 = 3.8e-6; factors and the division 2^-21: 7e-6 in all."""
+    hils = T.hils_()
+    p = hils.Params(B=B, Hq=8, Hkv=8, N=1, L=64, d=d, topk=1, window=64, scale=0.125, dtype="f32")
+    r = np.random.default_rng(d)
+    q = np.zeros((B, 8, 1, d), np.float32)
+    q[..., 0] = r.integers(154, 206, (B, 8, 1)) / 128  # logits 7 q[0] apart: 8.4 to 11.3
+    k, v = np.zeros((B, 8, 64, d), np.uint8), Q.encode(r.uniform(100, 448, (B, 8, d, 64)))
+    k[:, :, 0, 0], v[..., 0] = Q.encode(448), 0
+    scale = np.full((B, 8, 2), 2.0 ** -3, np.float32)
+    table, lmk = np.arange(B, dtype=np.int32)[:, None], np.zeros((B, 8, d), np.uint8)
+    ref = Q.decode(p, q, k, v, scale, lmk, table)
+    out = hils.hils_decode_q8_fwd(p, T.dev(q), T.f8(k), T.f8(v), T.dev(scale), T.f8(lmk), T.dev(table))[0]
+    off = np.abs(T.host(out) - ref[0]) / ref[0]
+    print("off", off.max(), flush=True)
+    assert off.max() <= 1e-5
