@@ -351,8 +351,9 @@ int hils_q8_landmark_fwd(const hils_params* p, const void* lq, const void* k_pag
  *            the selected chunks (slot k as in idx; 0 for -1 entries) and of the window's
  *            pieces (entry K + j: chunk |C_i| + j; 0 past the query's position).  A row's
  *            weights add up to Hq / Hkv.
- * A bias of -inf masks a chunk for its head, whatever NaN its keys hold (and its values,
- * if every head of the group masks it); it is still chosen where candidates are few.
+ * A bias of -inf masks a chunk for its head, whatever NaN its keys and landmark hold (and
+ * its values, if every head of the group masks it); it is still chosen where candidates
+ * are few.
  * Every position's own token must have been appended, the landmarks of every candidate
  * chunk written.  HILS_FLAG_HEAD_NORM_SELECT returns HILS_ERR_UNSUPPORTED.  The
  * workspace is hils_workspace_size(p, HILS_OP_DECODE_Q8); calls that may overlap (other

@@ -630,7 +630,9 @@ __global__ __launch_bounds__(kQ8RowWaves * kWave, 2) void k_q8_row(Q8DecodeArgs 
 #pragma unroll
             for (int i = 1; i < 4; ++i)
                 if (n16 % 4 == i) dg = d4[i];
-            const float sh = c1 * __shfl(dg, n16 + 16 * (n16 / 4), kWave) + (a.bias ? x.bias * kLog2e : 0.f);
+            // (a bias of -inf is a mask, though the landmark be NaN)
+            const float bias = a.bias ? x.bias : 0.f, score = c1 * __shfl(dg, n16 + 16 * (n16 / 4), kWave) + bias * kLog2e;
+            const float sh = bias == -INFINITY ? bias : score;
             if constexpr (kAhead) load_l(page, on);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {

@@ -184,3 +184,22 @@ def test_two_streams_at_once(dtype):
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(x, y) for g in got[i] for x, y in zip(g, want[i]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,B,n", [(64, 2, 1), (128, 70, 1), (64, 3, 4)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_decode_nan_landmarks_of_masked_chunks(d, B, n, dtype, shared):
+    """A chunk of NaN keys has a NaN landmark; a bias of -inf masks it all the same."""
+    hils = T.hils_()
+    p = hils.Params(B=B, Hq=8, Hkv=2, Hl=2 if shared else 8, N=n, L=512, d=d, topk=8, window=64, scale=0.125, dtype=dtype)
+    t = T.world(p, 18)
+    for b in range(B):
+        t["bias"][t["table"][b, 2]] = -np.inf
+        t["bias"][t["table"][b, 4], 0] = -np.inf
+    clean = T.run_decode(p, t, bias=True)
+    T.check_decode(p, clean, Q.decode(p, t["q"], t["k"], t["v"], t["scale"], t["lmk"], t["table"], bias=t["bias"]))
+    for b in range(B):
+        t["k"][t["table"][b, 2], :, 9], t["lmk"][t["table"][b, 2]] = 0x7f, 0x7f
+        t["lmk"][t["table"][b, 4], 0] = 0xff
+    assert all(torch.equal(x, y) for x, y in zip(T.run_decode(p, t, bias=True), clean))
