@@ -465,11 +465,11 @@ __device__ int q8_merge_block(const FwdArgs& a, const DecLayout& ly, size_t rg, 
 // itself a workgroup has many parts per wave, and the next one's K, landmark row and V are loaded as
 // soon as the current one is done with their registers (the loads are the same in every
 // iteration, so that the compiler counts the outstanding ones; float32 with routing queries, d = 128,
-// spills 12 to 52 bytes a lane for it); with few there is nothing to load ahead (1024 rows 79 us,
-// without 83; a step of 32 rows the other way round, 19.9 and 18.3).
+// spills 20 to 60 bytes a lane for it); with few there is nothing to load ahead (1024 rows 79 us when
+// measured, without 83; a step of 32 rows the other way round, 19.9 and 18.3).
 // The waves' results meet in LDS, those of several workgroups in the last of them to arrive.
 // (A wave per part with its record in memory and the fusion in a launch of its own: 1024 rows of
-// 25 parts 95 + 10 us, now 79.)
+// 25 parts 95 + 10 us, now 76.)
 constexpr int kQ8RowWaves = 4;
 template <typename T>
 __device__ __forceinline__ void q8_store_out(const FwdArgs& a, size_t at, const f32x4& o) {
