@@ -116,7 +116,12 @@ typedef enum {
     HILS_OP_DECODE_Q8 = 4,
     HILS_OP_Q8_APPEND = 5,
     HILS_OP_Q8_LANDMARK = 6,
-    HILS_OP_CACHE_EVICT = 7
+    HILS_OP_CACHE_EVICT = 7,
+    HILS_OP_PREFILL_PAGED = 8,
+    HILS_OP_CACHE_RESERVE = 9,
+    HILS_OP_CACHE_FORK = 10,
+    HILS_OP_CACHE_FREE = 11,
+    HILS_OP_CACHE_COMPACT = 12
 } hils_op;
 
 typedef struct {
@@ -230,6 +235,31 @@ int hils_decode_paged_fwd(const hils_params* p, const void* q, const void* k_pag
                           const void* lmk_pages, const float* bias_pages, const void* q_route,
                           const int32_t* block_table, int num_pages, const int32_t* seqlens, void* out, float* lse,
                           int32_t* idx, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Attention of a chunk of new tokens over a paged cache (a piece of a prompt, or all of it): the
+ * last newlens[b] tokens of sequence b are its new ones (newlens [B] int32, NULL: N each;
+ * clamped into [0, N] and to the length len = seqlens[b], which counts them and is clamped
+ * into [0, L]; NULL: L), and row n < newlens[b] of q is the query at position
+ * len - newlens[b] + n.  Same computation as hils_prefill_fwd at that position, over the
+ * pools and table of hils_decode_paged_fwd: every position's own k/v and the landmark rows of
+ * every complete chunk have been written, those of the new tokens' chunks among them.
+ *   q, q_route, out [B, Hq, N, d], lse [B, Hq, N], idx [B, Hkv, N, K]; rows at or past
+ *   newlens[b] are neither read nor written.
+ * A bias of -inf masks a chunk for its head, whatever NaN its landmark and keys hold (and its
+ * values, if every head of the group masks it); it is still chosen where candidates are few.
+ * Tokens at or past a sequence's length may hold anything, and what a later token holds does
+ * not reach an earlier row.  k_pages, v_pages and lmk_pages need their elements' alignment
+ * only, the workspace 16 bytes.  HILS_FLAG_GIVEN_IDX as for hils_prefill_fwd;
+ * HILS_FLAG_UNION_PACKING is ignored; HILS_FLAG_HEAD_NORM_SELECT returns HILS_ERR_UNSUPPORTED.
+ * The workspace is hils_workspace_size(p, HILS_OP_PREFILL_PAGED); its records are held to
+ * hils_prefill_record_cap as the prefill's are (more rows: several passes, the same bits).  Calls
+ * that may overlap need one each.  Deterministic.
+ */
+int hils_prefill_paged_fwd(const hils_params* p, const void* q, const void* k_pages, const void* v_pages,
+                           const void* lmk_pages, const float* bias_pages, const void* q_route,
+                           const int32_t* block_table, int num_pages, const int32_t* seqlens, const int32_t* newlens,
+                           void* out, float* lse, int32_t* idx, void* workspace, size_t ws_bytes, void* stream);
 
 /*
  * Backward of the prefill forward with the selection fixed to `idx`.
@@ -389,6 +419,77 @@ int hils_decode_q8_fwd(const hils_params* p, const void* q, const void* k_pages,
 int hils_cache_evict(const hils_params* p, const float* acc, const int32_t* block_table, const int32_t* seqlens,
                      const float* weights, const int32_t* idx, int budget, int sink, int max_evict, float* acc_out,
                      int32_t* table_out, int32_t* seqlens_out, int32_t* freed, int32_t* nfreed, void* stream);
+
+/*
+ * The pages of a cache as a resource.  page_refs [num_pages] int32 (device) says how many
+ * entries of the table name each page (and what other holders the caller counts); a page
+ * whose count is 0 or less is free.  Entries in use are those of chunks below
+ * ceil(seqlens[b] / S) (seqlens [B] int32, NULL: L; clamped into [0, L]); entries among
+ * them that name no page of the pool are left out of all counts.  Pages may be of any type
+ * and any of the layouts above; calls that copy pages take every pool that the table
+ * indexes, of every layer, as hils_pool (HOST array, num_pools <= 65536, NULL for none).
+ * Outputs may be the inputs themselves (in place) except where said, but not overlap them
+ * otherwise.  Free pages are taken lowest index first.  All use B, L and chunk of `p` and
+ * ignore the forward flags.  Deterministic.
+ */
+typedef struct {
+    void* data;        /* device: num_pages pages, one after the other */
+    size_t page_bytes;
+} hils_pool;
+
+/*
+ * Pages for new tokens, before they are written: seqlens counts the new tokens, newlens as for
+ * hils_prefill_paged_fwd.  Every chunk that begins with a new token is given a free page
+ * (whatever its entry held).  A page that holds older tokens and is about to get new ones is
+ * left to its other sequences and copied to a free page if its count is above 1; where all that
+ * count it write to it in this call, the first of them (lowest b) keeps it.  Given pages have
+ * count 1.  All or nothing: if the pool has fewer free pages than the call needs, table and
+ * counts stay as they were.
+ *   copied [B, 2]  the page copied from and to, -1 -1 where none was
+ *   counts [2]     pages needed, and free pages found, at most as many: the call took place if
+ *                  both are equal
+ * Uses N too.
+ */
+int hils_cache_reserve(const hils_params* p, const int32_t* block_table, const int32_t* page_refs, int num_pages,
+                       const int32_t* seqlens, const int32_t* newlens, const hils_pool* pools, int num_pools,
+                       int32_t* table_out, int32_t* refs_out, int32_t* copied, int32_t* counts, void* stream);
+
+/*
+ * Fork: row r of the result goes on from row parent[r] (parent [rows] int32, outside [0, B): an
+ * empty row): it names the same pages and has the same length.  Each entry in use of row
+ * b gains a count for every row that goes on from it and loses one for row b itself, so that
+ * rows nobody goes on from are freed; nothing is copied (hils_cache_reserve does that when a
+ * shared page is written to).  Serves copies of a prompt, beams that take each other's places,
+ * rows that leave or close up.
+ *   table_out [rows, L/S] (-1 past the row's chunks), seqlens_out [rows]: not the inputs'
+ *   buffers; refs_out [num_pages]
+ */
+int hils_cache_fork(const hils_params* p, const int32_t* parent, int rows, const int32_t* block_table,
+                    const int32_t* page_refs, int num_pages, const int32_t* seqlens, int32_t* table_out,
+                    int32_t* seqlens_out, int32_t* refs_out, void* stream);
+
+/*
+ * Free: sequence b keeps its first keep[b] tokens (keep [B] int32; 0 or less: none; its length or
+ * more: all).  Entries of the chunks past them become -1 and their pages lose a count.  pages
+ * [B, max_pages] with npages [B] (NULL: max_pages each; clamped into [0, max_pages]) lists
+ * further pages that lose one, as `freed` and `nfreed` of hils_cache_evict (NULL: none).
+ */
+int hils_cache_free(const hils_params* p, const int32_t* keep, const int32_t* pages, const int32_t* npages,
+                    int max_pages, const int32_t* block_table, const int32_t* page_refs, int num_pages,
+                    const int32_t* seqlens, int32_t* table_out, int32_t* seqlens_out, int32_t* refs_out, void* stream);
+
+/*
+ * Compact: with n pages in use, the i-th used page at or past n moves to the i-th free page before
+ * it, in every pool; counts move along and entries in use follow, so that the pool can be cut to
+ * n pages.
+ *   new_page [num_pages]  where each page is now (-1: free before the call), for holders of
+ *                         pages outside the table
+ *   moved    [num_pages]  the pages that moved, ascending, then -1
+ *   counts   [2]          n, and how many moved
+ */
+int hils_cache_compact(const hils_params* p, const int32_t* block_table, const int32_t* page_refs, int num_pages,
+                       const int32_t* seqlens, const hils_pool* pools, int num_pools, int32_t* table_out,
+                       int32_t* refs_out, int32_t* new_page, int32_t* moved, int32_t* counts, void* stream);
 
 /*
  * Prefill (bf16, chunk-major): the most bytes of per-slot records (the chunk

@@ -48,7 +48,7 @@ int ok() {
 
 int check_params(const hils_params* p, int op) {
     if (!p) return fail(HILS_ERR_INVALID, "params is NULL");
-    if (op < HILS_OP_PREFILL || op > HILS_OP_CACHE_EVICT)
+    if (op < HILS_OP_PREFILL || op > HILS_OP_CACHE_COMPACT)
         return fail(HILS_ERR_INVALID, "unknown op %d", op);
     if (p->B < 1 || p->Hq < 1 || p->Hkv < 1 || p->N < 1 || p->L < 1 || p->d < 1)
         return fail(HILS_ERR_INVALID, "B, Hq, Hkv, N, L and d must be >= 1 (B=%d Hq=%d Hkv=%d N=%d L=%d d=%d)",
@@ -70,10 +70,11 @@ int check_params(const hils_params* p, int op) {
     if (p->flags & ~(HILS_FLAG_GIVEN_IDX | HILS_FLAG_SHARED_LMK_QUERY | HILS_FLAG_HEAD_NORM_SELECT |
                      HILS_FLAG_UNION_PACKING))
         return fail(HILS_ERR_INVALID, "unknown flags 0x%x", p->flags);
-    const bool q8_cache = op == HILS_OP_Q8_APPEND || op == HILS_OP_Q8_LANDMARK || op == HILS_OP_CACHE_EVICT;
-    // (the eviction takes the decode call's parameters, whose forward flags mean nothing to it)
+    const bool pages = op >= HILS_OP_CACHE_RESERVE;
+    const bool q8_cache = op == HILS_OP_Q8_APPEND || op == HILS_OP_Q8_LANDMARK || op == HILS_OP_CACHE_EVICT || pages;
+    // (the cache's own operators take the decode call's parameters, whose forward flags mean nothing to them)
     const unsigned q8_flags = op == HILS_OP_Q8_LANDMARK ? HILS_FLAG_SHARED_LMK_QUERY
-                              : op == HILS_OP_CACHE_EVICT
+                              : op == HILS_OP_CACHE_EVICT || pages
                                   ? HILS_FLAG_GIVEN_IDX | HILS_FLAG_HEAD_NORM_SELECT | HILS_FLAG_UNION_PACKING
                                   : 0u;
     if (q8_cache && (p->flags & ~q8_flags))
@@ -107,6 +108,11 @@ int check_params(const hils_params* p, int op) {
         return fail(HILS_ERR_UNSUPPORTED, "window=%d: the decode kernels cover windows <= 4032", p->window);
     if (op == HILS_OP_DECODE_Q8 && (p->flags & HILS_FLAG_HEAD_NORM_SELECT))
         return fail(HILS_ERR_UNSUPPORTED, "HILS_FLAG_HEAD_NORM_SELECT: no kernel over the 8-bit cache");
+    if (op == HILS_OP_PREFILL_PAGED && (p->flags & HILS_FLAG_HEAD_NORM_SELECT))
+        return fail(HILS_ERR_UNSUPPORTED, "HILS_FLAG_HEAD_NORM_SELECT: no kernel for new tokens over a paged cache");
+    // (64 threads a row, or 64 entries, in one-dimensional grids)
+    if (op == HILS_OP_PREFILL_PAGED && 64. * p->B * p->Hkv * (p->N + 127.) > 4294967295.)
+        return fail(HILS_ERR_UNSUPPORTED, "B=%d Hkv=%d N=%d: more workgroups than one grid holds", p->B, p->Hkv, p->N);
     return HILS_OK;
 }
 
@@ -127,7 +133,13 @@ size_t ws_bytes_for(const hils_params* p, int op) {
         case HILS_OP_Q8_APPEND:
         case HILS_OP_Q8_LANDMARK:
         case HILS_OP_CACHE_EVICT:
+        case HILS_OP_CACHE_RESERVE:
+        case HILS_OP_CACHE_FORK:
+        case HILS_OP_CACHE_FREE:
+        case HILS_OP_CACHE_COMPACT:
             return 0;
+        case HILS_OP_PREFILL_PAGED:
+            return hils::prefill_paged_workspace_bytes(p->B, p->Hq, p->Hkv, p->N, p->L, p->d, p->topk);
         default:
             return hils::prefill_workspace_bytes(p->B, p->Hq, p->Hkv, p->N, p->L, p->d, p->topk,
                                                  p->dtype == HILS_BF16,
@@ -176,6 +188,22 @@ hils::FwdArgs fwd_args(const hils_params* p, const void* q, const void* k, const
     a.union_pack = (p->flags & HILS_FLAG_UNION_PACKING) ? 1 : 0;
     a.ws = ws; a.ws_bytes = ws_bytes;
     return a;
+}
+
+// Pools that a call copies pages of; the launchers take them as they are.
+static_assert(sizeof(hils_pool) == sizeof(hils::PoolArg) && offsetof(hils_pool, data) == offsetof(hils::PoolArg, data) &&
+                  offsetof(hils_pool, page_bytes) == offsetof(hils::PoolArg, page_bytes),
+              "a pool has one layout");
+int check_pools(const hils_pool* pools, int num_pools) {
+    if (num_pools < 0 || num_pools > 65536)
+        return fail(HILS_ERR_INVALID, "num_pools=%d: 0 to 65536 are possible", num_pools);
+    if (num_pools > 0 && !pools) return fail(HILS_ERR_INVALID, "num_pools=%d, so pools must be non-NULL", num_pools);
+    for (int i = 0; i < num_pools; ++i) {
+        if (!pools[i].data) return fail(HILS_ERR_INVALID, "pool %d is NULL", i);
+        if (pools[i].page_bytes == 0 || pools[i].page_bytes > ((size_t)1 << 32))
+            return fail(HILS_ERR_INVALID, "pool %d: a page has %zu bytes (1 to 2^32 are possible)", i, pools[i].page_bytes);
+    }
+    return HILS_OK;
 }
 
 }  // namespace
@@ -320,6 +348,26 @@ int hils_decode_paged_fwd(const hils_params* p, const void* q, const void* k_pag
     return hip_status(hils::launch_decode_fwd(a, (hipStream_t)stream), "hils_decode_paged_fwd launch");
 }
 
+int hils_prefill_paged_fwd(const hils_params* p, const void* q, const void* k_pages, const void* v_pages,
+                           const void* lmk_pages, const float* bias_pages, const void* q_route,
+                           const int32_t* block_table, int num_pages, const int32_t* seqlens, const int32_t* newlens,
+                           void* out, float* lse, int32_t* idx, void* workspace, size_t ws_bytes, void* stream) {
+    int rc = check_params(p, HILS_OP_PREFILL_PAGED);
+    if (rc) return rc;
+    REQUIRE(q); REQUIRE(k_pages); REQUIRE(v_pages); REQUIRE(lmk_pages); REQUIRE(block_table);
+    REQUIRE(out); REQUIRE(lse); REQUIRE(idx);
+    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    rc = check_ws(p, HILS_OP_PREFILL_PAGED, workspace, ws_bytes);
+    if (rc) return rc;
+    REQUIRE_ALIGNED(workspace, 16);
+    hils::PrefillPagedArgs a;
+    a.f = fwd_args(p, q, k_pages, v_pages, lmk_pages, bias_pages, q_route, seqlens, out, lse, idx, workspace, ws_bytes);
+    a.f.block_table = block_table;
+    a.f.num_pages = num_pages;
+    a.newlens = newlens;
+    return hip_status(hils::launch_prefill_paged(a, (hipStream_t)stream), "hils_prefill_paged_fwd launch");
+}
+
 int hils_bwd(const hils_params* p, const void* dout, const void* q, const void* k, const void* v, const void* lmk,
              const float* lmk_bias, const void* q_route, const void* out, const float* lse, const int32_t* idx,
              void* dq, void* dk, void* dv, void* dlmk, float* dlmk_bias, void* dq_route, void* workspace,
@@ -457,6 +505,66 @@ int hils_cache_evict(const hils_params* p, const float* acc, const int32_t* bloc
     a.B = p->B; a.Hkv = p->Hkv; a.N = p->N; a.L = p->L; a.K = p->topk; a.W = p->window;
     a.budget = budget; a.sink = sink; a.most = max_evict;
     return hip_status(hils::launch_evict(a, (hipStream_t)stream), "hils_cache_evict launch");
+}
+
+int hils_cache_reserve(const hils_params* p, const int32_t* block_table, const int32_t* page_refs, int num_pages,
+                       const int32_t* seqlens, const int32_t* newlens, const hils_pool* pools, int num_pools,
+                       int32_t* table_out, int32_t* refs_out, int32_t* copied, int32_t* counts, void* stream) {
+    int rc = check_params(p, HILS_OP_CACHE_RESERVE);
+    if (rc) return rc;
+    REQUIRE(block_table); REQUIRE(page_refs); REQUIRE(table_out); REQUIRE(refs_out); REQUIRE(copied); REQUIRE(counts);
+    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    if ((double)p->B * (p->L / 64) > 0x7fffffff)
+        return fail(HILS_ERR_UNSUPPORTED, "B=%d L=%d: more than 2^31 table entries", p->B, p->L);
+    rc = check_pools(pools, num_pools);
+    if (rc) return rc;
+    const hils::ReserveArgs a{block_table, page_refs, seqlens, newlens, table_out, refs_out, copied, counts,
+                              num_pages, p->B, p->N, p->L};
+    return hip_status(hils::launch_reserve(a, reinterpret_cast<const hils::PoolArg*>(pools), num_pools, (hipStream_t)stream), "hils_cache_reserve launch");
+}
+
+int hils_cache_fork(const hils_params* p, const int32_t* parent, int rows, const int32_t* block_table,
+                    const int32_t* page_refs, int num_pages, const int32_t* seqlens, int32_t* table_out,
+                    int32_t* seqlens_out, int32_t* refs_out, void* stream) {
+    int rc = check_params(p, HILS_OP_CACHE_FORK);
+    if (rc) return rc;
+    REQUIRE(parent); REQUIRE(block_table); REQUIRE(page_refs); REQUIRE(table_out); REQUIRE(seqlens_out); REQUIRE(refs_out);
+    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    if (rows < 1) return fail(HILS_ERR_INVALID, "rows must be >= 1 (got %d)", rows);
+    if (table_out == block_table || (seqlens && seqlens_out == seqlens))
+        return fail(HILS_ERR_INVALID, "a fork's rows and lengths cannot be written in place");
+    const hils::ForkArgs a{parent, block_table, page_refs, seqlens, table_out, seqlens_out, refs_out, num_pages, p->B,
+                           p->L, rows};
+    return hip_status(hils::launch_fork(a, (hipStream_t)stream), "hils_cache_fork launch");
+}
+
+int hils_cache_free(const hils_params* p, const int32_t* keep, const int32_t* pages, const int32_t* npages,
+                    int max_pages, const int32_t* block_table, const int32_t* page_refs, int num_pages,
+                    const int32_t* seqlens, int32_t* table_out, int32_t* seqlens_out, int32_t* refs_out, void* stream) {
+    int rc = check_params(p, HILS_OP_CACHE_FREE);
+    if (rc) return rc;
+    REQUIRE(keep); REQUIRE(block_table); REQUIRE(page_refs); REQUIRE(table_out); REQUIRE(seqlens_out); REQUIRE(refs_out);
+    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    if (max_pages < 0) return fail(HILS_ERR_INVALID, "max_pages must be >= 0 (got %d)", max_pages);
+    if (npages && !pages) return fail(HILS_ERR_INVALID, "npages is given, so pages must be non-NULL");
+    const hils::FreeArgs a{keep, max_pages ? pages : nullptr, npages, block_table, page_refs, seqlens, table_out,
+                           seqlens_out, refs_out, num_pages, p->B, p->L, max_pages};
+    return hip_status(hils::launch_free(a, (hipStream_t)stream), "hils_cache_free launch");
+}
+
+int hils_cache_compact(const hils_params* p, const int32_t* block_table, const int32_t* page_refs, int num_pages,
+                       const int32_t* seqlens, const hils_pool* pools, int num_pools, int32_t* table_out,
+                       int32_t* refs_out, int32_t* new_page, int32_t* moved, int32_t* counts, void* stream) {
+    int rc = check_params(p, HILS_OP_CACHE_COMPACT);
+    if (rc) return rc;
+    REQUIRE(block_table); REQUIRE(page_refs); REQUIRE(table_out); REQUIRE(refs_out); REQUIRE(new_page); REQUIRE(moved);
+    REQUIRE(counts);
+    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    rc = check_pools(pools, num_pools);
+    if (rc) return rc;
+    const hils::CompactArgs a{block_table, page_refs, seqlens, table_out, refs_out, new_page, moved, counts, num_pages,
+                              p->B, p->L};
+    return hip_status(hils::launch_compact(a, reinterpret_cast<const hils::PoolArg*>(pools), num_pools, (hipStream_t)stream), "hils_cache_compact launch");
 }
 
 }  // extern "C"

@@ -102,6 +102,11 @@ struct Q8DecodeArgs {
     const float* kv_scale;
     float* weights;              // nullable: [B, Hkv, N, K + window pieces]
 };
+// Attention of a chunk of new tokens over a paged cache: f.k, f.v, f.lmk, f.bias are the pools.
+struct PrefillPagedArgs {
+    FwdArgs f;
+    const int32_t* newlens;      // nullable: N
+};
 // Eviction by accumulated weight; the outputs may be the inputs.
 struct EvictArgs {
     const float* acc;            // [B, L/S]
@@ -115,6 +120,56 @@ struct EvictArgs {
     int32_t* freed;              // [B, most], -1 past nfreed[b]
     int32_t* nfreed;
     int B, Hkv, N, L, K, W, budget, sink, most;
+};
+// The pages of a cache as a resource (hils_pages.hip); P pages, table rows of L/S entries.  But for
+// a fork's rows and lengths the outputs may be the inputs.
+struct PoolArg {
+    void* data;                  // P pages of page_bytes each
+    size_t page_bytes;
+};
+struct ReserveArgs {
+    const int32_t* table;
+    const int32_t* refs;         // [P]
+    const int32_t* seqlens;      // nullable: L
+    const int32_t* newlens;      // nullable: N
+    int32_t* table_out;
+    int32_t* refs_out;
+    int32_t* copied;             // [B, 2] page copied from and to, -1: none
+    int32_t* counts;             // pages needed, pages found
+    int P, B, N, L;
+};
+struct ForkArgs {
+    const int32_t* parent;       // [rows]
+    const int32_t* table;
+    const int32_t* refs;
+    const int32_t* seqlens;
+    int32_t* table_out;          // [rows, L/S]
+    int32_t* seqlens_out;        // [rows]
+    int32_t* refs_out;
+    int P, B, L, rows;
+};
+struct FreeArgs {
+    const int32_t* keep;         // [B]
+    const int32_t* pages;        // nullable: [B, most] more pages to give up
+    const int32_t* npages;       // nullable: most
+    const int32_t* table;
+    const int32_t* refs;
+    const int32_t* seqlens;
+    int32_t* table_out;
+    int32_t* seqlens_out;
+    int32_t* refs_out;
+    int P, B, L, most;
+};
+struct CompactArgs {
+    const int32_t* table;
+    const int32_t* refs;
+    const int32_t* seqlens;
+    int32_t* table_out;
+    int32_t* refs_out;
+    int32_t* new_page;           // [P]
+    int32_t* moved;              // [P]
+    int32_t* counts;             // pages in use, pages moved
+    int P, B, L;
 };
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -211,6 +266,12 @@ hipError_t launch_q8_decode_bf16_d128(const Q8DecodeArgs& a, hipStream_t s);
 hipError_t launch_q8_decode_f32_d64(const Q8DecodeArgs& a, hipStream_t s);
 hipError_t launch_q8_decode_f32_d128(const Q8DecodeArgs& a, hipStream_t s);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
+size_t prefill_paged_workspace_bytes(int B, int Hq, int Hkv, int N, int L, int d, int K);
+hipError_t launch_prefill_paged(const PrefillPagedArgs& a, hipStream_t s);
+hipError_t launch_reserve(const ReserveArgs& a, const PoolArg* pools, int num_pools, hipStream_t s);
+hipError_t launch_fork(const ForkArgs& a, hipStream_t s);
+hipError_t launch_free(const FreeArgs& a, hipStream_t s);
+hipError_t launch_compact(const CompactArgs& a, const PoolArg* pools, int num_pools, hipStream_t s);
 hipError_t launch_bwd(const BwdArgs& a, hipStream_t s);
 hipError_t launch_bwd_f32(const BwdArgs& a, hipStream_t s);   // fp32 storage
 size_t bwd_f32_workspace_bytes(int B, int Hq, int Hkv, int N, int L, int d, int K, int W);

@@ -1,0 +1,409 @@
+// The pages of a cache as a resource: giving sequences pages to write to (copy on write), forking,
+// freeing and compacting.  Integers and copies only.
+//
+// State: a table row of pages per sequence, its length, and page_refs[page], how many table
+// entries name the page; a count of 0 (or less) marks a free page.  Every choice is by lowest index
+// first, so that results do not depend on the order in which threads run (the counts'
+// atomics are integer sums).
+#include <algorithm>
+
+#include "hils_device.hpp"
+#include "hils_internal.hpp"
+
+namespace hils {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPlan = 1024;             // threads of the one workgroup that plans
+constexpr int kPlanWaves = kPlan / kWave;
+constexpr int kPer = 16;                // pages of a thread per step of a scan over the pool
+constexpr size_t kSlice = 16 * 1024;    // bytes of a page that a workgroup copies at a time
+constexpr int kPools = 16;              // pools of one copying launch
+
+__device__ __forceinline__ int length_of(const int32_t* seqlens, int b, int L) {
+    return seqlens ? min(max(seqlens[b], 0), L) : L;
+}
+__device__ __forceinline__ int chunks_of(int tokens) { return (tokens + kChunk - 1) / kChunk; }
+
+// Exclusive prefix sum over the planning workgroup; `all` is the total.
+__device__ __forceinline__ int block_scan(int x, int* s_sum, int& all) {
+    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
+    int incl = x;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const int y = __shfl_up(incl, o, kWave);
+        if (lane >= o) incl += y;
+    }
+    __syncthreads();  // the last call's sums have been read
+    if (lane == kWave - 1) s_sum[w] = incl;
+    __syncthreads();
+    int before = incl - x;
+    all = 0;
+    for (int i = 0; i < kPlanWaves; ++i) {
+        before += i < w ? s_sum[i] : 0;
+        all += s_sum[i];
+    }
+    return before;
+}
+
+__global__ __launch_bounds__(kThreads) void k_cache_copy_state(const int32_t* table, int32_t* table_out, size_t nt,
+                                                              const int32_t* refs, int32_t* refs_out, size_t np) {
+    const size_t step = (size_t)gridDim.x * kThreads;
+    for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < nt; i += step) table_out[i] = table[i];
+    for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < np; i += step) refs_out[i] = refs[i];
+}
+
+// ---------------------------------------------------------------------------
+// pages for new tokens
+// ---------------------------------------------------------------------------
+// One workgroup.  First what every sequence needs: a copy of the page that its first new token
+// goes to, if others have it too, and a page for every chunk that begins; then, if the
+// pool holds as many, the free pages by index, the r-th for the sequence whose range of needs
+// r lies in.  copied[b] holds (source or state, first need) meanwhile.
+constexpr int kNone = -1, kNew = -2;  // no page to copy; (kNew: the entry names no page, a fresh one takes its place)
+
+__global__ __launch_bounds__(kPlan) void k_cache_reserve(ReserveArgs a) {
+    __shared__ int s_sum[kPlanWaves];
+    const int tid = threadIdx.x, C = a.L / kChunk;
+    auto seq = [&](int b, int& len, int& start) {
+        len = length_of(a.seqlens, b, a.L);
+        start = len - min(a.newlens ? min(max(a.newlens[b], 0), a.N) : a.N, len);
+    };
+    for (int b = tid; b < a.B; b += kPlan) {
+        int len, start, src = kNone;
+        seq(b, len, start);
+        if (len > start && start % kChunk) {
+            src = a.table[(size_t)b * C + start / kChunk];
+            if (src < 0 || src >= a.P) src = kNew;
+        }
+        a.copied[2 * b] = src;
+    }
+    __syncthreads();
+    // (the workgroup's own stores, visible to it after the barrier)
+    int base = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kPlan) {
+        const int b = b0 + tid;
+        int need = 0, src = kNone;
+        if (b < a.B) {
+            int len, start;
+            seq(b, len, start);
+            src = a.copied[2 * b];
+            if (src >= 0) {
+                // the first of the sequences that write to the page keeps it if no others have it
+                const int refs = a.refs[src];
+                int writers = 0;
+                bool first = true;
+                if (refs > 1)
+                    for (int o = 0; o < a.B; ++o) {
+                        const int x = a.copied[2 * o];
+                        const bool same = x == src || x == -3 - src;
+                        writers += same;
+                        first = first && !(same && o < b);
+                    }
+                if (refs <= 1 || (first && writers >= refs)) src = -3 - src;  // its own
+            }
+            need = chunks_of(len) - chunks_of(start) + (src >= 0 || src == kNew);
+        }
+        int all;
+        const int before = block_scan(need, s_sum, all);
+        if (b < a.B) {
+            if (src < kNew) a.copied[2 * b] = src;
+            a.copied[2 * b + 1] = base + before;
+        }
+        base += all;
+    }
+    __syncthreads();
+    const int total = base;
+    // free pages, up to as many as are needed
+    int found = 0;
+    for (int p0 = 0; p0 < a.P && found < total; p0 += kPlan * kPer) {
+        int n = 0;
+        for (int i = 0; i < kPer; ++i) {
+            const int p = p0 + tid * kPer + i;
+            n += p < a.P && a.refs[p] <= 0;
+        }
+        int all;
+        (void)block_scan(n, s_sum, all);
+        found += all;
+    }
+    const bool enough = found >= total;
+    if (tid == 0) {
+        a.counts[0] = total;
+        a.counts[1] = min(found, total);
+    }
+    if (!enough) {
+        for (int b = tid; b < a.B; b += kPlan) a.copied[2 * b] = a.copied[2 * b + 1] = -1;
+        return;
+    }
+    int given = 0;
+    for (int p0 = 0; p0 < a.P && given < total; p0 += kPlan * kPer) {
+        unsigned mine = 0;
+        for (int i = 0; i < kPer; ++i) {
+            const int p = p0 + tid * kPer + i;
+            mine |= (unsigned)(p < a.P && a.refs[p] <= 0) << i;
+        }
+        int all;
+        int r = given + block_scan(__popc(mine), s_sum, all);
+        given += all;
+        for (; mine && r < total; mine &= mine - 1, ++r) {
+            const int p = p0 + tid * kPer + __ffs(mine) - 1;
+            int lo = 0, hi = a.B - 1;  // the last sequence whose needs begin at or before r, of those that begin there
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if (a.copied[2 * mid + 1] <= r)
+                    lo = mid;
+                else
+                    hi = mid - 1;
+            }
+            int len, start;
+            seq(lo, len, start);
+            const int src = a.copied[2 * lo];
+            const int k = r - a.copied[2 * lo + 1];
+            // the need's chunk: the page in use that is replaced comes first
+            const int c = (src >= 0 || src == kNew ? start / kChunk : chunks_of(start)) + k;
+            a.table_out[(size_t)lo * C + c] = p;
+            a.refs_out[p] = 1;
+        }
+    }
+    __syncthreads();
+    for (int b = tid; b < a.B; b += kPlan) {
+        const int src = a.copied[2 * b];
+        int len, start;
+        seq(b, len, start);
+        if (src >= 0) atomicSub(&a.refs_out[src], 1);
+        a.copied[2 * b] = src >= 0 ? src : -1;
+        a.copied[2 * b + 1] = src >= 0 ? a.table_out[(size_t)b * C + start / kChunk] : -1;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// copies of pages
+// ---------------------------------------------------------------------------
+struct PoolList {
+    char* data[kPools];
+    size_t bytes[kPools];
+    int slices[kPools + 1];  // slices of the pools before
+    int n;
+};
+// Copy i of *count (or n_max): page from[i * stride] to page to[...]; MAP: to[the source page].
+struct CopyList {
+    const int32_t* from;
+    const int32_t* to;
+    const int32_t* count;  // nullable: n_max
+    int n_max, stride, map;
+};
+__global__ __launch_bounds__(kThreads) void k_cache_copy_pages(PoolList pools, CopyList list, int P) {
+    const int n = list.count ? min(*list.count, list.n_max) : list.n_max;
+    const int per = pools.slices[pools.n];
+    for (size_t u = blockIdx.x; u < (size_t)n * per; u += gridDim.x) {
+        const int i = (int)(u / per), part = (int)(u % per);
+        const int src = list.from[(size_t)i * list.stride];
+        if (src < 0 || src >= P) continue;
+        const int dst = list.map ? list.to[src] : list.to[(size_t)i * list.stride];
+        if (dst < 0 || dst >= P) continue;
+        int k = 0;
+        while (part >= pools.slices[k + 1]) ++k;
+        const size_t bytes = pools.bytes[k], at = (size_t)(part - pools.slices[k]) * kSlice;
+        const size_t len = min(kSlice, bytes - at);
+        const char* x = pools.data[k] + (size_t)src * bytes + at;
+        char* y = pools.data[k] + (size_t)dst * bytes + at;
+        if ((((size_t)pools.data[k] | bytes) & 15) == 0) {
+            for (size_t j = threadIdx.x; j < len / 16; j += kThreads)
+                reinterpret_cast<uint4*>(y)[j] = reinterpret_cast<const uint4*>(x)[j];
+        } else if ((((size_t)pools.data[k] | bytes) & 3) == 0) {
+            for (size_t j = threadIdx.x; j < len / 4; j += kThreads)
+                reinterpret_cast<uint32_t*>(y)[j] = reinterpret_cast<const uint32_t*>(x)[j];
+        } else {
+            for (size_t j = threadIdx.x; j < len; j += kThreads) y[j] = x[j];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// forking
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kThreads) void k_cache_fork_rows(ForkArgs a) {
+    const int C = a.L / kChunk;
+    const size_t step = (size_t)gridDim.x * kThreads, at = (size_t)blockIdx.x * kThreads + threadIdx.x;
+    for (size_t i = at; i < (size_t)a.rows * C; i += step) {
+        const int b = (int)(i / C), c = (int)(i % C), u = a.parent[b];
+        const bool lives = u >= 0 && u < a.B;
+        const int len = lives ? length_of(a.seqlens, u, a.L) : 0;
+        a.table_out[i] = c < chunks_of(len) ? a.table[(size_t)u * C + c] : -1;
+        if (c == 0) a.seqlens_out[b] = len;
+    }
+    if (a.refs_out != a.refs)
+        for (size_t i = at; i < (size_t)a.P; i += step) a.refs_out[i] = a.refs[i];
+}
+// A workgroup per (input row, range of its chunks): the row's pages gain a reference for every
+// row that goes on from it and lose the row's own.
+__global__ __launch_bounds__(kThreads) void k_cache_fork_refs(ForkArgs a, int per) {
+    __shared__ int s_times;
+    const int b = blockIdx.y, C = a.L / kChunk, n = chunks_of(length_of(a.seqlens, b, a.L));
+    const int c0 = blockIdx.x * per;
+    if (c0 >= n) return;
+    if (threadIdx.x == 0) s_times = 0;
+    __syncthreads();
+    int t = 0;
+    for (int i = threadIdx.x; i < a.rows; i += kThreads) t += a.parent[i] == b;
+    if (t) atomicAdd(&s_times, t);
+    __syncthreads();
+    const int change = s_times - 1;
+    if (change == 0) return;
+    for (int c = c0 + threadIdx.x; c < min(n, c0 + per); c += kThreads) {
+        const int p = a.table[(size_t)b * C + c];
+        if (p >= 0 && p < a.P) atomicAdd(&a.refs_out[p], change);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// freeing
+// ---------------------------------------------------------------------------
+// A workgroup per sequence (a length may be overwritten in place: read once, first).
+__global__ __launch_bounds__(kPlan) void k_cache_free(FreeArgs a) {
+    const int b = blockIdx.x, C = a.L / kChunk;
+    const int len = length_of(a.seqlens, b, a.L), kept = min(len, max(a.keep[b], 0));
+    __syncthreads();
+    if (threadIdx.x == 0) a.seqlens_out[b] = kept;
+    const int beg = chunks_of(kept), end = chunks_of(len);
+    for (int c = threadIdx.x; c < C; c += kPlan) {
+        const size_t i = (size_t)b * C + c;
+        const int p = a.table[i];
+        const bool gone = c >= beg && c < end;
+        if (gone && p >= 0 && p < a.P) atomicSub(&a.refs_out[p], 1);
+        if (gone || a.table_out != a.table) a.table_out[i] = gone ? -1 : p;
+    }
+    if (a.pages) {
+        const int n = a.npages ? min(max(a.npages[b], 0), a.most) : a.most;
+        for (int i = threadIdx.x; i < n; i += kPlan) {
+            const int p = a.pages[(size_t)b * a.most + i];
+            if (p >= 0 && p < a.P) atomicSub(&a.refs_out[p], 1);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// compacting
+// ---------------------------------------------------------------------------
+// One workgroup: n pages are in use; the i-th used page at or past n goes to the i-th free one
+// before it.  Both lists are as long, at most half of the pool: the free pages are listed in the
+// second half of `moved` until the pairs are made.
+__global__ __launch_bounds__(kPlan) void k_cache_compact(CompactArgs a) {
+    __shared__ int s_sum[kPlanWaves];
+    const int tid = threadIdx.x, half = (a.P + 1) / 2;
+    int used = 0;
+    for (int p0 = 0; p0 < a.P; p0 += kPlan * kPer) {
+        int n = 0, all;
+        for (int i = 0; i < kPer; ++i) {
+            const int p = p0 + tid * kPer + i;
+            n += p < a.P && a.refs[p] > 0;
+        }
+        (void)block_scan(n, s_sum, all);
+        used += all;
+    }
+    int movers = 0, holes = 0;
+    for (int p0 = 0; p0 < a.P; p0 += kPlan * kPer) {
+        int r[kPer], n = 0, h = 0, all;
+        for (int i = 0; i < kPer; ++i) {
+            const int p = p0 + tid * kPer + i;
+            r[i] = p < a.P ? a.refs[p] : 0;
+            n += p < a.P && p >= used && r[i] > 0;
+            h += p < used && r[i] <= 0;
+        }
+        int at = movers + block_scan(n, s_sum, all);
+        movers += all;
+        int to = holes + block_scan(h, s_sum, all);
+        holes += all;
+        for (int i = 0; i < kPer; ++i) {
+            const int p = p0 + tid * kPer + i;
+            if (p >= a.P) continue;
+            a.new_page[p] = r[i] > 0 ? p : -1;
+            if (a.refs_out != a.refs) a.refs_out[p] = max(r[i], 0);
+            if (p >= used && r[i] > 0) a.moved[at++] = p;
+            if (p < used && r[i] <= 0) a.moved[half + to++] = p;
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < movers; i += kPlan) {
+        const int src = a.moved[i], dst = a.moved[half + i];
+        a.new_page[src] = dst;
+        const int r = a.refs_out[src];  // (a copy of refs, or refs themselves)
+        a.refs_out[dst] = r;
+        a.refs_out[src] = 0;
+    }
+    __syncthreads();
+    for (int i = movers + tid; i < a.P; i += kPlan) a.moved[i] = -1;
+    if (tid == 0) {
+        a.counts[0] = used;
+        a.counts[1] = movers;
+    }
+}
+__global__ __launch_bounds__(kThreads) void k_cache_rename(CompactArgs a) {
+    const int C = a.L / kChunk;
+    const size_t step = (size_t)gridDim.x * kThreads;
+    for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < (size_t)a.B * C; i += step) {
+        const int b = (int)(i / C), c = (int)(i % C), p = a.table[i];
+        const bool held = c < chunks_of(length_of(a.seqlens, b, a.L)) && p >= 0 && p < a.P;
+        a.table_out[i] = held ? a.new_page[p] : p;
+    }
+}
+
+unsigned blocks_for(size_t items, size_t per = kThreads, size_t most = 4096) {
+    return (unsigned)std::max<size_t>(1, std::min(most, (items + per - 1) / per));
+}
+
+void copy_pages(const PoolArg* pools, int num_pools, int P, const CopyList& list, hipStream_t s) {
+    for (int k0 = 0; k0 < num_pools; k0 += kPools) {
+        PoolList x;
+        x.n = std::min(kPools, num_pools - k0);
+        x.slices[0] = 0;
+        for (int k = 0; k < x.n; ++k) {
+            x.data[k] = static_cast<char*>(pools[k0 + k].data);
+            x.bytes[k] = pools[k0 + k].page_bytes;
+            x.slices[k + 1] = x.slices[k] + (int)((x.bytes[k] + kSlice - 1) / kSlice);
+        }
+        HILS_LAUNCH("k_cache_copy_pages", k_cache_copy_pages,
+                    dim3(blocks_for((size_t)list.n_max * x.slices[x.n], 1, 8 * (size_t)device_cus())), dim3(kThreads), 0, s,
+                    x, list, P);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_reserve(const ReserveArgs& a, const PoolArg* pools, int num_pools, hipStream_t s) {
+    const size_t nt = a.table_out != a.table ? (size_t)a.B * (a.L / kChunk) : 0;
+    const size_t np = a.refs_out != a.refs ? (size_t)a.P : 0;
+    if (nt + np)
+        HILS_LAUNCH("k_cache_copy_state", k_cache_copy_state, dim3(blocks_for(std::max(nt, np))), dim3(kThreads), 0, s,
+                    a.table, a.table_out, nt, a.refs, a.refs_out, np);
+    HILS_LAUNCH("k_cache_reserve", k_cache_reserve, dim3(1), dim3(kPlan), 0, s, a);
+    copy_pages(pools, num_pools, a.P, CopyList{a.copied, a.copied + 1, nullptr, a.B, 2, 0}, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_fork(const ForkArgs& a, hipStream_t s) {
+    const int C = a.L / kChunk;
+    const size_t items = std::max((size_t)a.rows * C, a.refs_out != a.refs ? (size_t)a.P : 0);
+    HILS_LAUNCH("k_cache_fork_rows", k_cache_fork_rows, dim3(blocks_for(items)), dim3(kThreads), 0, s, a);
+    const int per = 4 * kThreads;
+    HILS_LAUNCH("k_cache_fork_refs", k_cache_fork_refs, dim3((C + per - 1) / per, a.B), dim3(kThreads), 0, s, a, per);
+    return hipGetLastError();
+}
+
+hipError_t launch_free(const FreeArgs& a, hipStream_t s) {
+    if (a.refs_out != a.refs)
+        HILS_LAUNCH("k_cache_copy_state", k_cache_copy_state, dim3(blocks_for(a.P)), dim3(kThreads), 0, s, a.table,
+                    a.table_out, (size_t)0, a.refs, a.refs_out, (size_t)a.P);
+    HILS_LAUNCH("k_cache_free", k_cache_free, dim3(a.B), dim3(kPlan), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_compact(const CompactArgs& a, const PoolArg* pools, int num_pools, hipStream_t s) {
+    HILS_LAUNCH("k_cache_compact", k_cache_compact, dim3(1), dim3(kPlan), 0, s, a);
+    HILS_LAUNCH("k_cache_rename", k_cache_rename, dim3(blocks_for((size_t)a.B * (a.L / kChunk))), dim3(kThreads), 0, s, a);
+    copy_pages(pools, num_pools, a.P, CopyList{a.moved, a.new_page, a.counts + 1, a.P / 2, 1, 1}, s);
+    return hipGetLastError();
+}
+
+}  // namespace hils

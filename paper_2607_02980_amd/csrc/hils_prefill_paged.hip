@@ -1,0 +1,816 @@
+// Attention of a chunk of new tokens over a paged cache (f32 and bf16 storage, fp32 sums), gfx950.
+//
+// Row n < fresh_b of sequence b is the query at position len_b - fresh_b + n; everything else
+// is the prefill's (Eqs. (1), (9), (10)), with chunk c of sequence b in page block_table[b, c]:
+//
+//   k_pp_score    sigma_ic = max_h s^_hc of 128 rows of a KV group against a slice of the
+//                 candidates, on MFMA tiles; to the workspace, a block of rows at a time
+//   k_pp_select   the K best of each row (exact radix select, ties to the smaller chunk); each
+//                 chosen chunk counts the row and gives it a rank
+//   k_pp_plan     per (b, g): where each chunk's rows start, and the work items
+//   k_pp_fill     the rows of every chunk, by offset and rank
+//   k_pp_chunks   chunk-major: a chunk's K and V are read once and attended by all the rows that
+//                 chose it, 16 (row, head) columns at a time; o_c and s^ of every (row, slot,
+//                 head) go to the workspace as records
+//   k_pp_local    the window [l(i), i] of 16 * 8 / G rows x G heads per workgroup, and the
+//                 fusion with the records
+//
+// A row is computed the same way wherever the rows are cut; the order of a chunk's rows, which
+// depends on atomics, decides only which of them share a matrix instruction, and columns of one
+// do not meet, so results repeat bit for bit.
+//
+// Operands: a 16-byte piece of a row-major row is an MFMA operand in either type.  bf16: 8 of
+// the 32 k-values of v_mfma_f32_16x16x32_bf16; f32: four k-values, one for each of four
+// v_mfma_f32_16x16x4_f32, which take the contraction index in any order as long as both
+// operands agree.  S^T = K Q^T leaves 4 consecutive keys of a column in each lane, the other
+// product's B operand.  O^T = V^T P^T: V by transposing LDS reads (bf16), or as
+// 16-byte reads that each feed four products, accumulator [4 dd + j][i] being dim
+// 64 dd + 16 lg + 4 i + j (f32; lg = l / 16 of lane l).
+#include <algorithm>
+
+#include "hils_device.hpp"
+#include "hils_dispatch.hpp"
+#include "hils_internal.hpp"
+#include "hils_mfma.hpp"
+
+namespace hils {
+
+namespace {
+
+constexpr int kScoreWaves = 8;
+constexpr int kScoreRows = 16 * kScoreWaves;  // rows of a score tile
+constexpr int kScoreCand = 64;                // candidates of a staged landmark block
+constexpr int kSelWaves = 4;
+constexpr int kChunkWaves = 4;
+constexpr int kSegRows = 64;                  // rows of a work item, at most
+constexpr int kLocalWaves = 8;
+
+// 16 bytes of global memory of which only the elements' alignment is known (one instruction).
+template <typename T>
+__device__ __forceinline__ uint4 ld16(const T* p) {
+    uint4 x;
+    __builtin_memcpy(&x, p, 16);
+    return x;
+}
+__device__ __forceinline__ uint4 lds16(const char* p) { return *reinterpret_cast<const uint4*>(p); }
+
+template <typename T, int D>
+struct Cfg {
+    static constexpr int ES = sizeof(T);
+    static constexpr int KS = D * ES / 64;          // operands of a row (64 bytes of it each, over the lane groups)
+    static constexpr int EP = 16 / ES;              // elements of a 16-byte piece
+    static constexpr int DB = D / 16;               // accumulators of O^T
+    static constexpr int KROW = D * ES + 16;        // bytes of a K (landmark) row in LDS
+    static constexpr int VROW = D * ES + (ES == 2 ? 32 : 16);  // and of a V row
+};
+
+template <typename T>
+__device__ __forceinline__ f32x4 mma(const uint4& a, const uint4& b, f32x4 c) {
+    if constexpr (sizeof(T) == 2) {
+        return mfma16x16x32(as_bf16x8(a), as_bf16x8(b), c);
+    } else {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+        return c;
+    }
+}
+
+// o += V^T P^T for the 64 keys of a V tile in LDS, P as the accumulators st of S^T hold it.  bf16:
+// the weights (unnormalised, at most 1) are rounded to bf16, 2^-9 of each, the type they are
+// multiplied in.
+template <typename T, int D>
+__device__ __forceinline__ void add_pv(const char* s_v, const f32x4 (&st)[4], f32x4 (&o)[D / 16], int lane) {
+    using C = Cfg<T, D>;
+    if constexpr (sizeof(T) == 2) {
+        const bf16* v = reinterpret_cast<const bf16*>(s_v);
+        bf16x8 pb[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const float x[8] = {st[2 * t][0],     st[2 * t][1],     st[2 * t][2],     st[2 * t][3],
+                                st[2 * t + 1][0], st[2 * t + 1][1], st[2 * t + 1][2], st[2 * t + 1][3]};
+            pb[t] = pack_bf16x8(x);
+        }
+#pragma unroll
+        for (int db = 0; db < C::DB; ++db) {
+            o[db] = mfma16x16x32(tr_operand_perm(v, C::VROW / 2, 0, db * 16, lane), pb[0], o[db]);
+            o[db] = mfma16x16x32(tr_operand_perm(v, C::VROW / 2, 32, db * 16, lane), pb[1], o[db]);
+            if (db % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const char* row = s_v + (16 * kb + 4 * (lane / 16) + i) * C::VROW + 16 * (lane % 16);
+#pragma unroll
+                for (int dd = 0; dd < D / 64; ++dd) {
+                    const f32x4 v = *reinterpret_cast<const f32x4*>(row + 256 * dd);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        o[4 * dd + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], st[kb][i], o[4 * dd + j], 0, 0, 0);
+                }
+            }
+    }
+}
+
+// Dim of accumulator element [db][i] of lane group lg.
+template <typename T>
+__device__ __forceinline__ int dim_of(int db, int i, int lg) {
+    return sizeof(T) == 2 ? 16 * db + 4 * lg + i : 64 * (db / 4) + 16 * lg + 4 * i + db % 4;
+}
+
+// New tokens of a sequence: `fresh` of them, the last of `len`.
+struct Seq {
+    int len, fresh, pos0;
+};
+__device__ __forceinline__ Seq sequence(const FwdArgs& f, const int32_t* newlens, int b) {
+    Seq s;
+    s.len = f.seqlens ? min(max(f.seqlens[b], 0), f.L) : f.L;
+    s.fresh = min(newlens ? min(max(newlens[b], 0), f.N) : f.N, s.len);
+    s.pos0 = s.len - s.fresh;
+    return s;
+}
+__device__ __forceinline__ size_t page_of(const FwdArgs& f, int b, int c) {
+    return (size_t)min(max(f.block_table[(size_t)b * (f.L / kChunk) + c], 0), f.num_pages - 1);
+}
+
+// Workspace of one segment of rows n0 .. n0 + Ns - 1 of every sequence.
+struct Ws {
+    int* counts;   // [bg][nC] rows of each chunk, then one word: the work items
+    int* offs;     // [bg][nC] start of its rows in list
+    int* ranks;    // [bg][Ns][K] rank of a row among its chunk's, -1: no chunk
+    int* list;     // [bg][Ns * K] row << 6 | slot
+    int4* work;    // (bg, chunk, offset, rows)
+    float* sigma;  // [bg][Rs][nC]
+    float* rec_s;  // [bg][Ns][K][G]
+    float* rec_o;  // [bg][Ns][K][G][D], as the accumulators hold them
+};
+struct Layout {
+    size_t counts, offs, ranks, list, work, sigma, rec_s, rec_o, total;
+    int Ns, Rs;
+    size_t max_work;
+};
+
+// sigma of a block of rows: as many as fit the last-level cache, in whole score tiles
+constexpr size_t kSigmaBytes = size_t(128) << 20;
+
+Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K) {
+    Layout w;
+    const size_t nC = L / kChunk, bg = (size_t)B * Hkv;
+    const size_t per_row = (size_t)B * Hq * K * (d + 1) * sizeof(float);
+    const size_t cap = prefill_record_cap(0);
+    size_t ns = N;
+    if (ns * per_row > cap) ns = std::min<size_t>(N, std::max<size_t>(kScoreRows, cap / per_row / kScoreRows * kScoreRows));
+    size_t rs = kSigmaBytes / (bg * nC * sizeof(float)) / kScoreRows * kScoreRows;
+    rs = std::min(ns, std::max<size_t>(rs, kScoreRows));
+    w.Ns = (int)ns;
+    w.Rs = (int)rs;
+    w.max_work = bg * (std::min(nC, ns * K) + ns * K / kSegRows);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at = align256(at + bytes);
+        return here;
+    };
+    w.counts = take((bg * nC + 1) * sizeof(int));
+    w.offs = take(bg * nC * sizeof(int));
+    w.ranks = take(bg * ns * K * sizeof(int));
+    w.list = take(bg * ns * K * sizeof(int));
+    w.work = take(w.max_work * sizeof(int4));
+    w.sigma = take(bg * rs * nC * sizeof(float));
+    w.rec_s = take(bg * ns * K * (Hq / Hkv) * sizeof(float));
+    w.rec_o = take(bg * ns * K * (Hq / Hkv) * d * sizeof(float));
+    w.total = at;
+    return w;
+}
+
+// ---------------------------------------------------------------------------
+// scores
+// ---------------------------------------------------------------------------
+// A workgroup of 8 waves takes 128 rows of a KV group (16 each) and `slice` candidates; 64
+// landmark rows of one head at a time come through LDS (double-buffered) and serve all rows;
+// the maximum over the heads stays in registers until a block of candidates is done.
+template <typename T, int D, int G>
+__global__ __launch_bounds__(kScoreWaves * kWave) void k_pp_score(FwdArgs f, const int32_t* newlens, float* sigma,
+                                                                 int r0, int Rs, int slice, int nslices) {
+    using C = Cfg<T, D>;
+    constexpr int NT = kScoreWaves * kWave;
+    constexpr int PPT = kScoreCand * D * C::ES / 16 / NT;
+    constexpr bool kHold = C::ES == 2;  // the query operands of all heads fit in registers
+    static_assert(PPT >= 1 && PPT * NT * 16 == kScoreCand * D * C::ES, "landmark blocks split evenly over the threads");
+    __shared__ __align__(16) char s_l[2][kScoreCand * C::KROW];
+    __shared__ float s_b[2][kScoreCand];
+    const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave, lg = lane / 16;
+    const int ntiles = (Rs + kScoreRows - 1) / kScoreRows;
+    int at = blockIdx.x;
+    const int g = at % f.Hkv;
+    at /= f.Hkv;
+    const int part = at % nslices;
+    at /= nslices;
+    const int tile = at % ntiles, b = at / ntiles;
+    const Seq sq = sequence(f, newlens, b);
+    const int q0 = r0 + tile * kScoreRows;
+    const int qend = min(min(q0 + kScoreRows, r0 + Rs), sq.fresh);
+    if (q0 >= qend) return;
+    const int nC = f.L / kChunk;
+    const int c_beg = part * slice, c_end = min(n_candidates(sq.pos0 + qend - 1, f.W), c_beg + slice);
+    if (c_beg >= c_end) return;
+    const bool shared_lmk = f.Hl != f.Hq;
+    const int NH = shared_lmk ? 1 : G;
+    const T* qr = as<T>(f.q_route ? f.q_route : f.q);
+    const int qa = min(q0 + 16 * w + lane % 16, qend - 1);
+    auto q_operand = [&](int hh, int ks) {
+        return ld16(qr + (((size_t)b * f.Hq + g * G + hh) * f.N + qa) * D + ks * 4 * C::EP + lg * C::EP);
+    };
+    uint4 aq[kHold ? G : 1][C::KS];
+    if constexpr (kHold) {
+#pragma unroll
+        for (int hh = 0; hh < G; ++hh)
+#pragma unroll
+            for (int ks = 0; ks < C::KS; ++ks) aq[hh][ks] = q_operand(hh, ks);
+    }
+    struct Regs {
+        uint4 x[PPT];
+        float bv;
+    };
+    // step t: candidate block t / NH, landmark head t % NH
+    auto fetch = [&](int t) {
+        const int hl = shared_lmk ? g : g * G + t % NH, c0 = c_beg + (t / NH) * kScoreCand;
+        Regs r;
+#pragma unroll
+        for (int u = 0; u < PPT; ++u) {
+            const int e = tid + u * NT, j = e / (D / C::EP), d0 = (e % (D / C::EP)) * C::EP;
+            const size_t pg = page_of(f, b, min(c0 + j, c_end - 1));
+            r.x[u] = ld16(as<T>(f.lmk) + (pg * f.Hl + hl) * D + d0);
+        }
+        r.bv = f.bias && tid < kScoreCand ? f.bias[page_of(f, b, min(c0 + tid, c_end - 1)) * f.Hl + hl] : 0.f;
+        return r;
+    };
+    auto store = [&](int buf, const Regs& r) {
+#pragma unroll
+        for (int u = 0; u < PPT; ++u) {
+            const int e = tid + u * NT, j = e / (D / C::EP), d0 = (e % (D / C::EP)) * C::EP;
+            *reinterpret_cast<uint4*>(&s_l[buf][j * C::KROW + d0 * C::ES]) = r.x[u];
+        }
+        if (tid < kScoreCand) s_b[buf][tid] = r.bv;
+    };
+    const size_t bg = (size_t)b * f.Hkv + g;
+    const int nsteps = (c_end - c_beg + kScoreCand - 1) / kScoreCand * NH;
+    Regs nx = fetch(0);
+    store(0, nx);
+    __syncthreads();
+    f32x4 sg[4];
+    for (int t = 0; t < nsteps; ++t) {
+        const int buf = t & 1, lh = t % NH;
+        const bool more = t + 1 < nsteps;  // uniform
+        if (more) nx = fetch(t + 1);
+        if (lh == 0)
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb) sg[nb] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto head = [&](const uint4 (&q)[C::KS]) {
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb) {
+                f32x4 acc = zero4();
+#pragma unroll
+                for (int ks = 0; ks < C::KS; ++ks)
+                    acc = mma<T>(q[ks], lds16(&s_l[buf][(nb * 16 + lane % 16) * C::KROW + ks * 64 + lg * 16]), acc);
+                const float bv = s_b[buf][nb * 16 + lane % 16];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sg[nb][i] = fmaxf(sg[nb][i], f.scale * acc[i] + bv);  // (a NaN loses)
+            }
+        };
+        if constexpr (kHold) {
+#pragma unroll
+            for (int hh = 0; hh < G; ++hh)
+                if (shared_lmk || hh == lh) head(aq[hh]);
+        } else {
+            for (int hh = shared_lmk ? 0 : lh; hh <= (shared_lmk ? G - 1 : lh); ++hh) {
+#pragma unroll
+                for (int ks = 0; ks < C::KS; ++ks) aq[0][ks] = q_operand(hh, ks);
+                head(aq[0]);
+            }
+        }
+        if (lh == NH - 1) {
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb) {
+                const int c = c_beg + (t / NH) * kScoreCand + nb * 16 + lane % 16;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int n = q0 + 16 * w + 4 * lg + i;
+                    if (n < qend && c < c_end) sigma[(bg * Rs + (n - r0)) * nC + c] = sg[nb][i];
+                }
+            }
+        }
+        if (more) store(buf ^ 1, nx);
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(256) void k_pp_clear(int* p, size_t n) {
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
+}
+
+// One wave per row: the K best of its candidates (E registers of 64 at a time, the best so far
+// beside them), or the valid entries of a given selection; each counts the row for its chunk.
+template <int E>
+__global__ __launch_bounds__(kSelWaves * kWave) void k_pp_select(FwdArgs f, const int32_t* newlens, const float* sigma,
+                                                                int* counts, int* ranks, int n0, int Ns, int r0,
+                                                                int Rs) {
+    __shared__ int s_tid[kSelWaves][kWave];
+    __shared__ __align__(16) float s_tsc[kSelWaves][kWave];
+    __shared__ int s_oid[kSelWaves][kWave];
+    __shared__ float s_osc[kSelWaves][kWave];
+    const int w = wave_id(), lane = threadIdx.x % kWave;
+    const size_t r = (size_t)blockIdx.x * kSelWaves + w;
+    if (r >= (size_t)f.B * f.Hkv * Rs) return;  // whole wave
+    const size_t bg = r / Rs;
+    const int b = (int)(bg / f.Hkv), n = r0 + (int)(r % Rs);
+    const Seq sq = sequence(f, newlens, b);
+    if (n >= sq.fresh) return;
+    const int nC = f.L / kChunk, lim = n_candidates(sq.pos0 + n, f.W);
+    int32_t* orow = f.idx + (bg * f.N + n) * f.K;
+    int c = -1;
+    if (f.given_idx) {
+        if (lane < f.K && idx_entry_valid(orow, lane, lim)) c = orow[lane];
+    } else {
+        const float* row = sigma + r * nC;
+        int m = 0;
+        for (int c0 = 0; c0 < lim; c0 += E * kWave) {
+            float sc[E + 1];
+            int id[E + 1];
+            bool ok[E + 1];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                id[e] = c0 + e * kWave + lane;
+                ok[e] = id[e] < lim;
+                sc[e] = ok[e] ? row[id[e]] : 0.f;
+            }
+            ok[E] = lane < m;
+            sc[E] = ok[E] ? s_osc[w][lane] : 0.f;
+            id[E] = ok[E] ? s_oid[w][lane] : -1;
+            m = wave_topk_reg<E + 1, E>(sc, id, ok, f.K, s_oid[w], s_osc[w], s_tid[w], s_tsc[w]);
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        if (lane < m) c = s_oid[w][lane];
+        if (lane < f.K) orow[lane] = c;
+    }
+    if (lane < f.K) ranks[(bg * Ns + (n - n0)) * f.K + lane] = c >= 0 ? atomicAdd(&counts[bg * nC + c], 1) : -1;
+}
+
+// ---------------------------------------------------------------------------
+// rows of every chunk
+// ---------------------------------------------------------------------------
+// One workgroup per (b, g): offsets of the chunks' rows in the list, and the work items (runs of
+// up to kSegRows rows of a chunk), which take a range of `work` of their own.
+constexpr int kPlanThreads = 1024;
+__global__ __launch_bounds__(kPlanThreads) void k_pp_plan(int nC, const int* counts, int* offs, int4* work,
+                                                         int* nwork) {
+    __shared__ int s_rows[kPlanThreads / kWave], s_items[kPlanThreads / kWave], s_base;
+    const int bg = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, w = tid / kWave;
+    const int* cnt = counts + (size_t)bg * nC;
+    auto scan = [&](int x, int* s_sum, int& before, int& all) {  // over the workgroup
+        int incl = x;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int y = __shfl_up(incl, o, kWave);
+            if (lane >= o) incl += y;
+        }
+        if (lane == kWave - 1) s_sum[w] = incl;
+        __syncthreads();
+        before = incl - x;
+        all = 0;
+        for (int i = 0; i < kPlanThreads / kWave; ++i) {
+            before += i < w ? s_sum[i] : 0;
+            all += s_sum[i];
+        }
+    };
+    int items = 0;
+    for (int c = tid; c < nC; c += kPlanThreads) items += (cnt[c] + kSegRows - 1) / kSegRows;
+    int before, all;
+    scan(items, s_items, before, all);
+    if (tid == 0) s_base = all ? atomicAdd(nwork, all) : 0;
+    __syncthreads();
+    int rows0 = 0, items0 = s_base;
+    for (int c0 = 0; c0 < nC; c0 += kPlanThreads) {
+        const int c = c0 + tid, n = c < nC ? cnt[c] : 0, k = (n + kSegRows - 1) / kSegRows;
+        int r, ra, i, ia;
+        scan(n, s_rows, r, ra);
+        scan(k, s_items, i, ia);
+        if (c < nC) offs[(size_t)bg * nC + c] = rows0 + r;
+        for (int s = 0; s < k; ++s)
+            work[items0 + i + s] = make_int4(bg, c, rows0 + r + s * kSegRows, min(kSegRows, n - s * kSegRows));
+        rows0 += ra;
+        items0 += ia;
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(256) void k_pp_fill(FwdArgs f, const int32_t* newlens, const int* offs, const int* ranks,
+                                                 int* list, int n0, int Ns) {
+    const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= (size_t)f.B * f.Hkv * Ns * f.K) return;
+    const int slot = (int)(e % f.K);
+    const size_t row = e / f.K, bg = row / Ns;
+    const int n = (int)(row % Ns);
+    if (n0 + n >= sequence(f, newlens, (int)(bg / f.Hkv)).fresh) return;
+    const int rank = ranks[e];
+    if (rank < 0) return;
+    const int c = f.idx[(bg * f.N + n0 + n) * f.K + slot];
+    list[bg * Ns * f.K + offs[bg * (f.L / kChunk) + c] + rank] = n << 6 | slot;
+}
+
+// ---------------------------------------------------------------------------
+// retrieved chunks
+// ---------------------------------------------------------------------------
+// A workgroup takes one work item after the other: K and V of the chunk and the landmark rows of
+// the group's heads in LDS, then columns p = (entry p / G, head p % G), 16 to a wave at a
+// time, so that a chunk with few rows still fills its instructions with their heads.
+template <typename T, int D, int G>
+__global__ __launch_bounds__(kChunkWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k_pp_chunks(FwdArgs f, Ws ws,
+                                                                                          const int* nwork, int n0,
+                                                                                          int Ns) {
+    using C = Cfg<T, D>;
+    constexpr int NT = kChunkWaves * kWave;
+    constexpr int PPT = kChunk * D * C::ES / 16 / NT;
+    __shared__ __align__(16) char s_k[kChunk * C::KROW];
+    __shared__ __align__(16) char s_v[kChunk * C::VROW];
+    __shared__ __align__(16) char s_l[G * D * C::ES];
+    __shared__ float s_b[G];
+    const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave, lg = lane / 16;
+    const int col = lane % 16, hh = col % G;
+    const int items = *nwork;
+    const float c1 = f.scale * kLog2e;
+    for (int it = blockIdx.x; it < items; it += gridDim.x) {
+        const int4 wi = ws.work[it];
+        const int b = wi.x / f.Hkv, g = wi.x % f.Hkv, c = wi.y, len = wi.w;
+        const size_t bg = wi.x, pg = page_of(f, b, c);
+        {
+            const T* k = as<T>(f.k) + (pg * f.Hkv + g) * kChunk * D;
+            const T* v = as<T>(f.v) + (pg * f.Hkv + g) * kChunk * D;
+            uint4 kr[PPT], vr[PPT];
+#pragma unroll
+            for (int u = 0; u < PPT; ++u) {
+                kr[u] = ld16(k + (size_t)(tid + u * NT) * C::EP);
+                vr[u] = ld16(v + (size_t)(tid + u * NT) * C::EP);
+            }
+            __syncthreads();  // the previous item has been read
+            for (int e = tid; e < G * D / C::EP; e += NT) {
+                const int h = e / (D / C::EP), d0 = (e % (D / C::EP)) * C::EP;
+                const size_t lrow = pg * f.Hl + (f.Hl == f.Hq ? g * G + h : g);
+                *reinterpret_cast<uint4*>(s_l + h * D * C::ES + d0 * C::ES) = ld16(as<T>(f.lmk) + lrow * D + d0);
+                if (d0 == 0) s_b[h] = f.bias ? f.bias[lrow] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < PPT; ++u) {
+                const int e = tid + u * NT, j = e / (D / C::EP), at = (e % (D / C::EP)) * 16;
+                *reinterpret_cast<uint4*>(s_k + j * C::KROW + at) = kr[u];
+                *reinterpret_cast<uint4*>(s_v + j * C::VROW + at) = vr[u];
+            }
+        }
+        __syncthreads();
+        const int* seg = ws.list + bg * (size_t)Ns * f.K + wi.z;
+        const int units = (len * G + 15) / 16;
+        for (int u = w; u < units; u += kChunkWaves) {
+            const int e = u * (16 / G) + col / G;
+            const bool live = e < len;
+            const int ent = seg[min(e, len - 1)], n = ent >> 6, slot = ent & 63;
+            const size_t qrow = (((size_t)b * f.Hq + g * G + hh) * f.N + n0 + n) * D;
+            uint4 q[C::KS];
+#pragma unroll
+            for (int ks = 0; ks < C::KS; ++ks) q[ks] = ld16(as<T>(f.q) + qrow + ks * 4 * C::EP + lg * C::EP);
+            // s^: the heads' landmark rows are rows 0 .. G - 1 of the A operand, so column p's is
+            // accumulator row p % G, which lane group hh / 4 holds as element hh % 4
+            f32x4 sh = zero4();
+#pragma unroll
+            for (int ks = 0; ks < C::KS; ++ks) {
+                uint4 al = lds16(s_l + min(col, G - 1) * D * C::ES + ks * 64 + lg * 16);
+                if (col >= G) al = make_uint4(0, 0, 0, 0);
+                const uint4 qs = f.q_route ? ld16(as<T>(f.q_route) + qrow + ks * 4 * C::EP + lg * C::EP) : q[ks];
+                sh = mma<T>(al, qs, sh);
+            }
+            const int hi = hh & 3;
+            const float shv = hi == 0 ? sh[0] : hi == 1 ? sh[1] : hi == 2 ? sh[2] : sh[3];
+            const float shr = __shfl(shv, (hh >> 2) * 16 + col, kWave);
+            const float bias = s_b[hh];
+            const float shat = bias == -INFINITY ? -INFINITY : f.scale * shr + bias;
+            f32x4 st[4];
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                st[kb] = zero4();
+#pragma unroll
+                for (int ks = 0; ks < C::KS; ++ks)
+                    st[kb] = mma<T>(lds16(s_k + (kb * 16 + col) * C::KROW + ks * 64 + lg * 16), q[ks], st[kb]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    st[kb][i] *= c1;
+                    mx = fmaxf(mx, st[kb][i]);
+                }
+            mx = group4_max(mx);
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    st[kb][i] = fexp2(st[kb][i] - mx);
+                    sum += st[kb][i];
+                }
+            sum = group4_sum(sum);
+            f32x4 o[C::DB];
+#pragma unroll
+            for (int db = 0; db < C::DB; ++db) o[db] = zero4();
+            add_pv<T, D>(s_v, st, o, lane);
+            const float inv = 1.f / sum;
+            if (live) {
+                const size_t rec = ((bg * Ns + n) * f.K + slot) * G + hh;
+#pragma unroll
+                for (int db = 0; db < C::DB; ++db)
+                    *reinterpret_cast<f32x4*>(ws.rec_o + rec * D + db * 16 + lg * 4) = o[db] * inv;
+                if (lg == 0) ws.rec_s[rec] = shat;
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// window and fusion
+// ---------------------------------------------------------------------------
+template <int G>
+struct Tile {
+    static constexpr int WR = 16 / G;            // rows of a wave (x G heads: 16 columns)
+    static constexpr int QT = WR * kLocalWaves;  // rows of a workgroup
+};
+
+// The 64-key blocks of the tile's windows are double-buffered in LDS; then each row's records
+// are added, every (row, head) stabilised by its own maximum M of log Z_swa and the s^:
+//   out = (e^{log Z_swa - M} o_swa + sum_k e^{s^_k - M} o_k) / (e^{log Z_swa - M} + sum_k e^{s^_k - M})
+// Rows of V at or past the length are staged as zeros (nobody has written them).  Where a block
+// holds an infinity or a NaN among values that some row of the tile must not see, 0 * it
+// would reach that row: such a block's values are added one key at a time.
+template <typename T, int D, int G>
+__global__ __launch_bounds__(kLocalWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k_pp_local(FwdArgs f,
+                                                                                         const int32_t* newlens,
+                                                                                         const float* rec_s,
+                                                                                         const float* rec_o, int n0,
+                                                                                         int Ns) {
+    using C = Cfg<T, D>;
+    constexpr int NT = kLocalWaves * kWave, QT = Tile<G>::QT, WR = Tile<G>::WR;
+    constexpr int PPT = kChunk * D * C::ES / 16 / NT;
+    __shared__ __align__(16) char s_k[2][kChunk * C::KROW];
+    __shared__ __align__(16) char s_v[2][kChunk * C::VROW];
+    __shared__ int s_bad[2];  // first key of the block in the buffer if its values are not all finite
+    const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave, lg = lane / 16;
+    const int col = lane % 16, hh = col % G;
+    const int ntiles = (Ns + QT - 1) / QT;
+    int at = blockIdx.x;
+    const int g = at % f.Hkv;
+    at /= f.Hkv;
+    const int tile = at % ntiles, b = at / ntiles;
+    const Seq sq = sequence(f, newlens, b);
+    const int q0 = n0 + tile * QT, qend = min(min(q0 + QT, n0 + Ns), sq.fresh);
+    if (q0 >= qend) return;
+    const size_t bg = (size_t)b * f.Hkv + g;
+    const int n = min(q0 + w * WR + col / G, qend - 1), pos = sq.pos0 + n;
+    const bool live = q0 + w * WR + col / G < qend;
+    const int ncand = n_candidates(pos, f.W), ell = ncand * kChunk;
+    const int kbeg = n_candidates(sq.pos0 + q0, f.W) * kChunk, klast = sq.pos0 + qend - 1;
+    const int kfull = n_candidates(klast, f.W) * kChunk;  // keys from here to pos0 + q0 are in every row's window
+    const size_t row = ((size_t)b * f.Hq + g * G + hh) * f.N + n;
+    const float c1 = f.scale * kLog2e;
+    if (tid < 2) s_bad[tid] = -1;
+
+    struct KV {
+        uint4 k[PPT], v[PPT];
+    };
+    auto fetch = [&](int j0) {
+        const size_t base = (page_of(f, b, j0 / kChunk) * f.Hkv + g) * kChunk * D;
+        KV x;
+#pragma unroll
+        for (int u = 0; u < PPT; ++u) {
+            x.k[u] = ld16(as<T>(f.k) + base + (size_t)(tid + u * NT) * C::EP);
+            x.v[u] = ld16(as<T>(f.v) + base + (size_t)(tid + u * NT) * C::EP);
+        }
+        return x;
+    };
+    auto masked = [&](int j0) { return j0 < kfull || j0 + kChunk - 1 > sq.pos0 + q0; };
+    auto stage = [&](int buf, int j0, const KV& x) {
+        bool bad = false;
+#pragma unroll
+        for (int u = 0; u < PPT; ++u) {
+            const int e = tid + u * NT, j = e / (D / C::EP), piece = (e % (D / C::EP)) * 16;
+            uint4 v = x.v[u];
+            if (j0 + j >= sq.len) v = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(&s_k[buf][j * C::KROW + piece]) = x.k[u];
+            *reinterpret_cast<uint4*>(&s_v[buf][j * C::VROW + piece]) = v;
+            const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                bad |= (y[i] & 0x7f800000u) == 0x7f800000u;
+                if constexpr (C::ES == 2) bad |= (y[i] & 0x7f80u) == 0x7f80u;
+            }
+        }
+        if (bad && masked(j0)) s_bad[buf] = j0;
+    };
+
+    uint4 q[C::KS];
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks) q[ks] = ld16(as<T>(f.q) + row * D + ks * 4 * C::EP + lg * C::EP);
+    f32x4 o[C::DB];
+#pragma unroll
+    for (int db = 0; db < C::DB; ++db) o[db] = zero4();
+    float m = -INFINITY, l = 0.f;  // running maximum (log2 units) and sum
+    __syncthreads();               // s_bad is set
+    KV nx = fetch(kbeg);
+    stage(0, kbeg, nx);
+    __syncthreads();
+    int buf = 0;
+    for (int j0 = kbeg; j0 <= klast; j0 += kChunk, buf ^= 1) {
+        const bool more = j0 + kChunk <= klast;  // uniform
+        if (more) nx = fetch(j0 + kChunk);
+        f32x4 st[4];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            st[kb] = zero4();
+#pragma unroll
+            for (int ks = 0; ks < C::KS; ++ks)
+                st[kb] = mma<T>(lds16(&s_k[buf][(kb * 16 + col) * C::KROW + ks * 64 + lg * 16]), q[ks], st[kb]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        const bool part = masked(j0);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = j0 + kb * 16 + lg * 4 + i;
+                st[kb][i] = !part || (j <= pos && j >= ell) ? st[kb][i] * c1 : -INFINITY;
+                mx = fmaxf(mx, st[kb][i]);
+            }
+        mx = group4_max(mx);
+        const float mnew = fmaxf(m, mx), muse = mnew == -INFINITY ? 0.f : mnew;
+        const float alpha = fexp2(m - muse);
+        float psum = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                st[kb][i] = fexp2(st[kb][i] - muse);
+                psum += st[kb][i];
+            }
+        psum = group4_sum(psum);
+        l = l * alpha + psum;
+        m = mnew;
+#pragma unroll
+        for (int db = 0; db < C::DB; ++db) o[db] *= alpha;
+        if (part && s_bad[buf] == j0) {  // uniform
+            for (int j = 0; j < kChunk; ++j) {
+                const int kb = j / 16, i = j % 4;
+                float mine = 0.f;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) mine = kb == x && i == y ? st[x][y] : mine;
+                const float p = __shfl(mine, (j % 16) / 4 * 16 + col, kWave);
+                const bool sees = j0 + j <= pos && j0 + j >= ell;
+                const T* v = reinterpret_cast<const T*>(&s_v[buf][j * C::VROW]);
+#pragma unroll
+                for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        o[db][y] = sees ? fmaf(p, to_f32(v[dim_of<T>(db, y, lg)]), o[db][y]) : o[db][y];
+            }
+        } else {
+            add_pv<T, D>(s_v[buf], st, o, lane);
+        }
+        if (more) stage(buf ^ 1, j0 + kChunk, nx);
+        __syncthreads();
+    }
+
+    // the fusion (lane: its column's dims), slots in idx order
+    // (the query's own key is in its window; l is 0 only where every key scores -inf)
+    const float lam0 = l > 0.f ? (m + __log2f(l)) * (1.f / kLog2e) : -INFINITY;
+    float M = lam0, zs = l > 0.f ? 1.f : 0.f;
+    const float inv_l = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int db = 0; db < C::DB; ++db) o[db] *= inv_l;
+    const int32_t* irow = f.idx + (bg * f.N + n) * f.K;
+    const size_t rec0 = (bg * Ns + (n - n0)) * f.K;
+    int prev = -1;
+    for (int k = 0; k < f.K; ++k) {
+        const int c = irow[k];
+        const bool ok = c >= 0 && c < ncand && c > prev;  // as idx_entry_valid
+        prev = c;
+        if (__ballot(ok) == 0ull) continue;
+        const size_t rec = (rec0 + k) * G + hh;
+        const float s = ok ? rec_s[rec] : -INFINITY;
+        const bool adds = s != -INFINITY;  // (a masked chunk's record may hold anything)
+        const float Mn = adds ? fmaxf(M, s) : M;
+        const float rs = Mn == M ? 1.f : fexp(M - Mn), wk = adds ? fexp(s - Mn) : 0.f;
+        M = Mn;
+        zs = zs * rs + wk;
+#pragma unroll
+        for (int db = 0; db < C::DB; ++db) {
+            f32x4 x = zero4();
+            if (adds) x = *reinterpret_cast<const f32x4*>(rec_o + rec * D + db * 16 + lg * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[db][i] = fmaf(wk, x[i], o[db][i] * rs);
+        }
+    }
+    if (!live) return;
+    const float inv = 1.f / zs;
+    T* out = as_mut<T>(f.out) + row * D;
+#pragma unroll
+    for (int db = 0; db < C::DB; ++db) {
+        if constexpr (C::ES == 2) {
+            const f32x4 r = o[db] * inv;
+            store_unaligned(out + 16 * db + 4 * lg, make_uint2(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])));
+        } else {
+            const int dd = db / 4, i = db % 4;  // element i of the four accumulators of block dd: four dims in a row
+            const f32x4 r = {o[4 * dd][i] * inv, o[4 * dd + 1][i] * inv, o[4 * dd + 2][i] * inv, o[4 * dd + 3][i] * inv};
+            __builtin_memcpy(out + 64 * dd + 16 * lg + 4 * i, &r, 16);
+        }
+    }
+    if (lg == 0) f.lse[row] = M + __logf(zs);
+}
+
+struct Run {
+    template <typename T, int D, int G>
+    static hipError_t run(const PrefillPagedArgs& a, hipStream_t s) {
+        const FwdArgs& f = a.f;
+        const Layout ly = layout(f.B, f.Hq, f.Hkv, f.N, f.L, D, f.K);
+        char* base = static_cast<char*>(f.ws);
+        Ws ws;
+        ws.counts = reinterpret_cast<int*>(base + ly.counts);
+        ws.offs = reinterpret_cast<int*>(base + ly.offs);
+        ws.ranks = reinterpret_cast<int*>(base + ly.ranks);
+        ws.list = reinterpret_cast<int*>(base + ly.list);
+        ws.work = reinterpret_cast<int4*>(base + ly.work);
+        ws.sigma = reinterpret_cast<float*>(base + ly.sigma);
+        ws.rec_s = reinterpret_cast<float*>(base + ly.rec_s);
+        ws.rec_o = reinterpret_cast<float*>(base + ly.rec_o);
+        const int nC = f.L / kChunk, maxc = n_candidates(f.L - 1, f.W);  // candidates of any row, at most
+        const size_t bg = (size_t)f.B * f.Hkv, ncount = bg * nC;
+        const int cus = device_cus();
+        for (int n0 = 0; n0 < f.N; n0 += ly.Ns) {
+            const int Ns = std::min(ly.Ns, f.N - n0);
+            HILS_LAUNCH("k_pp_clear", k_pp_clear, dim3((unsigned)std::min<size_t>((ncount + 256) / 256, 4096)), dim3(256),
+                        0, s, ws.counts, ncount + 1);
+            for (int r0 = n0; r0 < n0 + Ns; r0 += ly.Rs) {
+                const int Rs = std::min(ly.Rs, n0 + Ns - r0);
+                if (!f.given_idx && maxc > 0) {
+                    // slices of candidates for a few workgroups per CU where there are few rows
+                    const size_t tiles = bg * ((Rs + kScoreRows - 1) / kScoreRows);
+                    const size_t want = std::max<size_t>(1, 4 * (size_t)cus / tiles);
+                    const int blocks = (maxc + kScoreCand - 1) / kScoreCand;
+                    const int slice = kScoreCand * (int)((blocks + want - 1) / want);
+                    const int nslices = (maxc + slice - 1) / slice;
+                    HILS_LAUNCH("k_pp_score", (k_pp_score<T, D, G>), dim3((unsigned)(tiles * nslices)),
+                                dim3(kScoreWaves * kWave), 0, s, f, a.newlens, ws.sigma, r0, Rs, slice, nslices);
+                }
+                const dim3 grid((unsigned)((bg * Rs + kSelWaves - 1) / kSelWaves));
+                auto select = [&](auto e_tag) {
+                    constexpr int E = decltype(e_tag)::value;
+                    HILS_LAUNCH("k_pp_select", k_pp_select<E>, grid, dim3(kSelWaves * kWave), 0, s, f, a.newlens,
+                                (const float*)ws.sigma, ws.counts, ws.ranks, n0, Ns, r0, Rs);
+                };
+                if (maxc <= kWave)
+                    select(std::integral_constant<int, 1>{});
+                else if (maxc <= 4 * kWave)
+                    select(std::integral_constant<int, 4>{});
+                else
+                    select(std::integral_constant<int, 16>{});
+            }
+            int* nwork = ws.counts + ncount;
+            if (maxc > 0) {
+                HILS_LAUNCH("k_pp_plan", k_pp_plan, dim3((unsigned)bg), dim3(kPlanThreads), 0, s, nC,
+                            (const int*)ws.counts, ws.offs, ws.work, nwork);
+                HILS_LAUNCH("k_pp_fill", k_pp_fill, dim3((unsigned)((bg * Ns * f.K + 255) / 256)), dim3(256), 0, s, f,
+                            a.newlens, (const int*)ws.offs, (const int*)ws.ranks, ws.list, n0, Ns);
+                const size_t most = bg * (std::min<size_t>(maxc, (size_t)Ns * f.K) + (size_t)Ns * f.K / kSegRows);
+                HILS_LAUNCH("k_pp_chunks", (k_pp_chunks<T, D, G>), dim3((unsigned)std::min<size_t>(most, 16 * cus)),
+                            dim3(kChunkWaves * kWave), 0, s, f, ws, (const int*)nwork, n0, Ns);
+            }
+            const int ntiles = (Ns + Tile<G>::QT - 1) / Tile<G>::QT;
+            HILS_LAUNCH("k_pp_local", (k_pp_local<T, D, G>), dim3((unsigned)(bg * ntiles)), dim3(kLocalWaves * kWave), 0,
+                        s, f, a.newlens, (const float*)ws.rec_s, (const float*)ws.rec_o, n0, Ns);
+        }
+        return hipGetLastError();
+    }
+};
+
+}  // namespace
+
+size_t prefill_paged_workspace_bytes(int B, int Hq, int Hkv, int N, int L, int d, int K) {
+    return layout(B, Hq, Hkv, N, L, d, K).total;
+}
+
+hipError_t launch_prefill_paged(const PrefillPagedArgs& a, hipStream_t s) {
+    return dispatch<Run>(a.f.bf16, a.f.d, a.f.Hq / a.f.Hkv, a, s);
+}
+
+}  // namespace hils

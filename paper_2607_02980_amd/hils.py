@@ -4,7 +4,8 @@ The entry points keep the C names (``hils_prefill_fwd``, ``hils_decode_fwd``,
 ``hils_decode_fwd_noalloc``, ``hils_decode_paged_fwd``, ``hils_bwd``,
 ``hils_landmark_fwd``, ``hils_landmark_bwd``, ``hils_q8_append``,
 ``hils_q8_landmark_fwd``, ``hils_decode_q8_fwd``, ``hils_cache_evict``,
-``hils_workspace_size``, ``hils_prefill_record_cap``, ``hils_last_error``, ``hils_version``).
+``hils_prefill_paged_fwd``, ``hils_cache_reserve``, ``hils_cache_fork``,
+``hils_cache_free``, ``hils_cache_compact``, ``hils_workspace_size``, ``hils_prefill_record_cap``, ``hils_last_error``, ``hils_version``).
 They take torch tensors already resident on the GPU, check dtype, shape,
 device and contiguity, allocate missing outputs and the workspace with
 ``torch.empty`` and pass raw pointers plus the current HIP stream.  Every step
@@ -32,6 +33,7 @@ HILS_FLAG_HEAD_NORM_SELECT = 4
 HILS_FLAG_UNION_PACKING = 8
 HILS_OP_PREFILL, HILS_OP_DECODE, HILS_OP_BWD, HILS_OP_LANDMARK = 0, 1, 2, 3
 HILS_OP_DECODE_Q8, HILS_OP_Q8_APPEND, HILS_OP_Q8_LANDMARK, HILS_OP_CACHE_EVICT = 4, 5, 6, 7
+HILS_OP_PREFILL_PAGED, HILS_OP_CACHE_RESERVE, HILS_OP_CACHE_FORK, HILS_OP_CACHE_FREE, HILS_OP_CACHE_COMPACT = 8, 9, 10, 11, 12
 
 
 class HilsError(RuntimeError):
@@ -45,6 +47,10 @@ class hils_params(ctypes.Structure):
                 ("N", ctypes.c_int), ("L", ctypes.c_int), ("d", ctypes.c_int), ("chunk", ctypes.c_int),
                 ("topk", ctypes.c_int), ("window", ctypes.c_int), ("scale", ctypes.c_float),
                 ("dtype", ctypes.c_int), ("flags", ctypes.c_uint)]
+
+
+class hils_pool(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("page_bytes", ctypes.c_size_t)]
 
 
 def _load():
@@ -68,6 +74,12 @@ def _load():
     lib.hils_q8_landmark_fwd.argtypes = [P, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp]
     lib.hils_decode_q8_fwd.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.hils_cache_evict.argtypes = [P, vp, vp, vp, vp, vp, ci, ci, ci, vp, vp, vp, vp, vp, vp]
+    lib.hils_prefill_paged_fwd.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    pools = ctypes.POINTER(hils_pool)
+    lib.hils_cache_reserve.argtypes = [P, vp, vp, ci, vp, vp, pools, ci, vp, vp, vp, vp, vp]
+    lib.hils_cache_fork.argtypes = [P, vp, ci, vp, vp, ci, vp, vp, vp, vp, vp]
+    lib.hils_cache_free.argtypes = [P, vp, vp, vp, ci, vp, vp, ci, vp, vp, vp, vp, vp]
+    lib.hils_cache_compact.argtypes = [P, vp, vp, ci, vp, pools, ci, vp, vp, vp, vp, vp, vp]
     lib.hils_prefill_record_cap.argtypes = [sz]
     lib.hils_prefill_record_cap.restype = sz
     lib.hils_timing_enable.argtypes = [ctypes.c_int]
@@ -76,7 +88,8 @@ def _load():
     for f in (lib.hils_workspace_size, lib.hils_prefill_fwd, lib.hils_decode_fwd, lib.hils_decode_fwd_noalloc,
               lib.hils_bwd,
               lib.hils_landmark_fwd, lib.hils_landmark_bwd, lib.hils_q8_append, lib.hils_q8_landmark_fwd,
-              lib.hils_decode_q8_fwd, lib.hils_cache_evict, lib.hils_timing_enable, lib.hils_timing_read):
+              lib.hils_decode_q8_fwd, lib.hils_cache_evict, lib.hils_prefill_paged_fwd, lib.hils_cache_reserve,
+              lib.hils_cache_fork, lib.hils_cache_free, lib.hils_cache_compact, lib.hils_timing_enable, lib.hils_timing_read):
         f.restype = ctypes.c_int
     return lib
 
@@ -497,6 +510,161 @@ def hils_cache_evict(p: Params, acc, block_table, seqlens=None, budget=0, sink=0
          _address(seqlens_out, "seqlens_out", (B,), _I32, dev), _address(freed, "freed", (B, most), _I32, dev),
          _address(nfreed, "nfreed", (B,), _I32, dev))
     return acc_out, table_out, seqlens_out, freed, nfreed
+
+
+def hils_prefill_paged_fwd(p: Params, q, k_pages, v_pages, lmk_pages, block_table, bias_pages=None, q_route=None,
+                           seqlens=None, newlens=None, out=None, lse=None, idx=None, workspace=None):
+    """Attention of a chunk of new tokens over paged pools (as hils_decode_paged_fwd's): row n < newlens[b] of
+    q [B, Hq, N, d] is the query at position seqlens[b] - newlens[b] + n; other rows are neither read nor
+    written.  Returns (out, lse, idx)."""
+    dev, dt, B, Hq, H, N, d, S = _gpu(q, "q"), p.torch_dtype, p.B, p.Hq, p.Hkv, p.N, p.d, p.chunk
+    n, Hl, qs, K = _pages(k_pages, "k_pages"), p.Hl or p.Hq, (B, Hq, N, d), p.topk
+    on = q.device
+    if out is None:
+        out = torch.empty(qs, dtype=dt, device=on)
+    if lse is None:
+        lse = torch.empty((B, Hq, N), dtype=_F32, device=on)
+    if idx is None:
+        if p.flags & HILS_FLAG_GIVEN_IDX:
+            raise ValueError("HILS_FLAG_GIVEN_IDX needs idx")
+        idx = torch.empty((B, H, N, K), dtype=_I32, device=on)
+    if workspace is None:
+        workspace = torch.empty(max(1, hils_workspace_size(p, HILS_OP_PREFILL_PAGED)), dtype=torch.uint8, device=on)
+    nbytes = workspace.numel() if isinstance(workspace, torch.Tensor) else 0  # the library says if that is too little
+    _run(LIB.hils_prefill_paged_fwd, dev, ctypes.byref(p.c()), _address(q, "q", qs, dt, dev),
+         _address(k_pages, "k_pages", (n, H, S, d), dt, dev), _address(v_pages, "v_pages", (n, H, S, d), dt, dev),
+         _address(lmk_pages, "lmk_pages", (n, Hl, d), dt, dev),
+         None if bias_pages is None else _address(bias_pages, "bias_pages", (n, Hl), _F32, dev),
+         None if q_route is None else _address(q_route, "q_route", qs, dt, dev),
+         _address(block_table, "block_table", (B, p.L // S), _I32, dev), n,
+         None if seqlens is None else _address(seqlens, "seqlens", (B,), _I32, dev),
+         None if newlens is None else _address(newlens, "newlens", (B,), _I32, dev), _address(out, "out", qs, dt, dev),
+         _address(lse, "lse", (B, Hq, N), _F32, dev), _address(idx, "idx", (B, H, N, K), _I32, dev),
+         _address(workspace, "workspace", (nbytes,), torch.uint8, dev), nbytes)
+    return out, lse, idx
+
+
+# ---- the pages of a cache as a resource: block_table [B, L/S], seqlens [B] and page_refs [P] (how many table
+# entries name a page; 0: free) are int32; pools are the tensors that the table indexes, [P, ...] of any type.
+
+
+def _pool_list(pools, P, dev):
+    pools = tuple(pools)
+    arr = (hils_pool * max(1, len(pools)))()
+    for i, t in enumerate(pools):
+        if _gpu(t, f"pools[{i}]") != dev or t.dim() == 0 or t.shape[0] != P or not t.is_contiguous():
+            raise ValueError(f"pools[{i}] must be a contiguous tensor of {P} pages on cuda:{dev}")
+        arr[i].data, arr[i].page_bytes = t.data_ptr(), t.nbytes // P
+    return arr, len(pools)
+
+
+def _refs(page_refs):
+    dev = _gpu(page_refs, "page_refs")
+    if page_refs.dim() != 1:
+        raise ValueError(f"page_refs has shape {tuple(page_refs.shape)}, expected one dimension")
+    return dev, page_refs.shape[0]
+
+
+def hils_cache_reserve(p: Params, block_table, page_refs, pools=(), seqlens=None, newlens=None, table_out=None,
+                       refs_out=None, copied=None, counts=None):
+    """Give every sequence pages for its last newlens[b] tokens (which seqlens counts), before they are written: a
+    free page for each chunk that begins, a copy (in all ``pools``) of a begun page that others have too.
+    Returns (block_table, page_refs, copied [B, 2], counts [2]); counts = (pages needed, free pages found), and
+    nothing has been done unless both are equal.  In place if the outputs are the inputs."""
+    dev, P = _refs(page_refs)
+    shape, on = (p.B, p.L // p.chunk), page_refs.device
+    if table_out is None:
+        table_out = torch.empty(shape, dtype=_I32, device=on)
+    if refs_out is None:
+        refs_out = torch.empty(P, dtype=_I32, device=on)
+    if copied is None:
+        copied = torch.empty((p.B, 2), dtype=_I32, device=on)
+    if counts is None:
+        counts = torch.empty(2, dtype=_I32, device=on)
+    arr, n = _pool_list(pools, P, dev)
+    _run(LIB.hils_cache_reserve, dev, ctypes.byref(p.c()), _address(block_table, "block_table", shape, _I32, dev),
+         _address(page_refs, "page_refs", (P,), _I32, dev), P,
+         None if seqlens is None else _address(seqlens, "seqlens", (p.B,), _I32, dev),
+         None if newlens is None else _address(newlens, "newlens", (p.B,), _I32, dev), arr, n,
+         _address(table_out, "table_out", shape, _I32, dev), _address(refs_out, "refs_out", (P,), _I32, dev),
+         _address(copied, "copied", (p.B, 2), _I32, dev), _address(counts, "counts", (2,), _I32, dev))
+    return table_out, refs_out, copied, counts
+
+
+def hils_cache_fork(p: Params, parent, block_table, page_refs, seqlens=None, table_out=None, seqlens_out=None,
+                    refs_out=None):
+    """Rows that go on from rows ``parent`` [rows] int32 (outside [0, B): empty rows): they share their pages.  Rows
+    of the input that nobody goes on from are freed.  Returns (block_table [rows, L/S], seqlens [rows], page_refs);
+    only the last may be written in place."""
+    dev, P = _refs(page_refs)
+    if not isinstance(parent, torch.Tensor) or parent.dim() != 1:
+        raise ValueError("parent must be a GPU tensor of one dimension")
+    rows, C, on = parent.shape[0], p.L // p.chunk, page_refs.device
+    if table_out is None:
+        table_out = torch.empty((rows, C), dtype=_I32, device=on)
+    if seqlens_out is None:
+        seqlens_out = torch.empty(rows, dtype=_I32, device=on)
+    if refs_out is None:
+        refs_out = torch.empty(P, dtype=_I32, device=on)
+    _run(LIB.hils_cache_fork, dev, ctypes.byref(p.c()), _address(parent, "parent", (rows,), _I32, dev), rows,
+         _address(block_table, "block_table", (p.B, C), _I32, dev), _address(page_refs, "page_refs", (P,), _I32, dev), P,
+         None if seqlens is None else _address(seqlens, "seqlens", (p.B,), _I32, dev),
+         _address(table_out, "table_out", (rows, C), _I32, dev), _address(seqlens_out, "seqlens_out", (rows,), _I32, dev),
+         _address(refs_out, "refs_out", (P,), _I32, dev))
+    return table_out, seqlens_out, refs_out
+
+
+def hils_cache_free(p: Params, keep, block_table, page_refs, seqlens=None, pages=None, npages=None, table_out=None,
+                    seqlens_out=None, refs_out=None):
+    """Cut every sequence to its first keep[b] tokens and give up the pages past them, and those that ``pages``
+    [B, M] with ``npages`` [B] list (``freed`` and ``nfreed`` of hils_cache_evict).  Returns (block_table, seqlens,
+    page_refs); in place if the outputs are the inputs."""
+    dev, P = _refs(page_refs)
+    shape, on = (p.B, p.L // p.chunk), page_refs.device
+    if pages is not None and (not isinstance(pages, torch.Tensor) or pages.dim() != 2):
+        raise ValueError("pages must be a GPU tensor of two dimensions")
+    most = 0 if pages is None else pages.shape[1]
+    if table_out is None:
+        table_out = torch.empty(shape, dtype=_I32, device=on)
+    if seqlens_out is None:
+        seqlens_out = torch.empty(p.B, dtype=_I32, device=on)
+    if refs_out is None:
+        refs_out = torch.empty(P, dtype=_I32, device=on)
+    _run(LIB.hils_cache_free, dev, ctypes.byref(p.c()), _address(keep, "keep", (p.B,), _I32, dev),
+         None if pages is None else _address(pages, "pages", (p.B, most), _I32, dev),
+         None if npages is None else _address(npages, "npages", (p.B,), _I32, dev), most,
+         _address(block_table, "block_table", shape, _I32, dev), _address(page_refs, "page_refs", (P,), _I32, dev), P,
+         None if seqlens is None else _address(seqlens, "seqlens", (p.B,), _I32, dev),
+         _address(table_out, "table_out", shape, _I32, dev), _address(seqlens_out, "seqlens_out", (p.B,), _I32, dev),
+         _address(refs_out, "refs_out", (P,), _I32, dev))
+    return table_out, seqlens_out, refs_out
+
+
+def hils_cache_compact(p: Params, block_table, page_refs, pools=(), seqlens=None, table_out=None, refs_out=None,
+                       new_page=None, moved=None, counts=None):
+    """Move the used pages of all ``pools`` to the front, into the lowest free ones.  Returns (block_table, page_refs,
+    new_page [P], moved [P], counts [2]): new_page[i] is where page i is now (-1: it was free), ``moved`` lists the
+    pages that moved, counts = (pages in use, pages moved).  In place if the outputs are the inputs."""
+    dev, P = _refs(page_refs)
+    shape, on = (p.B, p.L // p.chunk), page_refs.device
+    if table_out is None:
+        table_out = torch.empty(shape, dtype=_I32, device=on)
+    if refs_out is None:
+        refs_out = torch.empty(P, dtype=_I32, device=on)
+    if new_page is None:
+        new_page = torch.empty(P, dtype=_I32, device=on)
+    if moved is None:
+        moved = torch.empty(P, dtype=_I32, device=on)
+    if counts is None:
+        counts = torch.empty(2, dtype=_I32, device=on)
+    arr, n = _pool_list(pools, P, dev)
+    _run(LIB.hils_cache_compact, dev, ctypes.byref(p.c()), _address(block_table, "block_table", shape, _I32, dev),
+         _address(page_refs, "page_refs", (P,), _I32, dev), P,
+         None if seqlens is None else _address(seqlens, "seqlens", (p.B,), _I32, dev), arr, n,
+         _address(table_out, "table_out", shape, _I32, dev), _address(refs_out, "refs_out", (P,), _I32, dev),
+         _address(new_page, "new_page", (P,), _I32, dev), _address(moved, "moved", (P,), _I32, dev),
+         _address(counts, "counts", (2,), _I32, dev))
+    return table_out, refs_out, new_page, moved, counts
 
 
 def hils_timing_enable(on: bool = True) -> None:
