@@ -139,7 +139,8 @@ size_t ws_bytes_for(const hils_params* p, int op) {
         case HILS_OP_CACHE_COMPACT:
             return 0;
         case HILS_OP_PREFILL_PAGED:
-            return hils::prefill_paged_workspace_bytes(p->B, p->Hq, p->Hkv, p->N, p->L, p->d, p->topk);
+            return hils::prefill_paged_workspace_bytes(p->B, p->Hq, p->Hkv, p->N, p->L, p->d, p->topk,
+                                                       p->dtype == HILS_BF16);
         default:
             return hils::prefill_workspace_bytes(p->B, p->Hq, p->Hkv, p->N, p->L, p->d, p->topk,
                                                  p->dtype == HILS_BF16,

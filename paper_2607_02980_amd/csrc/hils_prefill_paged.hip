@@ -120,6 +120,75 @@ __device__ __forceinline__ int dim_of(int db, int i, int lg) {
     return sizeof(T) == 2 ? 16 * db + 4 * lg + i : 64 * (db / 4) + 16 * lg + 4 * i + db % 4;
 }
 
+// Records: a chunk's output o_c for one (row, head), as the accumulators hold it, with s^ and a scale.
+// They are written once and read once, a pass's largest traffic, so that bf16 calls keep them in
+// float16, in units of the power of two below the vector's largest finite element: 2^-11 of that
+// at most is lost, a fraction of what rounding the weights to bf16 loses (in bf16, 2^-8, it would be
+// as much again).  f32 calls keep floats.
+template <typename T, int D>
+struct Record {
+    static constexpr int BYTES = sizeof(T) == 2 ? 2 * D : 4 * D;
+    static constexpr int PIECES = BYTES / 64;  // 16-byte pieces of a lane
+    uint4 x[PIECES];
+
+    __device__ __forceinline__ void load(const char* rec, int lg) {
+#pragma unroll
+        for (int t = 0; t < PIECES; ++t) x[t] = *reinterpret_cast<const uint4*>(rec + 64 * t + 16 * lg);
+    }
+    // acc = acc * rs + w * record (of which any bits are possible where w is to add nothing: ok)
+    __device__ __forceinline__ void add(f32x4 (&acc)[D / 16], float rs, float w, bool ok) const {
+#pragma unroll
+        for (int t = 0; t < PIECES; ++t) {
+            const uint4 y = ok ? x[t] : make_uint4(0, 0, 0, 0);
+            if constexpr (sizeof(T) == 2) {
+                typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+                const h8 h = __builtin_bit_cast(h8, y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    acc[2 * t + i / 4][i % 4] = fmaf((float)h[i], w, acc[2 * t + i / 4][i % 4] * rs);
+            } else {
+                const f32x4 h = __builtin_bit_cast(f32x4, y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(h[i], w, acc[t][i] * rs);
+            }
+        }
+    }
+    // Stores o * inv; the scale that the record is in units of.
+    static __device__ __forceinline__ float store(char* rec, const f32x4 (&o)[D / 16], float inv, int lg, bool live) {
+        if constexpr (sizeof(T) == 2) {
+            float top = 0.f;
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a = fabsf(o[db][i]);
+                    top = fmaxf(top, a < INFINITY ? a : 0.f);
+                }
+            top = group4_max(top * inv);
+            // 2^e <= top (2^-126 for less, 2^126 for more), and 2^-e
+            const uint32_t e = min(max(__float_as_uint(top) >> 23, 1u), 253u);
+            const float unit = __uint_as_float(e << 23), down = inv * __uint_as_float((254u - e) << 23);
+            if (live) {
+                typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+#pragma unroll
+                for (int t = 0; t < PIECES; ++t) {
+                    h8 h;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[i] = static_cast<_Float16>(o[2 * t + i / 4][i % 4] * down);
+                    *reinterpret_cast<h8*>(rec + 64 * t + 16 * lg) = h;
+                }
+            }
+            return unit;
+        } else {
+            if (live) {
+#pragma unroll
+                for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4*>(rec + 64 * db + 16 * lg) = o[db] * inv;
+            }
+            return 1.f;
+        }
+    }
+};
+
 // New tokens of a sequence: `fresh` of them, the last of `len`.
 struct Seq {
     int len, fresh, pos0;
@@ -143,8 +212,8 @@ struct Ws {
     int* list;     // [bg][Ns * K] row << 6 | slot
     int4* work;    // (bg, chunk, offset, rows)
     float* sigma;  // [bg][Rs][nC]
-    float* rec_s;  // [bg][Ns][K][G]
-    float* rec_o;  // [bg][Ns][K][G][D], as the accumulators hold them
+    float2* rec_s; // [bg][Ns][K][G] s^ and the record's unit
+    char* rec_o;   // [bg][Ns][K][G] records
 };
 struct Layout {
     size_t counts, offs, ranks, list, work, sigma, rec_s, rec_o, total;
@@ -155,10 +224,10 @@ struct Layout {
 // sigma of a block of rows: as many as fit the last-level cache, in whole score tiles
 constexpr size_t kSigmaBytes = size_t(128) << 20;
 
-Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K) {
+Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int bf16) {
     Layout w;
     const size_t nC = L / kChunk, bg = (size_t)B * Hkv;
-    const size_t per_row = (size_t)B * Hq * K * (d + 1) * sizeof(float);
+    const size_t rec = (bf16 ? 2 : 4) * (size_t)d, per_row = (size_t)B * Hq * K * (rec + sizeof(float2));
     const size_t cap = prefill_record_cap(0);
     size_t ns = N;
     if (ns * per_row > cap) ns = std::min<size_t>(N, std::max<size_t>(kScoreRows, cap / per_row / kScoreRows * kScoreRows));
@@ -179,8 +248,8 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K) {
     w.list = take(bg * ns * K * sizeof(int));
     w.work = take(w.max_work * sizeof(int4));
     w.sigma = take(bg * rs * nC * sizeof(float));
-    w.rec_s = take(bg * ns * K * (Hq / Hkv) * sizeof(float));
-    w.rec_o = take(bg * ns * K * (Hq / Hkv) * d * sizeof(float));
+    w.rec_s = take((size_t)B * Hq * ns * K * sizeof(float2));
+    w.rec_o = take((size_t)B * Hq * ns * K * rec);
     w.total = at;
     return w;
 }
@@ -526,13 +595,9 @@ __global__ __launch_bounds__(kChunkWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
             for (int db = 0; db < C::DB; ++db) o[db] = zero4();
             add_pv<T, D>(s_v, st, o, lane);
             const float inv = 1.f / sum;
-            if (live) {
-                const size_t rec = ((bg * Ns + n) * f.K + slot) * G + hh;
-#pragma unroll
-                for (int db = 0; db < C::DB; ++db)
-                    *reinterpret_cast<f32x4*>(ws.rec_o + rec * D + db * 16 + lg * 4) = o[db] * inv;
-                if (lg == 0) ws.rec_s[rec] = shat;
-            }
+            const size_t rec = ((bg * Ns + n) * f.K + slot) * G + hh;
+            const float unit = Record<T, D>::store(ws.rec_o + rec * Record<T, D>::BYTES, o, inv, lg, live);
+            if (live && lg == 0) ws.rec_s[rec] = make_float2(shat, unit);
         }
     }
 }
@@ -555,8 +620,8 @@ struct Tile {
 template <typename T, int D, int G>
 __global__ __launch_bounds__(kLocalWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k_pp_local(FwdArgs f,
                                                                                          const int32_t* newlens,
-                                                                                         const float* rec_s,
-                                                                                         const float* rec_o, int n0,
+                                                                                         const float2* rec_s,
+                                                                                         const char* rec_o, int n0,
                                                                                          int Ns) {
     using C = Cfg<T, D>;
     constexpr int NT = kLocalWaves * kWave, QT = Tile<G>::QT, WR = Tile<G>::WR;
@@ -642,15 +707,23 @@ __global__ __launch_bounds__(kLocalWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
             __builtin_amdgcn_sched_barrier(0);
         }
         const bool part = masked(j0);
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) st[kb] *= c1;
+        if (part) {
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = j0 + kb * 16 + lg * 4 + i;
+                    const bool sees = (j <= pos) & (j >= ell);
+                    st[kb][i] = sees ? st[kb][i] : -INFINITY;
+                }
+        }
         float mx = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int j = j0 + kb * 16 + lg * 4 + i;
-                st[kb][i] = !part || (j <= pos && j >= ell) ? st[kb][i] * c1 : -INFINITY;
-                mx = fmaxf(mx, st[kb][i]);
-            }
+            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, st[kb][i]);
         mx = group4_max(mx);
         const float mnew = fmaxf(m, mx), muse = mnew == -INFINITY ? 0.f : mnew;
         const float alpha = fexp2(m - muse);
@@ -668,21 +741,21 @@ __global__ __launch_bounds__(kLocalWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
 #pragma unroll
         for (int db = 0; db < C::DB; ++db) o[db] *= alpha;
         if (part && s_bad[buf] == j0) {  // uniform
+#pragma unroll 1
             for (int j = 0; j < kChunk; ++j) {
-                const int kb = j / 16, i = j % 4;
                 float mine = 0.f;
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) mine = kb == x && i == y ? st[x][y] : mine;
+                for (int x = 0; x < 16; ++x) mine = j / 16 * 4 + j % 4 == x ? st[x / 4][x % 4] : mine;
                 const float p = __shfl(mine, (j % 16) / 4 * 16 + col, kWave);
                 const bool sees = j0 + j <= pos && j0 + j >= ell;
                 const T* v = reinterpret_cast<const T*>(&s_v[buf][j * C::VROW]);
 #pragma unroll
-                for (int db = 0; db < C::DB; ++db)
+                for (int db = 0; db < C::DB; ++db) {
 #pragma unroll
                     for (int y = 0; y < 4; ++y)
                         o[db][y] = sees ? fmaf(p, to_f32(v[dim_of<T>(db, y, lg)]), o[db][y]) : o[db][y];
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
         } else {
             add_pv<T, D>(s_v[buf], st, o, lane);
@@ -700,25 +773,36 @@ __global__ __launch_bounds__(kLocalWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
     for (int db = 0; db < C::DB; ++db) o[db] *= inv_l;
     const int32_t* irow = f.idx + (bg * f.N + n) * f.K;
     const size_t rec0 = (bg * Ns + (n - n0)) * f.K;
+    constexpr int SB = D == 128 ? 2 : 4;  // slots in flight together
     int prev = -1;
-    for (int k = 0; k < f.K; ++k) {
-        const int c = irow[k];
-        const bool ok = c >= 0 && c < ncand && c > prev;  // as idx_entry_valid
-        prev = c;
-        if (__ballot(ok) == 0ull) continue;
-        const size_t rec = (rec0 + k) * G + hh;
-        const float s = ok ? rec_s[rec] : -INFINITY;
-        const bool adds = s != -INFINITY;  // (a masked chunk's record may hold anything)
-        const float Mn = adds ? fmaxf(M, s) : M;
-        const float rs = Mn == M ? 1.f : fexp(M - Mn), wk = adds ? fexp(s - Mn) : 0.f;
+    for (int k0 = 0; k0 < f.K; k0 += SB) {
+        Record<T, D> r[SB];
+        float2 sv[SB];
+        bool ok[SB];
+#pragma unroll
+        for (int u = 0; u < SB; ++u) {
+            const int k = min(k0 + u, f.K - 1), c = irow[k];
+            const size_t rec = (rec0 + k) * G + hh;
+            sv[u] = rec_s[rec];  // (addresses that do not depend on c, so that all loads are issued at once)
+            r[u].load(rec_o + rec * Record<T, D>::BYTES, lg);
+            ok[u] = (k0 + u < f.K) & (c >= 0) & (c < ncand) & (c > prev);  // as idx_entry_valid
+            prev = c;
+        }
+        float Mn = M;
+#pragma unroll
+        for (int u = 0; u < SB; ++u) {
+            ok[u] = ok[u] && sv[u].x != -INFINITY;  // (a masked chunk's record may hold anything)
+            Mn = ok[u] ? fmaxf(Mn, sv[u].x) : Mn;
+        }
+        float rs = Mn == M ? 1.f : fexp(M - Mn);
         M = Mn;
-        zs = zs * rs + wk;
+        zs *= rs;
 #pragma unroll
-        for (int db = 0; db < C::DB; ++db) {
-            f32x4 x = zero4();
-            if (adds) x = *reinterpret_cast<const f32x4*>(rec_o + rec * D + db * 16 + lg * 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[db][i] = fmaf(wk, x[i], o[db][i] * rs);
+        for (int u = 0; u < SB; ++u) {
+            const float wk = ok[u] ? fexp(sv[u].x - M) : 0.f;
+            zs += wk;
+            r[u].add(o, rs, ok[u] ? wk * sv[u].y : 0.f, ok[u]);
+            rs = 1.f;
         }
     }
     if (!live) return;
@@ -742,7 +826,7 @@ struct Run {
     template <typename T, int D, int G>
     static hipError_t run(const PrefillPagedArgs& a, hipStream_t s) {
         const FwdArgs& f = a.f;
-        const Layout ly = layout(f.B, f.Hq, f.Hkv, f.N, f.L, D, f.K);
+        const Layout ly = layout(f.B, f.Hq, f.Hkv, f.N, f.L, D, f.K, f.bf16);
         char* base = static_cast<char*>(f.ws);
         Ws ws;
         ws.counts = reinterpret_cast<int*>(base + ly.counts);
@@ -751,8 +835,8 @@ struct Run {
         ws.list = reinterpret_cast<int*>(base + ly.list);
         ws.work = reinterpret_cast<int4*>(base + ly.work);
         ws.sigma = reinterpret_cast<float*>(base + ly.sigma);
-        ws.rec_s = reinterpret_cast<float*>(base + ly.rec_s);
-        ws.rec_o = reinterpret_cast<float*>(base + ly.rec_o);
+        ws.rec_s = reinterpret_cast<float2*>(base + ly.rec_s);
+        ws.rec_o = base + ly.rec_o;
         const int nC = f.L / kChunk, maxc = n_candidates(f.L - 1, f.W);  // candidates of any row, at most
         const size_t bg = (size_t)f.B * f.Hkv, ncount = bg * nC;
         const int cus = device_cus();
@@ -797,7 +881,7 @@ struct Run {
             }
             const int ntiles = (Ns + Tile<G>::QT - 1) / Tile<G>::QT;
             HILS_LAUNCH("k_pp_local", (k_pp_local<T, D, G>), dim3((unsigned)(bg * ntiles)), dim3(kLocalWaves * kWave), 0,
-                        s, f, a.newlens, (const float*)ws.rec_s, (const float*)ws.rec_o, n0, Ns);
+                        s, f, a.newlens, (const float2*)ws.rec_s, (const char*)ws.rec_o, n0, Ns);
         }
         return hipGetLastError();
     }
@@ -805,8 +889,8 @@ struct Run {
 
 }  // namespace
 
-size_t prefill_paged_workspace_bytes(int B, int Hq, int Hkv, int N, int L, int d, int K) {
-    return layout(B, Hq, Hkv, N, L, d, K).total;
+size_t prefill_paged_workspace_bytes(int B, int Hq, int Hkv, int N, int L, int d, int K, int bf16) {
+    return layout(B, Hq, Hkv, N, L, d, K, bf16).total;
 }
 
 hipError_t launch_prefill_paged(const PrefillPagedArgs& a, hipStream_t s) {
