@@ -27,6 +27,7 @@
 // 16-byte reads that each feed four products, accumulator [4 dd + j][i] being dim
 // 64 dd + 16 lg + 4 i + j (f32; lg = l / 16 of lane l).
 #include <algorithm>
+#include <type_traits>
 
 #include "hils_device.hpp"
 #include "hils_dispatch.hpp"
@@ -611,18 +612,19 @@ struct Tile {
     static constexpr int QT = WR * kLocalWaves;  // rows of a workgroup
 };
 
-// The 64-key blocks of the tile's windows are double-buffered in LDS; then each row's records
-// are added, every (row, head) stabilised by its own maximum M of log Z_swa and the s^:
-//   out = (e^{log Z_swa - M} o_swa + sum_k e^{s^_k - M} o_k) / (e^{log Z_swa - M} + sum_k e^{s^_k - M})
+// Of the fusion's softmax a record is one more key, with logit s^ and value o_c, so that window and
+// records go through one running (maximum, sum, numerator) per (row, head), in either order.  The
+// window keeps the matrix cores busy (its 64-key blocks are double-buffered in LDS and shared
+// by the waves), the records the memory; workgroups that share a CU take them in opposite order.
 // Rows of V at or past the length are staged as zeros (nobody has written them).  Where a block
 // holds an infinity or a NaN among values that some row of the tile must not see, 0 * it
 // would reach that row: such a block's values are added one key at a time.
 template <typename T, int D, int G>
-__global__ __launch_bounds__(kLocalWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k_pp_local(FwdArgs f,
+__global__ __launch_bounds__(kLocalWaves * kWave, D * sizeof(T) <= 256 ? 4 : 2) void k_pp_local(FwdArgs f,
                                                                                          const int32_t* newlens,
                                                                                          const float2* rec_s,
                                                                                          const char* rec_o, int n0,
-                                                                                         int Ns) {
+                                                                                         int Ns, int cus) {
     using C = Cfg<T, D>;
     constexpr int NT = kLocalWaves * kWave, QT = Tile<G>::QT, WR = Tile<G>::WR;
     constexpr int PPT = kChunk * D * C::ES / 16 / NT;
@@ -648,6 +650,8 @@ __global__ __launch_bounds__(kLocalWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
     const size_t row = ((size_t)b * f.Hq + g * G + hh) * f.N + n;
     const float c1 = f.scale * kLog2e;
     if (tid < 2) s_bad[tid] = -1;
+    // (not by the tile's place in the launch: the same bits however the rows are cut)
+    const bool records_first = (q0 / QT + (size_t)b * ((f.N + QT - 1) / QT)) * f.Hkv / cus % 2;
 
     struct KV {
         uint4 k[PPT], v[PPT];
@@ -689,124 +693,140 @@ __global__ __launch_bounds__(kLocalWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
 #pragma unroll
     for (int db = 0; db < C::DB; ++db) o[db] = zero4();
     float m = -INFINITY, l = 0.f;  // running maximum (log2 units) and sum
-    __syncthreads();               // s_bad is set
-    KV nx = fetch(kbeg);
-    stage(0, kbeg, nx);
-    __syncthreads();
-    int buf = 0;
-    for (int j0 = kbeg; j0 <= klast; j0 += kChunk, buf ^= 1) {
-        const bool more = j0 + kChunk <= klast;  // uniform
-        if (more) nx = fetch(j0 + kChunk);
-        f32x4 st[4];
+    auto records = [&] {
+        // the row's records, slots in idx order (lane: its column's dims)
+        const int32_t* irow = f.idx + (bg * f.N + n) * f.K;
+        const size_t rec0 = (bg * Ns + (n - n0)) * f.K;
+        constexpr int SB = D == 128 ? 2 : 4;  // slots in flight together
+        int prev = -1;
+        for (int k0 = 0; k0 < f.K; k0 += SB) {
+            Record<T, D> r[SB];
+            float2 sv[SB];
+            bool ok[SB];
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            st[kb] = zero4();
+            for (int u = 0; u < SB; ++u) {
+                const int k = min(k0 + u, f.K - 1), c = irow[k];
+                const size_t rec = (rec0 + k) * G + hh;
+                sv[u] = rec_s[rec];  // (addresses that do not depend on c, so that all loads are issued at once)
+                r[u].load(rec_o + rec * Record<T, D>::BYTES, lg);
+                ok[u] = (k0 + u < f.K) & (c >= 0) & (c < ncand) & (c > prev);  // as idx_entry_valid
+                prev = c;
+            }
+            float mnew = m;
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks)
-                st[kb] = mma<T>(lds16(&s_k[buf][(kb * 16 + col) * C::KROW + ks * 64 + lg * 16]), q[ks], st[kb]);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int u = 0; u < SB; ++u) {
+                ok[u] = ok[u] && sv[u].x != -INFINITY;  // (a masked chunk's record may hold anything)
+                sv[u].x *= kLog2e;
+                mnew = ok[u] ? fmaxf(mnew, sv[u].x) : mnew;
+            }
+            float rs = mnew == m ? 1.f : fexp2(m - mnew);
+            m = mnew;
+            l *= rs;
+#pragma unroll
+            for (int u = 0; u < SB; ++u) {
+                const float wk = ok[u] ? fexp2(sv[u].x - m) : 0.f;
+                l += wk;
+                r[u].add(o, rs, ok[u] ? wk * sv[u].y : 0.f, ok[u]);
+                rs = 1.f;
+            }
         }
-        const bool part = masked(j0);
+    };
+    bool seen_bad = false;  // uniform
+    auto window = [&](auto careful_tag) {
+        constexpr bool careful = decltype(careful_tag)::value;
+        KV nx = fetch(kbeg);
+        stage(0, kbeg, nx);
+        __syncthreads();
+        int buf = 0;
+        for (int j0 = kbeg; j0 <= klast; j0 += kChunk, buf ^= 1) {
+            const bool more = j0 + kChunk <= klast;  // uniform
+            if (more) nx = fetch(j0 + kChunk);
+            f32x4 st[4];
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) st[kb] *= c1;
-        if (part) {
+            for (int kb = 0; kb < 4; ++kb) {
+                st[kb] = zero4();
+#pragma unroll
+                for (int ks = 0; ks < C::KS; ++ks)
+                    st[kb] = mma<T>(lds16(&s_k[buf][(kb * 16 + col) * C::KROW + ks * 64 + lg * 16]), q[ks], st[kb]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const bool part = masked(j0);
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) st[kb] *= c1;
+            if (part) {
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = j0 + kb * 16 + lg * 4 + i;
+                        const bool sees = (j <= pos) & (j >= ell);
+                        st[kb][i] = sees ? st[kb][i] : -INFINITY;
+                    }
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, st[kb][i]);
+            mx = group4_max(mx);
+            const float mnew = fmaxf(m, mx), muse = mnew == -INFINITY ? 0.f : mnew;
+            const float alpha = fexp2(m - muse);
+            float psum = 0.f;
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int j = j0 + kb * 16 + lg * 4 + i;
-                    const bool sees = (j <= pos) & (j >= ell);
-                    st[kb][i] = sees ? st[kb][i] : -INFINITY;
+                    st[kb][i] = fexp2(st[kb][i] - muse);
+                    psum += st[kb][i];
                 }
-        }
-        float mx = -INFINITY;
+            psum = group4_sum(psum);
+            l = l * alpha + psum;
+            m = mnew;
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, st[kb][i]);
-        mx = group4_max(mx);
-        const float mnew = fmaxf(m, mx), muse = mnew == -INFINITY ? 0.f : mnew;
-        const float alpha = fexp2(m - muse);
-        float psum = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                st[kb][i] = fexp2(st[kb][i] - muse);
-                psum += st[kb][i];
-            }
-        psum = group4_sum(psum);
-        l = l * alpha + psum;
-        m = mnew;
-#pragma unroll
-        for (int db = 0; db < C::DB; ++db) o[db] *= alpha;
-        if (part && s_bad[buf] == j0) {  // uniform
+            for (int db = 0; db < C::DB; ++db) o[db] *= alpha;
+            if (careful && part && s_bad[buf] == j0) {  // uniform
 #pragma unroll 1
-            for (int j = 0; j < kChunk; ++j) {
-                float mine = 0.f;
+                for (int j = 0; j < kChunk; ++j) {
+                    float mine = 0.f;
 #pragma unroll
-                for (int x = 0; x < 16; ++x) mine = j / 16 * 4 + j % 4 == x ? st[x / 4][x % 4] : mine;
-                const float p = __shfl(mine, (j % 16) / 4 * 16 + col, kWave);
-                const bool sees = j0 + j <= pos && j0 + j >= ell;
-                const T* v = reinterpret_cast<const T*>(&s_v[buf][j * C::VROW]);
+                    for (int x = 0; x < 16; ++x) mine = j / 16 * 4 + j % 4 == x ? st[x / 4][x % 4] : mine;
+                    const float p = __shfl(mine, (j % 16) / 4 * 16 + col, kWave);
+                    const bool sees = j0 + j <= pos && j0 + j >= ell;
+                    const T* v = reinterpret_cast<const T*>(&s_v[buf][j * C::VROW]);
 #pragma unroll
-                for (int db = 0; db < C::DB; ++db) {
+                    for (int db = 0; db < C::DB; ++db) {
 #pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        o[db][y] = sees ? fmaf(p, to_f32(v[dim_of<T>(db, y, lg)]), o[db][y]) : o[db][y];
-                    __builtin_amdgcn_sched_barrier(0);
+                        for (int y = 0; y < 4; ++y)
+                            o[db][y] = sees ? fmaf(p, to_f32(v[dim_of<T>(db, y, lg)]), o[db][y]) : o[db][y];
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
+            } else {
+                add_pv<T, D>(s_v[buf], st, o, lane);
             }
-        } else {
-            add_pv<T, D>(s_v[buf], st, o, lane);
+            seen_bad |= part && s_bad[buf] == j0;
+            if (more) stage(buf ^ 1, j0 + kChunk, nx);
+            __syncthreads();
         }
-        if (more) stage(buf ^ 1, j0 + kChunk, nx);
-        __syncthreads();
+    };
+    __syncthreads();  // s_bad is set
+    if (records_first) {
+        records();
+        window(std::false_type{});
+    } else {
+        window(std::false_type{});
+        records();
     }
-
-    // the fusion (lane: its column's dims), slots in idx order
-    // (the query's own key is in its window; l is 0 only where every key scores -inf)
-    const float lam0 = l > 0.f ? (m + __log2f(l)) * (1.f / kLog2e) : -INFINITY;
-    float M = lam0, zs = l > 0.f ? 1.f : 0.f;
-    const float inv_l = l > 0.f ? 1.f / l : 0.f;
+    if (seen_bad) {  // (once more, apart from the usual way, whose registers it would take)
 #pragma unroll
-    for (int db = 0; db < C::DB; ++db) o[db] *= inv_l;
-    const int32_t* irow = f.idx + (bg * f.N + n) * f.K;
-    const size_t rec0 = (bg * Ns + (n - n0)) * f.K;
-    constexpr int SB = D == 128 ? 2 : 4;  // slots in flight together
-    int prev = -1;
-    for (int k0 = 0; k0 < f.K; k0 += SB) {
-        Record<T, D> r[SB];
-        float2 sv[SB];
-        bool ok[SB];
-#pragma unroll
-        for (int u = 0; u < SB; ++u) {
-            const int k = min(k0 + u, f.K - 1), c = irow[k];
-            const size_t rec = (rec0 + k) * G + hh;
-            sv[u] = rec_s[rec];  // (addresses that do not depend on c, so that all loads are issued at once)
-            r[u].load(rec_o + rec * Record<T, D>::BYTES, lg);
-            ok[u] = (k0 + u < f.K) & (c >= 0) & (c < ncand) & (c > prev);  // as idx_entry_valid
-            prev = c;
-        }
-        float Mn = M;
-#pragma unroll
-        for (int u = 0; u < SB; ++u) {
-            ok[u] = ok[u] && sv[u].x != -INFINITY;  // (a masked chunk's record may hold anything)
-            Mn = ok[u] ? fmaxf(Mn, sv[u].x) : Mn;
-        }
-        float rs = Mn == M ? 1.f : fexp(M - Mn);
-        M = Mn;
-        zs *= rs;
-#pragma unroll
-        for (int u = 0; u < SB; ++u) {
-            const float wk = ok[u] ? fexp(sv[u].x - M) : 0.f;
-            zs += wk;
-            r[u].add(o, rs, ok[u] ? wk * sv[u].y : 0.f, ok[u]);
-            rs = 1.f;
-        }
+        for (int db = 0; db < C::DB; ++db) o[db] = zero4();
+        m = -INFINITY;
+        l = 0.f;
+        window(std::true_type{});
+        records();
     }
     if (!live) return;
-    const float inv = 1.f / zs;
+    const float inv = 1.f / l;  // (the query's own key is in its window: l is 0 only where all logits are -inf)
     T* out = as_mut<T>(f.out) + row * D;
 #pragma unroll
     for (int db = 0; db < C::DB; ++db) {
@@ -819,7 +839,7 @@ __global__ __launch_bounds__(kLocalWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
             __builtin_memcpy(out + 64 * dd + 16 * lg + 4 * i, &r, 16);
         }
     }
-    if (lg == 0) f.lse[row] = M + __logf(zs);
+    if (lg == 0) f.lse[row] = (m + __log2f(l)) * (1.f / kLog2e);
 }
 
 struct Run {
@@ -881,7 +901,7 @@ struct Run {
             }
             const int ntiles = (Ns + Tile<G>::QT - 1) / Tile<G>::QT;
             HILS_LAUNCH("k_pp_local", (k_pp_local<T, D, G>), dim3((unsigned)(bg * ntiles)), dim3(kLocalWaves * kWave), 0,
-                        s, f, a.newlens, (const float2*)ws.rec_s, (const char*)ws.rec_o, n0, Ns);
+                        s, f, a.newlens, (const float2*)ws.rec_s, (const char*)ws.rec_o, n0, Ns, cus);
         }
         return hipGetLastError();
     }
