@@ -140,7 +140,7 @@ size_t ws_bytes_for(const hils_params* p, int op) {
             return 0;
         case HILS_OP_PREFILL_PAGED:
             return hils::prefill_paged_workspace_bytes(p->B, p->Hq, p->Hkv, p->N, p->L, p->d, p->topk,
-                                                       p->dtype == HILS_BF16);
+                                                       p->window, p->dtype == HILS_BF16);
         default:
             return hils::prefill_workspace_bytes(p->B, p->Hq, p->Hkv, p->N, p->L, p->d, p->topk,
                                                  p->dtype == HILS_BF16,

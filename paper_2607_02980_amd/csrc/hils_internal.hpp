@@ -266,7 +266,7 @@ hipError_t launch_q8_decode_bf16_d128(const Q8DecodeArgs& a, hipStream_t s);
 hipError_t launch_q8_decode_f32_d64(const Q8DecodeArgs& a, hipStream_t s);
 hipError_t launch_q8_decode_f32_d128(const Q8DecodeArgs& a, hipStream_t s);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
-size_t prefill_paged_workspace_bytes(int B, int Hq, int Hkv, int N, int L, int d, int K, int bf16);
+size_t prefill_paged_workspace_bytes(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf16);
 hipError_t launch_prefill_paged(const PrefillPagedArgs& a, hipStream_t s);
 hipError_t launch_reserve(const ReserveArgs& a, const PoolArg* pools, int num_pools, hipStream_t s);
 hipError_t launch_fork(const ForkArgs& a, hipStream_t s);

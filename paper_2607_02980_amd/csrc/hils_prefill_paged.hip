@@ -8,12 +8,14 @@
 //   k_pp_select   the K best of each row (exact radix select, ties to the smaller chunk); each
 //                 chosen chunk counts the row and gives it a rank
 //   k_pp_plan     per (b, g): where each chunk's rows start, and the work items
-//   k_pp_fill     the rows of every chunk, by offset and rank
+//   k_pp_fill     the rows of every chunk, by offset and rank (few rows: k_pp_plan does it)
 //   k_pp_chunks   chunk-major: a chunk's K and V are read once and attended by all the rows that
 //                 chose it, 16 (row, head) columns at a time; o_c and s^ of every (row, slot,
 //                 head) go to the workspace as records
 //   k_pp_local    the window [l(i), i] of 16 * 8 / G rows x G heads per workgroup, and the
 //                 fusion with the records
+//   k_pp_join     instead, where there are few rows: the blocks of the windows have been work items
+//                 of k_pp_chunks too, and only records are left to be added up
 //
 // A row is computed the same way wherever the rows are cut; the order of a chunk's rows, which
 // depends on atomics, decides only which of them share a matrix instruction, and columns of one
@@ -38,12 +40,15 @@ namespace hils {
 
 namespace {
 
-constexpr int kScoreWaves = 8;
-constexpr int kScoreRows = 16 * kScoreWaves;  // rows of a score tile
+// Waves of a score tile, 16 rows each (f32: its products take 8 times as long, and short calls have few tiles).
+constexpr int score_waves(bool bf16) { return bf16 ? 8 : 4; }
+constexpr int kScoreRows = 16 * score_waves(true);
 constexpr int kScoreCand = 64;                // candidates of a staged landmark block
 constexpr int kSelWaves = 4;
 constexpr int kChunkWaves = 4;
-constexpr int kSegRows = 64;                  // rows of a work item, at most
+// Rows of a work item, at most.  f32: 128 columns, as 16 of them take a wave 3 us (an item of 64 rows x 8 heads
+// alone 25 us).
+constexpr int seg_rows(bool bf16, int G) { return bf16 ? 64 : std::min(64, 128 / G); }
 constexpr int kLocalWaves = 8;
 
 // 16 bytes of global memory of which only the elements' alignment is known (one instruction).
@@ -121,6 +126,43 @@ __device__ __forceinline__ int dim_of(int db, int i, int lg) {
     return sizeof(T) == 2 ? 16 * db + 4 * lg + i : 64 * (db / 4) + 16 * lg + 4 * i + db % 4;
 }
 
+// No infinity or NaN among the elements of a 16-byte piece.
+template <typename T>
+__device__ __forceinline__ bool all_finite(const uint4& v) {
+    const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+    bool ok = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        ok &= (y[i] & 0x7f800000u) != 0x7f800000u;
+        if constexpr (sizeof(T) == 2) ok &= (y[i] & 0x7f80u) != 0x7f80u;
+    }
+    return ok;
+}
+
+// add_pv one key at a time, for a block with values that are not finite: keys past `last` or before `first`
+// (of the column's row) are left out, where 0 times them would not be.
+template <typename T, int D>
+__device__ __forceinline__ void add_pv_by_key(const char* s_v, const f32x4 (&st)[4], f32x4 (&o)[D / 16], int lane,
+                                              int last, int first) {
+    using C = Cfg<T, D>;
+#pragma unroll 1
+    for (int j = 0; j < kChunk; ++j) {
+        float mine = 0.f;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) mine = j / 16 * 4 + j % 4 == x ? st[x / 4][x % 4] : mine;
+        const float p = __shfl(mine, (j % 16) / 4 * 16 + lane % 16, kWave);
+        const bool sees = (j <= last) & (j >= first);
+        const T* v = reinterpret_cast<const T*>(s_v + j * C::VROW);
+#pragma unroll
+        for (int db = 0; db < C::DB; ++db) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                o[db][y] = sees ? fmaf(p, to_f32(v[dim_of<T>(db, y, lane / 16)]), o[db][y]) : o[db][y];
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
 // Records: a chunk's output o_c for one (row, head), as the accumulators hold it, with s^ and a scale.
 // They are written once and read once, a pass's largest traffic, so that bf16 calls keep them in
 // float16, in units of the power of two below the vector's largest finite element: 2^-11 of that
@@ -190,6 +232,29 @@ struct Record {
     }
 };
 
+// Adds NR records to a running softmax (maximum m in log2 units, sum l, numerator o).
+template <typename T, int D, int NR>
+__device__ __forceinline__ void add_records(const Record<T, D> (&r)[NR], const float2 (&sv)[NR], const bool (&valid)[NR],
+                                            f32x4 (&o)[D / 16], float& m, float& l) {
+    bool ok[NR];
+    float mnew = m;
+#pragma unroll
+    for (int u = 0; u < NR; ++u) {
+        ok[u] = valid[u] && sv[u].x != -INFINITY;  // (a masked chunk's record may hold anything)
+        mnew = ok[u] ? fmaxf(mnew, sv[u].x * kLog2e) : mnew;
+    }
+    float rs = mnew == m ? 1.f : fexp2(m - mnew);
+    m = mnew;
+    l *= rs;
+#pragma unroll
+    for (int u = 0; u < NR; ++u) {
+        const float wk = ok[u] ? fexp2(sv[u].x * kLog2e - m) : 0.f;
+        l += wk;
+        r[u].add(o, rs, ok[u] ? wk * sv[u].y : 0.f, ok[u]);
+        rs = 1.f;
+    }
+}
+
 // New tokens of a sequence: `fresh` of them, the last of `len`.
 struct Seq {
     int len, fresh, pos0;
@@ -213,22 +278,34 @@ struct Ws {
     int* list;     // [bg][Ns * K] row << 6 | slot
     int4* work;    // (bg, chunk, offset, rows)
     float* sigma;  // [bg][Rs][nC]
-    float2* rec_s; // [bg][Ns][K][G] s^ and the record's unit
-    char* rec_o;   // [bg][Ns][K][G] records
+    float2* rec_s; // [bg][Ns][slots][G] s^ and the record's unit
+    char* rec_o;   // [bg][Ns][slots][G] records
 };
 struct Layout {
     size_t counts, offs, ranks, list, work, sigma, rec_s, rec_o, total;
-    int Ns, Rs;
+    int Ns, Rs, slots;  // records of a (row, head)
+    bool few;           // the windows' pieces among them
     size_t max_work;
 };
 
 // sigma of a block of rows: as many as fit the last-level cache, in whole score tiles
 constexpr size_t kSigmaBytes = size_t(128) << 20;
 
-Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int bf16) {
+// Calls of so many records or fewer, those of the windows' pieces among them, take the windows as
+// work items too (k_pp_join instead of k_pp_local, whose workgroups, each with all blocks of its rows' windows one
+// after the other, take some 35 us however few they are).  Whole calls, K = 16, W = 512, k_pp_join and
+// k_pp_local in us: bf16, 32 heads in groups of 4, d = 128, over 16000 tokens: 16 new tokens (12K records) 50 and
+// 70, 256 (200K) 89 and 97, 512 (400K) 118 and 117, 1024 (800K) 218 and 185; f32: 512 291 and 314, 1024
+// 565 and 497; f32, 16 heads in groups of 8, d = 64: 1024 (400K) 188 and 212.
+constexpr size_t kFewRecords = size_t(5) << 16;
+
+Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf16) {
     Layout w;
-    const size_t nC = L / kChunk, bg = (size_t)B * Hkv;
-    const size_t rec = (bf16 ? 2 : 4) * (size_t)d, per_row = (size_t)B * Hq * K * (rec + sizeof(float2));
+    const size_t nC = L / kChunk, bg = (size_t)B * Hkv, columns = (size_t)B * Hq * N;
+    const size_t pieces = ((size_t)W + 62) / kChunk + 1;
+    w.few = columns * (K + pieces) <= kFewRecords;
+    w.slots = w.few ? K + (int)pieces : K;
+    const size_t rec = (bf16 ? 2 : 4) * (size_t)d + sizeof(float2), per_row = (size_t)B * Hq * w.slots * rec;
     const size_t cap = prefill_record_cap(0);
     size_t ns = N;
     if (ns * per_row > cap) ns = std::min<size_t>(N, std::max<size_t>(kScoreRows, cap / per_row / kScoreRows * kScoreRows));
@@ -236,7 +313,7 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int bf16) {
     rs = std::min(ns, std::max<size_t>(rs, kScoreRows));
     w.Ns = (int)ns;
     w.Rs = (int)rs;
-    w.max_work = bg * (std::min(nC, ns * K) + ns * K / kSegRows);
+    w.max_work = bg * (std::min(nC, ns * K) + ns * K / seg_rows(bf16, Hq / Hkv));
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -249,8 +326,10 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int bf16) {
     w.list = take(bg * ns * K * sizeof(int));
     w.work = take(w.max_work * sizeof(int4));
     w.sigma = take(bg * rs * nC * sizeof(float));
-    w.rec_s = take((size_t)B * Hq * ns * K * sizeof(float2));
-    w.rec_o = take((size_t)B * Hq * ns * K * rec);
+    // (no less than a call of fewer rows may need)
+    const size_t records = std::max((size_t)B * Hq * ns * w.slots, w.few ? 0 : std::min(kFewRecords, cap / rec));
+    w.rec_s = take(records * sizeof(float2));
+    w.rec_o = take(records * (rec - sizeof(float2)));
     w.total = at;
     return w;
 }
@@ -258,21 +337,24 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int bf16) {
 // ---------------------------------------------------------------------------
 // scores
 // ---------------------------------------------------------------------------
-// A workgroup of 8 waves takes 128 rows of a KV group (16 each) and `slice` candidates; 64
+// A workgroup takes 128 rows (f32: 64) of a KV group, 16 per wave, and `slice` candidates; 64
 // landmark rows of one head at a time come through LDS (double-buffered) and serve all rows;
-// the maximum over the heads stays in registers until a block of candidates is done.
+// the maximum over the heads stays in registers until a block of candidates is done.  It also
+// clears the words that the next launches count in.
 template <typename T, int D, int G>
-__global__ __launch_bounds__(kScoreWaves * kWave) void k_pp_score(FwdArgs f, const int32_t* newlens, float* sigma,
-                                                                 int r0, int Rs, int slice, int nslices) {
+__global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave) void k_pp_score(FwdArgs f, const int32_t* newlens,
+                                                                                 float* sigma, int r0, int Rs, int slice,
+                                                                                 int nslices, int* counts, size_t nclear) {
     using C = Cfg<T, D>;
-    constexpr int NT = kScoreWaves * kWave;
+    constexpr int NW = score_waves(C::ES == 2), NT = NW * kWave, ROWS = 16 * NW;
     constexpr int PPT = kScoreCand * D * C::ES / 16 / NT;
     constexpr bool kHold = C::ES == 2;  // the query operands of all heads fit in registers
     static_assert(PPT >= 1 && PPT * NT * 16 == kScoreCand * D * C::ES, "landmark blocks split evenly over the threads");
     __shared__ __align__(16) char s_l[2][kScoreCand * C::KROW];
     __shared__ float s_b[2][kScoreCand];
     const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave, lg = lane / 16;
-    const int ntiles = (Rs + kScoreRows - 1) / kScoreRows;
+    const int ntiles = (Rs + ROWS - 1) / ROWS;
+    for (size_t i = (size_t)blockIdx.x * NT + tid; i < nclear; i += (size_t)gridDim.x * NT) counts[i] = 0;
     int at = blockIdx.x;
     const int g = at % f.Hkv;
     at /= f.Hkv;
@@ -280,8 +362,8 @@ __global__ __launch_bounds__(kScoreWaves * kWave) void k_pp_score(FwdArgs f, con
     at /= nslices;
     const int tile = at % ntiles, b = at / ntiles;
     const Seq sq = sequence(f, newlens, b);
-    const int q0 = r0 + tile * kScoreRows;
-    const int qend = min(min(q0 + kScoreRows, r0 + Rs), sq.fresh);
+    const int q0 = r0 + tile * ROWS;
+    const int qend = min(min(q0 + ROWS, r0 + Rs), sq.fresh);
     if (q0 >= qend) return;
     const int nC = f.L / kChunk;
     const int c_beg = part * slice, c_end = min(n_candidates(sq.pos0 + qend - 1, f.W), c_beg + slice);
@@ -293,7 +375,7 @@ __global__ __launch_bounds__(kScoreWaves * kWave) void k_pp_score(FwdArgs f, con
     auto q_operand = [&](int hh, int ks) {
         return ld16(qr + (((size_t)b * f.Hq + g * G + hh) * f.N + qa) * D + ks * 4 * C::EP + lg * C::EP);
     };
-    uint4 aq[kHold ? G : 1][C::KS];
+    uint4 aq[kHold ? G : 2][C::KS];
     if constexpr (kHold) {
 #pragma unroll
         for (int hh = 0; hh < G; ++hh)
@@ -355,10 +437,19 @@ __global__ __launch_bounds__(kScoreWaves * kWave) void k_pp_score(FwdArgs f, con
             for (int hh = 0; hh < G; ++hh)
                 if (shared_lmk || hh == lh) head(aq[hh]);
         } else {
-            for (int hh = shared_lmk ? 0 : lh; hh <= (shared_lmk ? G - 1 : lh); ++hh) {
+            // one head's operands at a time, the next one's in flight
+            auto load = [&](int hh, uint4 (&q)[C::KS]) {
 #pragma unroll
-                for (int ks = 0; ks < C::KS; ++ks) aq[0][ks] = q_operand(hh, ks);
+                for (int ks = 0; ks < C::KS; ++ks) q[ks] = q_operand(min(hh, G - 1), ks);
+            };
+            const int h0 = shared_lmk ? 0 : lh, h1 = shared_lmk ? G : lh + 1;
+            load(h0, aq[0]);
+            for (int hh = h0; hh < h1; hh += 2) {
+                load(hh + 1, aq[1]);
                 head(aq[0]);
+                if (hh + 1 >= h1) break;
+                load(hh + 2, aq[0]);
+                head(aq[1]);
             }
         }
         if (lh == NH - 1) {
@@ -433,12 +524,24 @@ __global__ __launch_bounds__(kSelWaves * kWave) void k_pp_select(FwdArgs f, cons
 // rows of every chunk
 // ---------------------------------------------------------------------------
 // One workgroup per (b, g): offsets of the chunks' rows in the list, and the work items (runs of
-// up to kSegRows rows of a chunk), which take a range of `work` of their own.
+// up to `seg` rows of a chunk), which take a range of `work` of their own; few rows are put in
+// the list right here.
 constexpr int kPlanThreads = 1024;
-__global__ __launch_bounds__(kPlanThreads) void k_pp_plan(int nC, const int* counts, int* offs, int4* work,
-                                                         int* nwork) {
+constexpr size_t kPlanFill = 16 * kPlanThreads;  // entries of a (b, g) that are not worth a launch
+__device__ __forceinline__ void put_in_list(const FwdArgs& f, const int* offs, const int* ranks, int* list, size_t bg,
+                                            int n0, int Ns, int fresh, int e) {  // entry e of (b, g)
+    const int n = e / f.K, slot = e % f.K;
+    if (n0 + n >= fresh) return;
+    const int rank = ranks[bg * Ns * f.K + e];
+    if (rank < 0) return;
+    const int c = f.idx[(bg * f.N + n0 + n) * f.K + slot];
+    list[bg * Ns * f.K + offs[bg * (f.L / kChunk) + c] + rank] = n << 6 | slot;
+}
+__global__ __launch_bounds__(kPlanThreads) void k_pp_plan(FwdArgs f, const int32_t* newlens, const int* counts,
+                                                         int* offs, int4* work, int* nwork, const int* ranks,
+                                                         int* list, int n0, int Ns, int fill, int seg) {
     __shared__ int s_rows[kPlanThreads / kWave], s_items[kPlanThreads / kWave], s_base;
-    const int bg = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, w = tid / kWave;
+    const int bg = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, nC = f.L / kChunk;
     const int* cnt = counts + (size_t)bg * nC;
     auto scan = [&](int x, int* s_sum, int& before, int& all) {  // over the workgroup
         int incl = x;
@@ -457,38 +560,35 @@ __global__ __launch_bounds__(kPlanThreads) void k_pp_plan(int nC, const int* cou
         }
     };
     int items = 0;
-    for (int c = tid; c < nC; c += kPlanThreads) items += (cnt[c] + kSegRows - 1) / kSegRows;
+    for (int c = tid; c < nC; c += kPlanThreads) items += (cnt[c] + seg - 1) / seg;
     int before, all;
     scan(items, s_items, before, all);
     if (tid == 0) s_base = all ? atomicAdd(nwork, all) : 0;
     __syncthreads();
     int rows0 = 0, items0 = s_base;
     for (int c0 = 0; c0 < nC; c0 += kPlanThreads) {
-        const int c = c0 + tid, n = c < nC ? cnt[c] : 0, k = (n + kSegRows - 1) / kSegRows;
+        const int c = c0 + tid, n = c < nC ? cnt[c] : 0, k = (n + seg - 1) / seg;
         int r, ra, i, ia;
         scan(n, s_rows, r, ra);
         scan(k, s_items, i, ia);
         if (c < nC) offs[(size_t)bg * nC + c] = rows0 + r;
         for (int s = 0; s < k; ++s)
-            work[items0 + i + s] = make_int4(bg, c, rows0 + r + s * kSegRows, min(kSegRows, n - s * kSegRows));
+            work[items0 + i + s] = make_int4(bg, c, rows0 + r + s * seg, min(seg, n - s * seg));
         rows0 += ra;
         items0 += ia;
         __syncthreads();
     }
+    if (!fill) return;
+    const int fresh = sequence(f, newlens, bg / f.Hkv).fresh;
+    for (int e = tid; e < Ns * f.K; e += kPlanThreads) put_in_list(f, offs, ranks, list, bg, n0, Ns, fresh, e);
 }
 
 __global__ __launch_bounds__(256) void k_pp_fill(FwdArgs f, const int32_t* newlens, const int* offs, const int* ranks,
                                                  int* list, int n0, int Ns) {
-    const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= (size_t)f.B * f.Hkv * Ns * f.K) return;
-    const int slot = (int)(e % f.K);
-    const size_t row = e / f.K, bg = row / Ns;
-    const int n = (int)(row % Ns);
-    if (n0 + n >= sequence(f, newlens, (int)(bg / f.Hkv)).fresh) return;
-    const int rank = ranks[e];
-    if (rank < 0) return;
-    const int c = f.idx[(bg * f.N + n0 + n) * f.K + slot];
-    list[bg * Ns * f.K + offs[bg * (f.L / kChunk) + c] + rank] = n << 6 | slot;
+    const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x, per = (size_t)Ns * f.K;
+    if (e >= (size_t)f.B * f.Hkv * per) return;
+    const size_t bg = e / per;
+    put_in_list(f, offs, ranks, list, bg, n0, Ns, sequence(f, newlens, (int)(bg / f.Hkv)).fresh, (int)(e % per));
 }
 
 // ---------------------------------------------------------------------------
@@ -497,10 +597,15 @@ __global__ __launch_bounds__(256) void k_pp_fill(FwdArgs f, const int32_t* newle
 // A workgroup takes one work item after the other: K and V of the chunk and the landmark rows of
 // the group's heads in LDS, then columns p = (entry p / G, head p % G), 16 to a wave at a
 // time, so that a chunk with few rows still fills its instructions with their heads.
-template <typename T, int D, int G>
-__global__ __launch_bounds__(kChunkWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k_pp_chunks(FwdArgs f, Ws ws,
-                                                                                          const int* nwork, int n0,
-                                                                                          int Ns) {
+// WINDOW: blocks of the rows' windows are items too, SEG rows and a block each, with records of
+// their own (slots K .. K + P - 1 of a row are the pieces of its window, s^ is then the
+// log-sum-exp).  Values that some row must not see: as in k_pp_local.
+template <typename T, int D, int G, bool WINDOW>
+__global__ __launch_bounds__(kChunkWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k_pp_chunks(FwdArgs f,
+                                                                                          const int32_t* newlens,
+                                                                                          Ws ws, const int* nwork,
+                                                                                          int n0, int Ns, int slots,
+                                                                                          int blocks) {
     using C = Cfg<T, D>;
     constexpr int NT = kChunkWaves * kWave;
     constexpr int PPT = kChunk * D * C::ES / 16 / NT;
@@ -510,12 +615,36 @@ __global__ __launch_bounds__(kChunkWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
     __shared__ float s_b[G];
     const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave, lg = lane / 16;
     const int col = lane % 16, hh = col % G;
-    const int items = *nwork;
+    constexpr int SEG = seg_rows(C::ES == 2, G);
+    const int segs = (Ns + SEG - 1) / SEG;
+    const int listed = nwork ? *nwork : 0, items = listed + (WINDOW ? f.B * f.Hkv * segs * blocks : 0);
     const float c1 = f.scale * kLog2e;
     for (int it = blockIdx.x; it < items; it += gridDim.x) {
-        const int4 wi = ws.work[it];
-        const int b = wi.x / f.Hkv, g = wi.x % f.Hkv, c = wi.y, len = wi.w;
-        const size_t bg = wi.x, pg = page_of(f, b, c);
+        const bool win = WINDOW && it >= listed;  // uniform
+        int bgi, c, len, first = 0;               // first: the item's first row, or place in the list
+        Seq sq = {};
+        if (win) {
+            const int x = it - listed;
+            bgi = x / (segs * blocks);
+            sq = sequence(f, newlens, bgi / f.Hkv);
+            first = x / blocks % segs * SEG;
+            len = min(min(SEG, Ns - first), sq.fresh - n0 - first);
+            if (len <= 0) continue;
+            c = n_candidates(sq.pos0 + n0 + first, f.W) + x % blocks;
+            if (c > (sq.pos0 + n0 + first + len - 1) / kChunk) continue;
+        } else {
+            const int4 wi = ws.work[it];
+            bgi = wi.x;
+            c = wi.y;
+            first = wi.z;
+            len = wi.w;
+        }
+        const int b = bgi / f.Hkv, g = bgi % f.Hkv;
+        const size_t bg = bgi, pg = page_of(f, b, c);
+        // a window's block that some row of the item sees only part of
+        const bool part = win && (c < n_candidates(sq.pos0 + n0 + first + len - 1, f.W) ||
+                                  c * kChunk + kChunk - 1 > sq.pos0 + n0 + first);
+        bool bad = false;
         {
             const T* k = as<T>(f.k) + (pg * f.Hkv + g) * kChunk * D;
             const T* v = as<T>(f.v) + (pg * f.Hkv + g) * kChunk * D;
@@ -525,8 +654,14 @@ __global__ __launch_bounds__(kChunkWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
                 kr[u] = ld16(k + (size_t)(tid + u * NT) * C::EP);
                 vr[u] = ld16(v + (size_t)(tid + u * NT) * C::EP);
             }
+            if (part)
+#pragma unroll
+                for (int u = 0; u < PPT; ++u) {
+                    if (c * kChunk + (tid + u * NT) / (D / C::EP) >= sq.len) vr[u] = make_uint4(0, 0, 0, 0);
+                    bad |= !all_finite<T>(vr[u]);
+                }
             __syncthreads();  // the previous item has been read
-            for (int e = tid; e < G * D / C::EP; e += NT) {
+            if (!win) for (int e = tid; e < G * D / C::EP; e += NT) {
                 const int h = e / (D / C::EP), d0 = (e % (D / C::EP)) * C::EP;
                 const size_t lrow = pg * f.Hl + (f.Hl == f.Hq ? g * G + h : g);
                 *reinterpret_cast<uint4*>(s_l + h * D * C::ES + d0 * C::ES) = ld16(as<T>(f.lmk) + lrow * D + d0);
@@ -539,32 +674,43 @@ __global__ __launch_bounds__(kChunkWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
                 *reinterpret_cast<uint4*>(s_v + j * C::VROW + at) = vr[u];
             }
         }
-        __syncthreads();
-        const int* seg = ws.list + bg * (size_t)Ns * f.K + wi.z;
+        if (WINDOW)
+            bad = __syncthreads_or(bad);
+        else
+            __syncthreads();
+        const int* seg = ws.list + bg * (size_t)Ns * f.K + first;
         const int units = (len * G + 15) / 16;
         for (int u = w; u < units; u += kChunkWaves) {
             const int e = u * (16 / G) + col / G;
             const bool live = e < len;
-            const int ent = seg[min(e, len - 1)], n = ent >> 6, slot = ent & 63;
+            int n = first + min(e, len - 1), slot = 0;
+            if (!win) {
+                const int ent = seg[min(e, len - 1)];
+                n = ent >> 6;
+                slot = ent & 63;
+            }
             const size_t qrow = (((size_t)b * f.Hq + g * G + hh) * f.N + n0 + n) * D;
             uint4 q[C::KS];
 #pragma unroll
             for (int ks = 0; ks < C::KS; ++ks) q[ks] = ld16(as<T>(f.q) + qrow + ks * 4 * C::EP + lg * C::EP);
-            // s^: the heads' landmark rows are rows 0 .. G - 1 of the A operand, so column p's is
-            // accumulator row p % G, which lane group hh / 4 holds as element hh % 4
-            f32x4 sh = zero4();
+            float shat = 0.f;
+            if (!win) {
+                // s^: the heads' landmark rows are rows 0 .. G - 1 of the A operand, so column p's is
+                // accumulator row p % G, which lane group hh / 4 holds as element hh % 4
+                f32x4 sh = zero4();
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) {
-                uint4 al = lds16(s_l + min(col, G - 1) * D * C::ES + ks * 64 + lg * 16);
-                if (col >= G) al = make_uint4(0, 0, 0, 0);
-                const uint4 qs = f.q_route ? ld16(as<T>(f.q_route) + qrow + ks * 4 * C::EP + lg * C::EP) : q[ks];
-                sh = mma<T>(al, qs, sh);
+                for (int ks = 0; ks < C::KS; ++ks) {
+                    uint4 al = lds16(s_l + min(col, G - 1) * D * C::ES + ks * 64 + lg * 16);
+                    if (col >= G) al = make_uint4(0, 0, 0, 0);
+                    const uint4 qs = f.q_route ? ld16(as<T>(f.q_route) + qrow + ks * 4 * C::EP + lg * C::EP) : q[ks];
+                    sh = mma<T>(al, qs, sh);
+                }
+                const int hi = hh & 3;
+                const float shv = hi == 0 ? sh[0] : hi == 1 ? sh[1] : hi == 2 ? sh[2] : sh[3];
+                const float shr = __shfl(shv, (hh >> 2) * 16 + col, kWave);
+                const float bias = s_b[hh];
+                shat = bias == -INFINITY ? -INFINITY : f.scale * shr + bias;
             }
-            const int hi = hh & 3;
-            const float shv = hi == 0 ? sh[0] : hi == 1 ? sh[1] : hi == 2 ? sh[2] : sh[3];
-            const float shr = __shfl(shv, (hh >> 2) * 16 + col, kWave);
-            const float bias = s_b[hh];
-            const float shat = bias == -INFINITY ? -INFINITY : f.scale * shr + bias;
             f32x4 st[4];
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
@@ -574,31 +720,47 @@ __global__ __launch_bounds__(kChunkWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
                     st[kb] = mma<T>(lds16(s_k + (kb * 16 + col) * C::KROW + ks * 64 + lg * 16), q[ks], st[kb]);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            const int pos = sq.pos0 + n0 + n, ell = n_candidates(pos, f.W) * kChunk;  // (of a window's row)
             float mx = -INFINITY, sum = 0.f;
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     st[kb][i] *= c1;
+                    if (part) {
+                        const int j = c * kChunk + kb * 16 + lg * 4 + i;
+                        const bool sees = (j <= pos) & (j >= ell);
+                        st[kb][i] = sees ? st[kb][i] : -INFINITY;
+                    }
                     mx = fmaxf(mx, st[kb][i]);
                 }
             mx = group4_max(mx);
+            const float muse = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    st[kb][i] = fexp2(st[kb][i] - mx);
+                    st[kb][i] = fexp2(st[kb][i] - muse);
                     sum += st[kb][i];
                 }
             sum = group4_sum(sum);
             f32x4 o[C::DB];
 #pragma unroll
             for (int db = 0; db < C::DB; ++db) o[db] = zero4();
-            add_pv<T, D>(s_v, st, o, lane);
-            const float inv = 1.f / sum;
-            const size_t rec = ((bg * Ns + n) * f.K + slot) * G + hh;
-            const float unit = Record<T, D>::store(ws.rec_o + rec * Record<T, D>::BYTES, o, inv, lg, live);
-            if (live && lg == 0) ws.rec_s[rec] = make_float2(shat, unit);
+            if (WINDOW && bad)
+                add_pv_by_key<T, D>(s_v, st, o, lane, pos - c * kChunk, ell - c * kChunk);
+            else
+                add_pv<T, D>(s_v, st, o, lane);
+            const float inv = sum > 0.f ? 1.f / sum : 0.f;
+            bool keep = live;
+            if (win) {
+                slot = f.K + c - ell / kChunk;
+                keep = live && slot >= f.K && c <= pos / kChunk;
+                shat = (mx + __log2f(sum)) * (1.f / kLog2e);
+            }
+            const size_t rec = ((bg * Ns + n) * slots + slot) * G + hh;
+            const float unit = Record<T, D>::store(ws.rec_o + rec * Record<T, D>::BYTES, o, inv, lg, keep);
+            if (keep && lg == 0) ws.rec_s[rec] = make_float2(shat, unit);
         }
     }
 }
@@ -676,12 +838,7 @@ __global__ __launch_bounds__(kLocalWaves * kWave, D * sizeof(T) <= 256 ? 4 : 2) 
             if (j0 + j >= sq.len) v = make_uint4(0, 0, 0, 0);
             *reinterpret_cast<uint4*>(&s_k[buf][j * C::KROW + piece]) = x.k[u];
             *reinterpret_cast<uint4*>(&s_v[buf][j * C::VROW + piece]) = v;
-            const uint32_t y[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                bad |= (y[i] & 0x7f800000u) == 0x7f800000u;
-                if constexpr (C::ES == 2) bad |= (y[i] & 0x7f80u) == 0x7f80u;
-            }
+            bad |= !all_finite<T>(v);
         }
         if (bad && masked(j0)) s_bad[buf] = j0;
     };
@@ -712,23 +869,7 @@ __global__ __launch_bounds__(kLocalWaves * kWave, D * sizeof(T) <= 256 ? 4 : 2) 
                 ok[u] = (k0 + u < f.K) & (c >= 0) & (c < ncand) & (c > prev);  // as idx_entry_valid
                 prev = c;
             }
-            float mnew = m;
-#pragma unroll
-            for (int u = 0; u < SB; ++u) {
-                ok[u] = ok[u] && sv[u].x != -INFINITY;  // (a masked chunk's record may hold anything)
-                sv[u].x *= kLog2e;
-                mnew = ok[u] ? fmaxf(mnew, sv[u].x) : mnew;
-            }
-            float rs = mnew == m ? 1.f : fexp2(m - mnew);
-            m = mnew;
-            l *= rs;
-#pragma unroll
-            for (int u = 0; u < SB; ++u) {
-                const float wk = ok[u] ? fexp2(sv[u].x - m) : 0.f;
-                l += wk;
-                r[u].add(o, rs, ok[u] ? wk * sv[u].y : 0.f, ok[u]);
-                rs = 1.f;
-            }
+            add_records<T, D, SB>(r, sv, ok, o, m, l);
         }
     };
     bool seen_bad = false;  // uniform
@@ -785,22 +926,7 @@ __global__ __launch_bounds__(kLocalWaves * kWave, D * sizeof(T) <= 256 ? 4 : 2) 
 #pragma unroll
             for (int db = 0; db < C::DB; ++db) o[db] *= alpha;
             if (careful && part && s_bad[buf] == j0) {  // uniform
-#pragma unroll 1
-                for (int j = 0; j < kChunk; ++j) {
-                    float mine = 0.f;
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) mine = j / 16 * 4 + j % 4 == x ? st[x / 4][x % 4] : mine;
-                    const float p = __shfl(mine, (j % 16) / 4 * 16 + col, kWave);
-                    const bool sees = j0 + j <= pos && j0 + j >= ell;
-                    const T* v = reinterpret_cast<const T*>(&s_v[buf][j * C::VROW]);
-#pragma unroll
-                    for (int db = 0; db < C::DB; ++db) {
-#pragma unroll
-                        for (int y = 0; y < 4; ++y)
-                            o[db][y] = sees ? fmaf(p, to_f32(v[dim_of<T>(db, y, lg)]), o[db][y]) : o[db][y];
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                }
+                add_pv_by_key<T, D>(s_v[buf], st, o, lane, pos - j0, ell - j0);
             } else {
                 add_pv<T, D>(s_v[buf], st, o, lane);
             }
@@ -842,11 +968,109 @@ __global__ __launch_bounds__(kLocalWaves * kWave, D * sizeof(T) <= 256 ? 4 : 2) 
     if (lg == 0) f.lse[row] = (m + __log2f(l)) * (1.f / kLog2e);
 }
 
+// ---------------------------------------------------------------------------
+// records of chunks and window, joined
+// ---------------------------------------------------------------------------
+// A wave per (row, head): each 16 lanes take every fourth record, a sixteenth of it per lane, in
+// whole lines and independent of each other, and the four join at the end.
+constexpr int kJoinWaves = 4;
+template <typename T, int D>
+__global__ __launch_bounds__(kJoinWaves * kWave) void k_pp_join(FwdArgs f, const int32_t* newlens, const float2* rec_s,
+                                                               const char* rec_o, int n0, int Ns, int slots) {
+    using C = Cfg<T, D>;
+    // 16-byte pieces of a lane (a bf16 record of d = 64 has 8: the other 8 lanes read them too)
+    constexpr int BYTES = Record<T, D>::BYTES, PCS = (BYTES / 16 + 15) / 16;
+    constexpr int EPP = C::ES == 2 ? 8 : 4;  // elements of a piece
+    const int G = f.Hq / f.Hkv, lane = threadIdx.x % kWave, sub = lane % 16, part = lane / 16;
+    const size_t pair = (size_t)blockIdx.x * kJoinWaves + wave_id();  // (b, g, n, head)
+    if (pair >= (size_t)f.B * f.Hkv * Ns * G) return;
+    const int hh = (int)(pair % G), n = n0 + (int)(pair / G % Ns);
+    const size_t bg = pair / G / Ns;
+    const int b = (int)(bg / f.Hkv), g = (int)(bg % f.Hkv);
+    const Seq sq = sequence(f, newlens, b);
+    if (n >= sq.fresh) return;
+    const int pos = sq.pos0 + n, ncand = n_candidates(pos, f.W), nrec = f.K + pos / kChunk + 1 - ncand;
+    const int32_t* irow = f.idx + (bg * f.N + n) * f.K;
+    const size_t rec0 = (bg * Ns + (n - n0)) * slots;
+    float acc[PCS][EPP] = {}, m = -INFINITY, l = 0.f;
+    constexpr int SB = 4;  // records of a lane in flight together
+    for (int k0 = part; k0 < nrec; k0 += 4 * SB) {
+        uint4 x[SB][PCS];
+        float2 sv[SB];
+        bool ok[SB];
+#pragma unroll
+        for (int u = 0; u < SB; ++u) {
+            const int k = min(k0 + 4 * u, nrec - 1);
+            const size_t rec = (rec0 + k) * G + hh;
+            sv[u] = rec_s[rec];
+#pragma unroll
+            for (int t = 0; t < PCS; ++t)
+                x[u][t] = *reinterpret_cast<const uint4*>(rec_o + rec * BYTES + (sub * PCS + t) * 16 % BYTES);
+            ok[u] = k0 + 4 * u < nrec && (k >= f.K || idx_entry_valid(irow, k, ncand));
+        }
+        float mnew = m;
+#pragma unroll
+        for (int u = 0; u < SB; ++u) {
+            ok[u] = ok[u] && sv[u].x != -INFINITY;  // (a masked chunk's record may hold anything)
+            mnew = ok[u] ? fmaxf(mnew, sv[u].x * kLog2e) : mnew;
+        }
+        float rs = mnew == m ? 1.f : fexp2(m - mnew);
+        m = mnew;
+        l *= rs;
+#pragma unroll
+        for (int u = 0; u < SB; ++u) {
+            const float wk = ok[u] ? fexp2(sv[u].x * kLog2e - m) : 0.f, wu = ok[u] ? wk * sv[u].y : 0.f;
+            l += wk;
+#pragma unroll
+            for (int t = 0; t < PCS; ++t) {
+                const uint4 y = ok[u] ? x[u][t] : make_uint4(0, 0, 0, 0);
+                if constexpr (C::ES == 2) {
+                    typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+                    const h8 h = __builtin_bit_cast(h8, y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[t][e] = fmaf((float)h[e], wu, acc[t][e] * rs);
+                } else {
+                    const f32x4 h = __builtin_bit_cast(f32x4, y);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(h[e], wu, acc[t][e] * rs);
+                }
+            }
+            rs = 1.f;
+        }
+    }
+    const float M = group4_max(m), to = m == M ? 1.f : fexp2(m - M);
+    l = group4_sum(l * to);
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int t = 0; t < PCS; ++t)
+#pragma unroll
+        for (int e = 0; e < EPP; ++e) acc[t][e] = group4_sum(acc[t][e] * to) * inv;
+    if (part != 0) return;
+    const size_t row = ((size_t)b * f.Hq + g * G + hh) * f.N + n;
+    T* out = as_mut<T>(f.out) + row * D;
+#pragma unroll
+    for (int t = 0; t < PCS; ++t) {
+        const int piece = sub * PCS + t, pt = piece / 4, lg = piece % 4;  // piece 4 pt + lg of the record
+        if (piece >= BYTES / 16) break;
+        if constexpr (C::ES == 2) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                store_unaligned(out + dim_of<T>(2 * pt + h, 0, lg),
+                                make_uint2(pack_bf16x2(acc[t][4 * h], acc[t][4 * h + 1]),
+                                           pack_bf16x2(acc[t][4 * h + 2], acc[t][4 * h + 3])));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[dim_of<T>(pt, i, lg)] = acc[t][i];
+        }
+    }
+    if (sub == 0) f.lse[row] = (M + __log2f(l)) * (1.f / kLog2e);
+}
+
 struct Run {
     template <typename T, int D, int G>
     static hipError_t run(const PrefillPagedArgs& a, hipStream_t s) {
         const FwdArgs& f = a.f;
-        const Layout ly = layout(f.B, f.Hq, f.Hkv, f.N, f.L, D, f.K, f.bf16);
+        const Layout ly = layout(f.B, f.Hq, f.Hkv, f.N, f.L, D, f.K, f.W, f.bf16);
         char* base = static_cast<char*>(f.ws);
         Ws ws;
         ws.counts = reinterpret_cast<int*>(base + ly.counts);
@@ -859,22 +1083,25 @@ struct Run {
         ws.rec_o = base + ly.rec_o;
         const int nC = f.L / kChunk, maxc = n_candidates(f.L - 1, f.W);  // candidates of any row, at most
         const size_t bg = (size_t)f.B * f.Hkv, ncount = bg * nC;
-        const int cus = device_cus();
+        const int cus = device_cus(), seg = seg_rows(f.bf16, G);
         for (int n0 = 0; n0 < f.N; n0 += ly.Ns) {
             const int Ns = std::min(ly.Ns, f.N - n0);
-            HILS_LAUNCH("k_pp_clear", k_pp_clear, dim3((unsigned)std::min<size_t>((ncount + 256) / 256, 4096)), dim3(256),
-                        0, s, ws.counts, ncount + 1);
+            if (f.given_idx && maxc > 0)
+                HILS_LAUNCH("k_pp_clear", k_pp_clear, dim3((unsigned)std::min<size_t>((ncount + 256) / 256, 4096)),
+                            dim3(256), 0, s, ws.counts, ncount + 1);
             for (int r0 = n0; r0 < n0 + Ns; r0 += ly.Rs) {
                 const int Rs = std::min(ly.Rs, n0 + Ns - r0);
                 if (!f.given_idx && maxc > 0) {
                     // slices of candidates for a few workgroups per CU where there are few rows
-                    const size_t tiles = bg * ((Rs + kScoreRows - 1) / kScoreRows);
+                    constexpr int waves = score_waves(sizeof(T) == 2);
+                    const size_t tiles = bg * ((Rs + 16 * waves - 1) / (16 * waves));
                     const size_t want = std::max<size_t>(1, 4 * (size_t)cus / tiles);
                     const int blocks = (maxc + kScoreCand - 1) / kScoreCand;
                     const int slice = kScoreCand * (int)((blocks + want - 1) / want);
                     const int nslices = (maxc + slice - 1) / slice;
                     HILS_LAUNCH("k_pp_score", (k_pp_score<T, D, G>), dim3((unsigned)(tiles * nslices)),
-                                dim3(kScoreWaves * kWave), 0, s, f, a.newlens, ws.sigma, r0, Rs, slice, nslices);
+                                dim3(waves * kWave), 0, s, f, a.newlens, ws.sigma, r0, Rs, slice, nslices,
+                                ws.counts, r0 == n0 ? ncount + 1 : 0);
                 }
                 const dim3 grid((unsigned)((bg * Rs + kSelWaves - 1) / kSelWaves));
                 auto select = [&](auto e_tag) {
@@ -890,15 +1117,31 @@ struct Run {
                     select(std::integral_constant<int, 16>{});
             }
             int* nwork = ws.counts + ncount;
+            const size_t most = bg * (std::min<size_t>(maxc, (size_t)Ns * f.K) + (size_t)Ns * f.K / seg);
             if (maxc > 0) {
-                HILS_LAUNCH("k_pp_plan", k_pp_plan, dim3((unsigned)bg), dim3(kPlanThreads), 0, s, nC,
-                            (const int*)ws.counts, ws.offs, ws.work, nwork);
-                HILS_LAUNCH("k_pp_fill", k_pp_fill, dim3((unsigned)((bg * Ns * f.K + 255) / 256)), dim3(256), 0, s, f,
-                            a.newlens, (const int*)ws.offs, (const int*)ws.ranks, ws.list, n0, Ns);
-                const size_t most = bg * (std::min<size_t>(maxc, (size_t)Ns * f.K) + (size_t)Ns * f.K / kSegRows);
-                HILS_LAUNCH("k_pp_chunks", (k_pp_chunks<T, D, G>), dim3((unsigned)std::min<size_t>(most, 16 * cus)),
-                            dim3(kChunkWaves * kWave), 0, s, f, ws, (const int*)nwork, n0, Ns);
+                const bool fill = (size_t)Ns * f.K <= kPlanFill;
+                HILS_LAUNCH("k_pp_plan", k_pp_plan, dim3((unsigned)bg), dim3(kPlanThreads), 0, s, f, a.newlens,
+                            (const int*)ws.counts, ws.offs, ws.work, nwork, (const int*)ws.ranks, ws.list, n0, Ns, (int)fill, seg);
+                if (!fill)
+                    HILS_LAUNCH("k_pp_fill", k_pp_fill, dim3((unsigned)((bg * Ns * f.K + 255) / 256)), dim3(256), 0, s, f,
+                                a.newlens, (const int*)ws.offs, (const int*)ws.ranks, ws.list, n0, Ns);
             }
+            const size_t chunk_grid = 16 * (size_t)cus;
+            if (ly.few) {
+                const int blocks = (f.W + 61 + seg) / kChunk + 1;  // that the windows of `seg` rows reach into, at most
+                const size_t wins = bg * ((Ns + seg - 1) / seg) * blocks;
+                HILS_LAUNCH("k_pp_chunks", (k_pp_chunks<T, D, G, true>), dim3((unsigned)std::min(most + wins, chunk_grid)),
+                            dim3(kChunkWaves * kWave), 0, s, f, a.newlens, ws, maxc > 0 ? (const int*)nwork : nullptr, n0, Ns,
+                            ly.slots, blocks);
+                const size_t pairs = bg * Ns * G;
+                HILS_LAUNCH("k_pp_join", (k_pp_join<T, D>), dim3((unsigned)((pairs + kJoinWaves - 1) / kJoinWaves)),
+                            dim3(kJoinWaves * kWave), 0, s, f, a.newlens, (const float2*)ws.rec_s, (const char*)ws.rec_o, n0,
+                            Ns, ly.slots);
+                continue;
+            }
+            if (maxc > 0)
+                HILS_LAUNCH("k_pp_chunks", (k_pp_chunks<T, D, G, false>), dim3((unsigned)std::min(most, chunk_grid)),
+                            dim3(kChunkWaves * kWave), 0, s, f, a.newlens, ws, (const int*)nwork, n0, Ns, ly.slots, 0);
             const int ntiles = (Ns + Tile<G>::QT - 1) / Tile<G>::QT;
             HILS_LAUNCH("k_pp_local", (k_pp_local<T, D, G>), dim3((unsigned)(bg * ntiles)), dim3(kLocalWaves * kWave), 0,
                         s, f, a.newlens, (const float2*)ws.rec_s, (const char*)ws.rec_o, n0, Ns, cus);
@@ -909,8 +1152,8 @@ struct Run {
 
 }  // namespace
 
-size_t prefill_paged_workspace_bytes(int B, int Hq, int Hkv, int N, int L, int d, int K, int bf16) {
-    return layout(B, Hq, Hkv, N, L, d, K, bf16).total;
+size_t prefill_paged_workspace_bytes(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf16) {
+    return layout(B, Hq, Hkv, N, L, d, K, W, bf16).total;
 }
 
 hipError_t launch_prefill_paged(const PrefillPagedArgs& a, hipStream_t s) {
