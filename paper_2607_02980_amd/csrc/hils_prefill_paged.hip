@@ -44,6 +44,7 @@ namespace {
 constexpr int score_waves(bool bf16) { return bf16 ? 8 : 4; }
 constexpr int kScoreRows = 16 * score_waves(true);
 constexpr int kScoreCand = 64;                // candidates of a staged landmark block
+constexpr int kScoreSlice = 2048;             // candidates of a workgroup, at most
 constexpr int kSelWaves = 4;
 constexpr int kChunkWaves = 4;
 // Rows of a work item, at most.  f32: 128 columns, as 16 of them take a wave 3 us (an item of 64 rows x 8 heads
@@ -288,8 +289,9 @@ struct Layout {
     size_t max_work;
 };
 
-// sigma of a block of rows: as many as fit the last-level cache, in whole score tiles
-constexpr size_t kSigmaBytes = size_t(128) << 20;
+// sigma of a block of rows, in whole score tiles (4096 rows over 131K, 270 MB: in one block 121 us of scores and 88 of
+// selection; in two of 135 MB, which stay in the last-level cache, 137 and 96; in three 156 and 105).
+constexpr size_t kSigmaBytes = size_t(512) << 20;
 
 // Calls of so many records or fewer, those of the windows' pieces among them, take the windows as
 // work items too (k_pp_join instead of k_pp_local, whose workgroups, each with all blocks of its rows' windows one
@@ -310,7 +312,9 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf1
     size_t ns = N;
     if (ns * per_row > cap) ns = std::min<size_t>(N, std::max<size_t>(kScoreRows, cap / per_row / kScoreRows * kScoreRows));
     size_t rs = kSigmaBytes / (bg * nC * sizeof(float)) / kScoreRows * kScoreRows;
-    rs = std::min(ns, std::max<size_t>(rs, kScoreRows));
+    rs = std::max<size_t>(rs, kScoreRows);
+    const size_t parts = (ns + rs - 1) / rs;  // as equal as whole tiles allow
+    rs = std::min(ns, (ns + parts * kScoreRows - 1) / (parts * kScoreRows) * kScoreRows);
     w.Ns = (int)ns;
     w.Rs = (int)rs;
     w.max_work = bg * (std::min(nC, ns * K) + ns * K / seg_rows(bf16, Hq / Hkv));
@@ -341,17 +345,18 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf1
 // landmark rows of one head at a time come through LDS (double-buffered) and serve all rows;
 // the maximum over the heads stays in registers until a block of candidates is done.  It also
 // clears the words that the next launches count in.
-template <typename T, int D, int G>
-__global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave) void k_pp_score(FwdArgs f, const int32_t* newlens,
+template <typename T, int D, int G, int RT>
+__global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave, sizeof(T) == 2 && RT * G * D <= 512 ? 4 : 1) void k_pp_score(FwdArgs f, const int32_t* newlens,
                                                                                  float* sigma, int r0, int Rs, int slice,
                                                                                  int nslices, int* counts, size_t nclear) {
     using C = Cfg<T, D>;
-    constexpr int NW = score_waves(C::ES == 2), NT = NW * kWave, ROWS = 16 * NW;
+    constexpr int NW = score_waves(C::ES == 2), NT = NW * kWave, WROWS = 16 * RT, ROWS = WROWS * NW;
     constexpr int PPT = kScoreCand * D * C::ES / 16 / NT;
     constexpr bool kHold = C::ES == 2;  // the query operands of all heads fit in registers
     static_assert(PPT >= 1 && PPT * NT * 16 == kScoreCand * D * C::ES, "landmark blocks split evenly over the threads");
     __shared__ __align__(16) char s_l[2][kScoreCand * C::KROW];
     __shared__ float s_b[2][kScoreCand];
+    __shared__ int s_pg[kScoreSlice];  // the candidates' pages: a step's loads do not wait for them
     const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave, lg = lane / 16;
     const int ntiles = (Rs + ROWS - 1) / ROWS;
     for (size_t i = (size_t)blockIdx.x * NT + tid; i < nclear; i += (size_t)gridDim.x * NT) counts[i] = 0;
@@ -371,32 +376,37 @@ __global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave) void k_pp_scor
     const bool shared_lmk = f.Hl != f.Hq;
     const int NH = shared_lmk ? 1 : G;
     const T* qr = as<T>(f.q_route ? f.q_route : f.q);
-    const int qa = min(q0 + 16 * w + lane % 16, qend - 1);
-    auto q_operand = [&](int hh, int ks) {
+    auto q_operand = [&](int hh, int rt, int ks) {
+        const int qa = min(q0 + WROWS * w + 16 * rt + lane % 16, qend - 1);
         return ld16(qr + (((size_t)b * f.Hq + g * G + hh) * f.N + qa) * D + ks * 4 * C::EP + lg * C::EP);
     };
-    uint4 aq[kHold ? G : 2][C::KS];
+    uint4 aq[kHold ? G : 2][RT][C::KS];
     if constexpr (kHold) {
 #pragma unroll
         for (int hh = 0; hh < G; ++hh)
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) aq[hh][ks] = q_operand(hh, ks);
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int ks = 0; ks < C::KS; ++ks) aq[hh][rt][ks] = q_operand(hh, rt, ks);
     }
     struct Regs {
         uint4 x[PPT];
         float bv;
     };
+    const int nsteps = (c_end - c_beg + kScoreCand - 1) / kScoreCand * NH;
     // step t: candidate block t / NH, landmark head t % NH
+    for (int i = tid; i < c_end - c_beg; i += NT) s_pg[i] = (int)page_of(f, b, c_beg + i);
+    __syncthreads();
     auto fetch = [&](int t) {
-        const int hl = shared_lmk ? g : g * G + t % NH, c0 = c_beg + (t / NH) * kScoreCand;
+        t = min(t, nsteps - 1);
+        const int hl = shared_lmk ? g : g * G + t % NH, c0 = (t / NH) * kScoreCand, last = c_end - c_beg - 1;
         Regs r;
 #pragma unroll
         for (int u = 0; u < PPT; ++u) {
             const int e = tid + u * NT, j = e / (D / C::EP), d0 = (e % (D / C::EP)) * C::EP;
-            const size_t pg = page_of(f, b, min(c0 + j, c_end - 1));
-            r.x[u] = ld16(as<T>(f.lmk) + (pg * f.Hl + hl) * D + d0);
+            r.x[u] = ld16(as<T>(f.lmk) + ((size_t)s_pg[min(c0 + j, last)] * f.Hl + hl) * D + d0);
         }
-        r.bv = f.bias && tid < kScoreCand ? f.bias[page_of(f, b, min(c0 + tid, c_end - 1)) * f.Hl + hl] : 0.f;
+        r.bv = f.bias && tid < kScoreCand ? f.bias[(size_t)s_pg[min(c0 + tid, last)] * f.Hl + hl] : 0.f;
         return r;
     };
     auto store = [&](int buf, const Regs& r) {
@@ -408,28 +418,33 @@ __global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave) void k_pp_scor
         if (tid < kScoreCand) s_b[buf][tid] = r.bv;
     };
     const size_t bg = (size_t)b * f.Hkv + g;
-    const int nsteps = (c_end - c_beg + kScoreCand - 1) / kScoreCand * NH;
-    Regs nx = fetch(0);
-    store(0, nx);
-    __syncthreads();
-    f32x4 sg[4];
-    for (int t = 0; t < nsteps; ++t) {
+    f32x4 sg[RT][4];
+    // step t computes from buffer t % 2; the rows of the next two steps are in flight
+    auto step = [&](int t, const Regs& next, Regs& after) {
         const int buf = t & 1, lh = t % NH;
-        const bool more = t + 1 < nsteps;  // uniform
-        if (more) nx = fetch(t + 1);
+        after = fetch(t + 2);
         if (lh == 0)
 #pragma unroll
-            for (int nb = 0; nb < 4; ++nb) sg[nb] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        auto head = [&](const uint4 (&q)[C::KS]) {
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int nb = 0; nb < 4; ++nb) sg[rt][nb] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto head = [&](const uint4 (&q)[RT][C::KS]) {
 #pragma unroll
             for (int nb = 0; nb < 4; ++nb) {
-                f32x4 acc = zero4();
+                f32x4 acc[RT];
 #pragma unroll
-                for (int ks = 0; ks < C::KS; ++ks)
-                    acc = mma<T>(q[ks], lds16(&s_l[buf][(nb * 16 + lane % 16) * C::KROW + ks * 64 + lg * 16]), acc);
+                for (int rt = 0; rt < RT; ++rt) acc[rt] = zero4();
+#pragma unroll
+                for (int ks = 0; ks < C::KS; ++ks) {
+                    const uint4 x = lds16(&s_l[buf][(nb * 16 + lane % 16) * C::KROW + ks * 64 + lg * 16]);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) acc[rt] = mma<T>(q[rt][ks], x, acc[rt]);
+                }
                 const float bv = s_b[buf][nb * 16 + lane % 16];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sg[nb][i] = fmaxf(sg[nb][i], f.scale * acc[i] + bv);  // (a NaN loses)
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sg[rt][nb][i] = fmaxf(sg[rt][nb][i], f.scale * acc[rt][i] + bv);  // (a NaN loses)
             }
         };
         if constexpr (kHold) {
@@ -438,9 +453,11 @@ __global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave) void k_pp_scor
                 if (shared_lmk || hh == lh) head(aq[hh]);
         } else {
             // one head's operands at a time, the next one's in flight
-            auto load = [&](int hh, uint4 (&q)[C::KS]) {
+            auto load = [&](int hh, uint4 (&q)[RT][C::KS]) {
 #pragma unroll
-                for (int ks = 0; ks < C::KS; ++ks) q[ks] = q_operand(min(hh, G - 1), ks);
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int ks = 0; ks < C::KS; ++ks) q[rt][ks] = q_operand(min(hh, G - 1), rt, ks);
             };
             const int h0 = shared_lmk ? 0 : lh, h1 = shared_lmk ? G : lh + 1;
             load(h0, aq[0]);
@@ -457,14 +474,24 @@ __global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave) void k_pp_scor
             for (int nb = 0; nb < 4; ++nb) {
                 const int c = c_beg + (t / NH) * kScoreCand + nb * 16 + lane % 16;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int n = q0 + 16 * w + 4 * lg + i;
-                    if (n < qend && c < c_end) sigma[(bg * Rs + (n - r0)) * nC + c] = sg[nb][i];
-                }
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int n = q0 + WROWS * w + 16 * rt + 4 * lg + i;
+                        if (n < qend && c < c_end) sigma[(bg * Rs + (n - r0)) * nC + c] = sg[rt][nb][i];
+                    }
             }
         }
-        if (more) store(buf ^ 1, nx);
+        store(buf ^ 1, next);
         __syncthreads();
+    };
+    Regs ra = fetch(0), rb = fetch(1);
+    store(0, ra);
+    __syncthreads();
+    for (int t = 0; t < nsteps; t += 2) {
+        step(t, rb, ra);
+        if (t + 1 >= nsteps) break;
+        step(t + 1, ra, rb);
     }
 }
 
@@ -1092,16 +1119,26 @@ struct Run {
             for (int r0 = n0; r0 < n0 + Ns; r0 += ly.Rs) {
                 const int Rs = std::min(ly.Rs, n0 + Ns - r0);
                 if (!f.given_idx && maxc > 0) {
-                    // slices of candidates for a few workgroups per CU where there are few rows
-                    constexpr int waves = score_waves(sizeof(T) == 2);
-                    const size_t tiles = bg * ((Rs + 16 * waves - 1) / (16 * waves));
-                    const size_t want = std::max<size_t>(1, 4 * (size_t)cus / tiles);
-                    const int blocks = (maxc + kScoreCand - 1) / kScoreCand;
-                    const int slice = kScoreCand * (int)((blocks + want - 1) / want);
-                    const int nslices = (maxc + slice - 1) / slice;
-                    HILS_LAUNCH("k_pp_score", (k_pp_score<T, D, G>), dim3((unsigned)(tiles * nslices)),
-                                dim3(waves * kWave), 0, s, f, a.newlens, ws.sigma, r0, Rs, slice, nslices,
-                                ws.counts, r0 == n0 ? ncount + 1 : 0);
+                    // slices of candidates, so that the workgroups are one round of the chip
+                    auto score = [&](auto rt_tag) {
+                        constexpr int RT = decltype(rt_tag)::value, waves = score_waves(sizeof(T) == 2), rows = 16 * RT * waves;
+                        const size_t tiles = bg * ((Rs + rows - 1) / rows);
+                        const size_t want = std::max<size_t>(1, (2 / RT) * (size_t)cus / tiles);
+                        const int blocks = (maxc + kScoreCand - 1) / kScoreCand;
+                        const int slice = std::min(kScoreSlice, kScoreCand * (int)((blocks + want - 1) / want));
+                        const int nslices = (maxc + slice - 1) / slice;
+                        HILS_LAUNCH("k_pp_score", (k_pp_score<T, D, G, RT>), dim3((unsigned)(tiles * nslices)),
+                                    dim3(waves * kWave), 0, s, f, a.newlens, ws.sigma, r0, Rs, slice, nslices, ws.counts,
+                                    r0 == n0 ? ncount + 1 : 0);
+                    };
+                    // two row tiles per wave, each landmark operand feeding two products, where the heads' queries
+                    // just fill the registers (4096 rows over 131K, groups of 4: 142 -> 121 us; groups of 2
+                    // spill for no gain: 24 -> 43 us for 4 x 1500 rows over 8000)
+                    constexpr int kTwo = sizeof(T) == 2 && G * D == 512 ? 2 : 1;
+                    if (Rs > 16 * score_waves(sizeof(T) == 2))
+                        score(std::integral_constant<int, kTwo>{});
+                    else
+                        score(std::integral_constant<int, 1>{});
                 }
                 const dim3 grid((unsigned)((bg * Rs + kSelWaves - 1) / kSelWaves));
                 auto select = [&](auto e_tag) {
@@ -1113,6 +1150,8 @@ struct Run {
                     select(std::integral_constant<int, 1>{});
                 else if (maxc <= 4 * kWave)
                     select(std::integral_constant<int, 4>{});
+                else if (maxc <= 16 * kWave)
+                    select(std::integral_constant<int, 16>{});
                 else
                     select(std::integral_constant<int, 16>{});
             }
