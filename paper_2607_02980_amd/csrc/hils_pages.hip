@@ -17,7 +17,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPlan = 1024;             // threads of the one workgroup that plans
 constexpr int kPlanWaves = kPlan / kWave;
-constexpr int kPer = 16;                // pages of a thread per step of a scan over the pool
+constexpr int kPer = 16, kFewPer = 4;   // pages of a thread per step of a scan over the pool (small pools: few)
 constexpr size_t kSlice = 16 * 1024;    // bytes of a page that a workgroup copies at a time
 constexpr int kPools = 16;              // pools of one copying launch
 
@@ -60,16 +60,37 @@ __global__ __launch_bounds__(kThreads) void k_cache_copy_state(const int32_t* ta
 // One workgroup.  First what every sequence needs: a copy of the page that its first new token
 // goes to, if others have it too, and a page for every chunk that begins; then, if the
 // pool holds as many, the free pages by index, the r-th for the sequence whose range of needs
-// r lies in.  copied[b] holds (source or state, first need) meanwhile.
+// r lies in.  A chain of dependent steps, so what they exchange is in LDS: per sequence a state and where its
+// needs begin (more than kLdsSeqs sequences: in `copied`).  64 sequences, 992 pages: 14 us with all of it in
+// memory, XX now.
 constexpr int kNone = -1, kNew = -2;  // no page to copy; (kNew: the entry names no page, a fresh one takes its place)
+constexpr int kLdsSeqs = 2048;
+constexpr size_t kSmallState = 16 * 1024;  // entries of a table and counts that are copied on the way
 
-__global__ __launch_bounds__(kPlan) void k_cache_reserve(ReserveArgs a) {
+// The threads' free pages of a step: PER in a row each, as bits.
+template <int PER>
+__device__ __forceinline__ unsigned free_bits(const int32_t* refs, int P, int p0) {
+    unsigned bits = 0;
+    int r[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) r[i] = refs[min(p0 + i, P - 1)];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) bits |= (unsigned)(p0 + i < P && r[i] <= 0) << i;
+    return bits;
+}
+
+template <bool LDS, int PER>
+__global__ __launch_bounds__(kPlan) void k_cache_reserve(ReserveArgs a, size_t nt, size_t np) {
     __shared__ int s_sum[kPlanWaves];
+    __shared__ int s_state[LDS ? 2 * kLdsSeqs : 2], s_chunk[LDS ? kLdsSeqs : 1];  // s_chunk: the first need's chunk
     const int tid = threadIdx.x, C = a.L / kChunk;
+    int* st = LDS ? s_state : a.copied;  // st[2 b]: page to copy, or kNone, kNew, or -3 - a page of its own; st[2 b + 1]: needs before
     auto seq = [&](int b, int& len, int& start) {
         len = length_of(a.seqlens, b, a.L);
         start = len - min(a.newlens ? min(max(a.newlens[b], 0), a.N) : a.N, len);
     };
+    for (size_t i = tid; i < nt; i += kPlan) a.table_out[i] = a.table[i];
+    for (size_t i = tid; i < np; i += kPlan) a.refs_out[i] = a.refs[i];
     for (int b = tid; b < a.B; b += kPlan) {
         int len, start, src = kNone;
         seq(b, len, start);
@@ -77,18 +98,18 @@ __global__ __launch_bounds__(kPlan) void k_cache_reserve(ReserveArgs a) {
             src = a.table[(size_t)b * C + start / kChunk];
             if (src < 0 || src >= a.P) src = kNew;
         }
-        a.copied[2 * b] = src;
+        st[2 * b] = src;
     }
     __syncthreads();
-    // (the workgroup's own stores, visible to it after the barrier)
-    int base = 0;
+    const unsigned first_bits = free_bits<PER>(a.refs, a.P, tid * PER);
+    int total = 0;
     for (int b0 = 0; b0 < a.B; b0 += kPlan) {
         const int b = b0 + tid;
         int need = 0, src = kNone;
         if (b < a.B) {
             int len, start;
             seq(b, len, start);
-            src = a.copied[2 * b];
+            src = st[2 * b];
             if (src >= 0) {
                 // the first of the sequences that write to the page keeps it if no others have it
                 const int refs = a.refs[src];
@@ -96,35 +117,32 @@ __global__ __launch_bounds__(kPlan) void k_cache_reserve(ReserveArgs a) {
                 bool first = true;
                 if (refs > 1)
                     for (int o = 0; o < a.B; ++o) {
-                        const int x = a.copied[2 * o];
+                        const int x = st[2 * o];
                         const bool same = x == src || x == -3 - src;
                         writers += same;
                         first = first && !(same && o < b);
                     }
                 if (refs <= 1 || (first && writers >= refs)) src = -3 - src;  // its own
             }
-            need = chunks_of(len) - chunks_of(start) + (src >= 0 || src == kNew);
+            const bool replaced = src >= 0 || src == kNew;  // the page in use comes first
+            need = chunks_of(len) - chunks_of(start) + replaced;
+            if (LDS) s_chunk[b] = replaced ? start / kChunk : chunks_of(start);
         }
         int all;
-        const int before = block_scan(need, s_sum, all);
+        const int before = block_scan(need, s_sum, all);  // (its barriers are behind the loop over the others' states)
         if (b < a.B) {
-            if (src < kNew) a.copied[2 * b] = src;
-            a.copied[2 * b + 1] = base + before;
+            if (src < kNew) st[2 * b] = src;
+            st[2 * b + 1] = total + before;
         }
-        base += all;
+        total += all;
     }
-    __syncthreads();
-    const int total = base;
     // free pages, up to as many as are needed
-    int found = 0;
-    for (int p0 = 0; p0 < a.P && found < total; p0 += kPlan * kPer) {
-        int n = 0;
-        for (int i = 0; i < kPer; ++i) {
-            const int p = p0 + tid * kPer + i;
-            n += p < a.P && a.refs[p] <= 0;
-        }
+    int found = 0, first_before = 0;
+    for (int p0 = 0; p0 < a.P && found < total; p0 += kPlan * PER) {
+        const unsigned bits = p0 ? free_bits<PER>(a.refs, a.P, p0 + tid * PER) : first_bits;
         int all;
-        (void)block_scan(n, s_sum, all);
+        const int before = block_scan(__popc(bits), s_sum, all);
+        if (p0 == 0) first_before = before;
         found += all;
     }
     const bool enough = found >= total;
@@ -133,47 +151,51 @@ __global__ __launch_bounds__(kPlan) void k_cache_reserve(ReserveArgs a) {
         a.counts[1] = min(found, total);
     }
     if (!enough) {
+        __syncthreads();
         for (int b = tid; b < a.B; b += kPlan) a.copied[2 * b] = a.copied[2 * b + 1] = -1;
         return;
     }
+    __syncthreads();
     int given = 0;
-    for (int p0 = 0; p0 < a.P && given < total; p0 += kPlan * kPer) {
-        unsigned mine = 0;
-        for (int i = 0; i < kPer; ++i) {
-            const int p = p0 + tid * kPer + i;
-            mine |= (unsigned)(p < a.P && a.refs[p] <= 0) << i;
+    for (int p0 = 0; p0 < a.P && given < total; p0 += kPlan * PER) {
+        unsigned bits = first_bits;
+        int all = 0, r = first_before;
+        if (p0 || a.P > kPlan * PER) {
+            bits = free_bits<PER>(a.refs, a.P, p0 + tid * PER);
+            r = given + block_scan(__popc(bits), s_sum, all);
         }
-        int all;
-        int r = given + block_scan(__popc(mine), s_sum, all);
         given += all;
-        for (; mine && r < total; mine &= mine - 1, ++r) {
-            const int p = p0 + tid * kPer + __ffs(mine) - 1;
-            int lo = 0, hi = a.B - 1;  // the last sequence whose needs begin at or before r, of those that begin there
+        for (; bits && r < total; bits &= bits - 1, ++r) {
+            const int p = p0 + tid * PER + __ffs(bits) - 1;
+            int lo = 0, hi = a.B - 1;  // the last sequence whose needs begin at or before r
             while (lo < hi) {
                 const int mid = (lo + hi + 1) / 2;
-                if (a.copied[2 * mid + 1] <= r)
+                if (st[2 * mid + 1] <= r)
                     lo = mid;
                 else
                     hi = mid - 1;
             }
-            int len, start;
-            seq(lo, len, start);
-            const int src = a.copied[2 * lo];
-            const int k = r - a.copied[2 * lo + 1];
-            // the need's chunk: the page in use that is replaced comes first
-            const int c = (src >= 0 || src == kNew ? start / kChunk : chunks_of(start)) + k;
-            a.table_out[(size_t)lo * C + c] = p;
+            int c0;
+            if constexpr (LDS) {
+                c0 = s_chunk[lo];
+            } else {
+                int len, start;
+                seq(lo, len, start);
+                c0 = st[2 * lo] >= 0 || st[2 * lo] == kNew ? start / kChunk : chunks_of(start);
+            }
+            a.table_out[(size_t)lo * C + c0 + r - st[2 * lo + 1]] = p;
             a.refs_out[p] = 1;
         }
     }
     __syncthreads();
     for (int b = tid; b < a.B; b += kPlan) {
-        const int src = a.copied[2 * b];
+        const int src = st[2 * b];
         int len, start;
         seq(b, len, start);
         if (src >= 0) atomicSub(&a.refs_out[src], 1);
+        const int dst = src >= 0 ? a.table_out[(size_t)b * C + start / kChunk] : -1;
         a.copied[2 * b] = src >= 0 ? src : -1;
-        a.copied[2 * b + 1] = src >= 0 ? a.table_out[(size_t)b * C + start / kChunk] : -1;
+        a.copied[2 * b + 1] = dst;
     }
 }
 
@@ -193,7 +215,7 @@ struct CopyList {
     const int32_t* count;  // nullable: n_max
     int n_max, stride, map;
 };
-__global__ __launch_bounds__(kThreads) void k_cache_copy_pages(PoolList pools, CopyList list, int P) {
+__device__ __forceinline__ void copy_listed(const PoolList& pools, const CopyList& list, int P) {
     const int n = list.count ? min(*list.count, list.n_max) : list.n_max;
     const int per = pools.slices[pools.n];
     for (size_t u = blockIdx.x; u < (size_t)n * per; u += gridDim.x) {
@@ -218,6 +240,10 @@ __global__ __launch_bounds__(kThreads) void k_cache_copy_pages(PoolList pools, C
             for (size_t j = threadIdx.x; j < len; j += kThreads) y[j] = x[j];
         }
     }
+}
+
+__global__ __launch_bounds__(kThreads) void k_cache_copy_pages(PoolList pools, CopyList list, int P) {
+    copy_listed(pools, list, P);
 }
 
 // ---------------------------------------------------------------------------
@@ -289,34 +315,35 @@ __global__ __launch_bounds__(kPlan) void k_cache_free(FreeArgs a) {
 // One workgroup: n pages are in use; the i-th used page at or past n goes to the i-th free one
 // before it.  Both lists are as long, at most half of the pool: the free pages are listed in the
 // second half of `moved` until the pairs are made.
+template <int PER>
 __global__ __launch_bounds__(kPlan) void k_cache_compact(CompactArgs a) {
     __shared__ int s_sum[kPlanWaves];
     const int tid = threadIdx.x, half = (a.P + 1) / 2;
     int used = 0;
-    for (int p0 = 0; p0 < a.P; p0 += kPlan * kPer) {
-        int n = 0, all;
-        for (int i = 0; i < kPer; ++i) {
-            const int p = p0 + tid * kPer + i;
-            n += p < a.P && a.refs[p] > 0;
-        }
-        (void)block_scan(n, s_sum, all);
-        used += all;
+    for (int p0 = 0; p0 < a.P; p0 += kPlan * PER) {
+        int all;
+        (void)block_scan(__popc(free_bits<PER>(a.refs, a.P, p0 + tid * PER)), s_sum, all);
+        used += min(a.P - p0, kPlan * PER) - all;
     }
     int movers = 0, holes = 0;
-    for (int p0 = 0; p0 < a.P; p0 += kPlan * kPer) {
-        int r[kPer], n = 0, h = 0, all;
-        for (int i = 0; i < kPer; ++i) {
-            const int p = p0 + tid * kPer + i;
-            r[i] = p < a.P ? a.refs[p] : 0;
+    for (int p0 = 0; p0 < a.P; p0 += kPlan * PER) {
+        int r[PER], n = 0, h = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) r[i] = a.refs[min(p0 + tid * PER + i, a.P - 1)];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int p = p0 + tid * PER + i;
             n += p < a.P && p >= used && r[i] > 0;
             h += p < used && r[i] <= 0;
         }
-        int at = movers + block_scan(n, s_sum, all);
-        movers += all;
-        int to = holes + block_scan(h, s_sum, all);
-        holes += all;
-        for (int i = 0; i < kPer; ++i) {
-            const int p = p0 + tid * kPer + i;
+        int all;  // (both at once: a step has at most 2^14 of each)
+        const int before = block_scan(n << 16 | h, s_sum, all);
+        int at = movers + (before >> 16), to = holes + (before & 0xffff);
+        movers += all >> 16;
+        holes += all & 0xffff;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int p = p0 + tid * PER + i;
             if (p >= a.P) continue;
             a.new_page[p] = r[i] > 0 ? p : -1;
             if (a.refs_out != a.refs) a.refs_out[p] = max(r[i], 0);
@@ -339,7 +366,8 @@ __global__ __launch_bounds__(kPlan) void k_cache_compact(CompactArgs a) {
         a.counts[1] = movers;
     }
 }
-__global__ __launch_bounds__(kThreads) void k_cache_rename(CompactArgs a) {
+// The tables follow the pages, and (the first pools of) the pages move.
+__global__ __launch_bounds__(kThreads) void k_cache_move(CompactArgs a, PoolList pools, CopyList list) {
     const int C = a.L / kChunk;
     const size_t step = (size_t)gridDim.x * kThreads;
     for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < (size_t)a.B * C; i += step) {
@@ -347,37 +375,51 @@ __global__ __launch_bounds__(kThreads) void k_cache_rename(CompactArgs a) {
         const bool held = c < chunks_of(length_of(a.seqlens, b, a.L)) && p >= 0 && p < a.P;
         a.table_out[i] = held ? a.new_page[p] : p;
     }
+    copy_listed(pools, list, a.P);
 }
 
 unsigned blocks_for(size_t items, size_t per = kThreads, size_t most = 4096) {
     return (unsigned)std::max<size_t>(1, std::min(most, (items + per - 1) / per));
 }
 
+PoolList pool_list(const PoolArg* pools, int n) {
+    PoolList x;
+    x.n = n;
+    x.slices[0] = 0;
+    for (int k = 0; k < n; ++k) {
+        x.data[k] = static_cast<char*>(pools[k].data);
+        x.bytes[k] = pools[k].page_bytes;
+        x.slices[k + 1] = x.slices[k] + (int)((x.bytes[k] + kSlice - 1) / kSlice);
+    }
+    return x;
+}
+unsigned copy_blocks(const PoolList& x, const CopyList& list) {
+    return blocks_for((size_t)list.n_max * x.slices[x.n], 1, 8 * (size_t)device_cus());
+}
 void copy_pages(const PoolArg* pools, int num_pools, int P, const CopyList& list, hipStream_t s) {
-    for (int k0 = 0; k0 < num_pools; k0 += kPools) {
-        PoolList x;
-        x.n = std::min(kPools, num_pools - k0);
-        x.slices[0] = 0;
-        for (int k = 0; k < x.n; ++k) {
-            x.data[k] = static_cast<char*>(pools[k0 + k].data);
-            x.bytes[k] = pools[k0 + k].page_bytes;
-            x.slices[k + 1] = x.slices[k] + (int)((x.bytes[k] + kSlice - 1) / kSlice);
-        }
-        HILS_LAUNCH("k_cache_copy_pages", k_cache_copy_pages,
-                    dim3(blocks_for((size_t)list.n_max * x.slices[x.n], 1, 8 * (size_t)device_cus())), dim3(kThreads), 0, s,
-                    x, list, P);
+    for (int k = 0; k < num_pools; k += kPools) {
+        const PoolList x = pool_list(pools + k, std::min(kPools, num_pools - k));
+        HILS_LAUNCH("k_cache_copy_pages", k_cache_copy_pages, dim3(copy_blocks(x, list)), dim3(kThreads), 0, s, x, list, P);
     }
 }
 
 }  // namespace
 
 hipError_t launch_reserve(const ReserveArgs& a, const PoolArg* pools, int num_pools, hipStream_t s) {
-    const size_t nt = a.table_out != a.table ? (size_t)a.B * (a.L / kChunk) : 0;
-    const size_t np = a.refs_out != a.refs ? (size_t)a.P : 0;
-    if (nt + np)
+    size_t nt = a.table_out != a.table ? (size_t)a.B * (a.L / kChunk) : 0;
+    size_t np = a.refs_out != a.refs ? (size_t)a.P : 0;
+    const bool small = nt + np <= kSmallState;
+    if (!small)
         HILS_LAUNCH("k_cache_copy_state", k_cache_copy_state, dim3(blocks_for(std::max(nt, np))), dim3(kThreads), 0, s,
                     a.table, a.table_out, nt, a.refs, a.refs_out, np);
-    HILS_LAUNCH("k_cache_reserve", k_cache_reserve, dim3(1), dim3(kPlan), 0, s, a);
+    nt = small ? nt : 0;
+    np = small ? np : 0;
+    if (a.B > kLdsSeqs)
+        HILS_LAUNCH("k_cache_reserve", (k_cache_reserve<false, kPer>), dim3(1), dim3(kPlan), 0, s, a, nt, np);
+    else if (a.P > kFewPer * kPlan)
+        HILS_LAUNCH("k_cache_reserve", (k_cache_reserve<true, kPer>), dim3(1), dim3(kPlan), 0, s, a, nt, np);
+    else
+        HILS_LAUNCH("k_cache_reserve", (k_cache_reserve<true, kFewPer>), dim3(1), dim3(kPlan), 0, s, a, nt, np);
     copy_pages(pools, num_pools, a.P, CopyList{a.copied, a.copied + 1, nullptr, a.B, 2, 0}, s);
     return hipGetLastError();
 }
@@ -400,9 +442,16 @@ hipError_t launch_free(const FreeArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_compact(const CompactArgs& a, const PoolArg* pools, int num_pools, hipStream_t s) {
-    HILS_LAUNCH("k_cache_compact", k_cache_compact, dim3(1), dim3(kPlan), 0, s, a);
-    HILS_LAUNCH("k_cache_rename", k_cache_rename, dim3(blocks_for((size_t)a.B * (a.L / kChunk))), dim3(kThreads), 0, s, a);
-    copy_pages(pools, num_pools, a.P, CopyList{a.moved, a.new_page, a.counts + 1, a.P / 2, 1, 1}, s);
+    if (a.P > kFewPer * kPlan)
+        HILS_LAUNCH("k_cache_compact", k_cache_compact<kPer>, dim3(1), dim3(kPlan), 0, s, a);
+    else
+        HILS_LAUNCH("k_cache_compact", k_cache_compact<kFewPer>, dim3(1), dim3(kPlan), 0, s, a);
+    const CopyList list{a.moved, a.new_page, a.counts + 1, a.P / 2, 1, 1};
+    const int first = std::min(num_pools, kPools);
+    const PoolList x = pool_list(pools, first);
+    HILS_LAUNCH("k_cache_move", k_cache_move, dim3(std::max(blocks_for((size_t)a.B * (a.L / kChunk)), copy_blocks(x, list))),
+                dim3(kThreads), 0, s, a, x, list);
+    copy_pages(pools + first, num_pools - first, a.P, list, s);
     return hipGetLastError();
 }
 
