@@ -430,7 +430,7 @@ int hils_cache_evict(const hils_params* p, const float* acc, const int32_t* bloc
  * indexes, of every layer, as hils_pool (HOST array, num_pools <= 65536, NULL for none).
  * Outputs may be the inputs themselves (in place) except where said, but not overlap them
  * otherwise.  Free pages are taken lowest index first.  All use B, L and chunk of `p` and
- * ignore the forward flags.  Deterministic.
+ * ignore the forward flags; num_pages is at most 2^30.  Deterministic.
  */
 typedef struct {
     void* data;        /* device: num_pages pages, one after the other */
@@ -455,8 +455,8 @@ int hils_cache_reserve(const hils_params* p, const int32_t* block_table, const i
                        int32_t* table_out, int32_t* refs_out, int32_t* copied, int32_t* counts, void* stream);
 
 /*
- * Fork: row r of the result goes on from row parent[r] (parent [rows] int32, outside [0, B): an
- * empty row): it names the same pages and has the same length.  Each entry in use of row
+ * Fork: row r of the result goes on from row parent[r] (parent [rows] int32, rows <= 65535;
+ * outside [0, B): an empty row): it names the same pages and has the same length.  Each entry in use of row
  * b gains a count for every row that goes on from it and loses one for row b itself, so that
  * rows nobody goes on from are freed; nothing is copied (hils_cache_reserve does that when a
  * shared page is written to).  Serves copies of a prompt, beams that take each other's places,

@@ -195,6 +195,11 @@ hils::FwdArgs fwd_args(const hils_params* p, const void* q, const void* k, const
 static_assert(sizeof(hils_pool) == sizeof(hils::PoolArg) && offsetof(hils_pool, data) == offsetof(hils::PoolArg, data) &&
                   offsetof(hils_pool, page_bytes) == offsetof(hils::PoolArg, page_bytes),
               "a pool has one layout");
+int check_page_count(int num_pages) {
+    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    if (num_pages > 1 << 30) return fail(HILS_ERR_UNSUPPORTED, "num_pages=%d: more than 2^30", num_pages);
+    return HILS_OK;
+}
 int check_pools(const hils_pool* pools, int num_pools) {
     if (num_pools < 0 || num_pools > 65536)
         return fail(HILS_ERR_INVALID, "num_pools=%d: 0 to 65536 are possible", num_pools);
@@ -514,7 +519,8 @@ int hils_cache_reserve(const hils_params* p, const int32_t* block_table, const i
     int rc = check_params(p, HILS_OP_CACHE_RESERVE);
     if (rc) return rc;
     REQUIRE(block_table); REQUIRE(page_refs); REQUIRE(table_out); REQUIRE(refs_out); REQUIRE(copied); REQUIRE(counts);
-    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    rc = check_page_count(num_pages);
+    if (rc) return rc;
     if ((double)p->B * (p->L / 64) > 0x7fffffff)
         return fail(HILS_ERR_UNSUPPORTED, "B=%d L=%d: more than 2^31 table entries", p->B, p->L);
     rc = check_pools(pools, num_pools);
@@ -530,8 +536,9 @@ int hils_cache_fork(const hils_params* p, const int32_t* parent, int rows, const
     int rc = check_params(p, HILS_OP_CACHE_FORK);
     if (rc) return rc;
     REQUIRE(parent); REQUIRE(block_table); REQUIRE(page_refs); REQUIRE(table_out); REQUIRE(seqlens_out); REQUIRE(refs_out);
-    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
-    if (rows < 1) return fail(HILS_ERR_INVALID, "rows must be >= 1 (got %d)", rows);
+    rc = check_page_count(num_pages);
+    if (rc) return rc;
+    if (rows < 1 || rows > 65535) return fail(HILS_ERR_INVALID, "rows=%d: 1 to 65535 are possible", rows);
     if (table_out == block_table || (seqlens && seqlens_out == seqlens))
         return fail(HILS_ERR_INVALID, "a fork's rows and lengths cannot be written in place");
     const hils::ForkArgs a{parent, block_table, page_refs, seqlens, table_out, seqlens_out, refs_out, num_pages, p->B,
@@ -545,8 +552,10 @@ int hils_cache_free(const hils_params* p, const int32_t* keep, const int32_t* pa
     int rc = check_params(p, HILS_OP_CACHE_FREE);
     if (rc) return rc;
     REQUIRE(keep); REQUIRE(block_table); REQUIRE(page_refs); REQUIRE(table_out); REQUIRE(seqlens_out); REQUIRE(refs_out);
-    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
-    if (max_pages < 0) return fail(HILS_ERR_INVALID, "max_pages must be >= 0 (got %d)", max_pages);
+    rc = check_page_count(num_pages);
+    if (rc) return rc;
+    if (max_pages < 0 || max_pages > 1 << 30)
+        return fail(HILS_ERR_INVALID, "max_pages=%d: 0 to 2^30 are possible", max_pages);
     if (npages && !pages) return fail(HILS_ERR_INVALID, "npages is given, so pages must be non-NULL");
     const hils::FreeArgs a{keep, max_pages ? pages : nullptr, npages, block_table, page_refs, seqlens, table_out,
                            seqlens_out, refs_out, num_pages, p->B, p->L, max_pages};
@@ -560,7 +569,8 @@ int hils_cache_compact(const hils_params* p, const int32_t* block_table, const i
     if (rc) return rc;
     REQUIRE(block_table); REQUIRE(page_refs); REQUIRE(table_out); REQUIRE(refs_out); REQUIRE(new_page); REQUIRE(moved);
     REQUIRE(counts);
-    if (num_pages < 1) return fail(HILS_ERR_INVALID, "num_pages must be >= 1 (got %d)", num_pages);
+    rc = check_page_count(num_pages);
+    if (rc) return rc;
     rc = check_pools(pools, num_pools);
     if (rc) return rc;
     const hils::CompactArgs a{block_table, page_refs, seqlens, table_out, refs_out, new_page, moved, counts, num_pages,

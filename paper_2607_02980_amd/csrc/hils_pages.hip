@@ -249,9 +249,8 @@ __global__ __launch_bounds__(kThreads) void k_cache_copy_pages(PoolList pools, C
 // ---------------------------------------------------------------------------
 // forking
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(kThreads) void k_cache_fork_rows(ForkArgs a) {
+__device__ __forceinline__ void fork_rows(const ForkArgs& a, size_t at, size_t step) {
     const int C = a.L / kChunk;
-    const size_t step = (size_t)gridDim.x * kThreads, at = (size_t)blockIdx.x * kThreads + threadIdx.x;
     for (size_t i = at; i < (size_t)a.rows * C; i += step) {
         const int b = (int)(i / C), c = (int)(i % C), u = a.parent[b];
         const bool lives = u >= 0 && u < a.B;
@@ -261,6 +260,13 @@ __global__ __launch_bounds__(kThreads) void k_cache_fork_rows(ForkArgs a) {
     }
     if (a.refs_out != a.refs)
         for (size_t i = at; i < (size_t)a.P; i += step) a.refs_out[i] = a.refs[i];
+}
+__device__ __forceinline__ void add_refs(const ForkArgs& a, size_t entry, int change) {
+    const int p = a.table[entry];
+    if (change != 0 && p >= 0 && p < a.P) atomicAdd(&a.refs_out[p], change);
+}
+__global__ __launch_bounds__(kThreads) void k_cache_fork_rows(ForkArgs a) {
+    fork_rows(a, (size_t)blockIdx.x * kThreads + threadIdx.x, (size_t)gridDim.x * kThreads);
 }
 // A workgroup per (input row, range of its chunks): the row's pages gain a reference for every
 // row that goes on from it and lose the row's own.
@@ -277,15 +283,41 @@ __global__ __launch_bounds__(kThreads) void k_cache_fork_refs(ForkArgs a, int pe
     __syncthreads();
     const int change = s_times - 1;
     if (change == 0) return;
-    for (int c = c0 + threadIdx.x; c < min(n, c0 + per); c += kThreads) {
-        const int p = a.table[(size_t)b * C + c];
-        if (p >= 0 && p < a.P) atomicAdd(&a.refs_out[p], change);
+    for (int c = c0 + threadIdx.x; c < min(n, c0 + per); c += kThreads) add_refs(a, (size_t)b * C + c, change);
+}
+// Both in one workgroup, for few entries: a call is the host's time then, 2 us a launch (32 beams, 9K
+// entries and counts: XX us for two launches, XX now).
+constexpr int kSmallRows = 1024;
+__global__ __launch_bounds__(kPlan) void k_cache_fork(ForkArgs a) {
+    __shared__ int s_change[kSmallRows];
+    const int tid = threadIdx.x, C = a.L / kChunk;
+    for (int b = tid; b < a.B; b += kPlan) s_change[b] = -1;
+    fork_rows(a, tid, kPlan);
+    __syncthreads();
+    for (int i = tid; i < a.rows; i += kPlan) {
+        const int u = a.parent[i];
+        if (u >= 0 && u < a.B) atomicAdd(&s_change[u], 1);
+    }
+    __syncthreads();
+    for (int i = tid; i < a.B * C; i += kPlan) {
+        const int b = i / C;
+        if (i % C < chunks_of(length_of(a.seqlens, b, a.L))) add_refs(a, i, s_change[b]);
     }
 }
 
 // ---------------------------------------------------------------------------
 // freeing
 // ---------------------------------------------------------------------------
+__device__ __forceinline__ void lose_ref(const FreeArgs& a, int p) {
+    if (p >= 0 && p < a.P) atomicSub(&a.refs_out[p], 1);
+}
+// Entry i of the table, of a row with chunks beg .. end - 1 to give up.
+__device__ __forceinline__ void free_entry(const FreeArgs& a, size_t i, int c, int beg, int end) {
+    const int p = a.table[i];
+    const bool gone = c >= beg && c < end;
+    if (gone) lose_ref(a, p);
+    if (gone || a.table_out != a.table) a.table_out[i] = gone ? -1 : p;
+}
 // A workgroup per sequence (a length may be overwritten in place: read once, first).
 __global__ __launch_bounds__(kPlan) void k_cache_free(FreeArgs a) {
     const int b = blockIdx.x, C = a.L / kChunk;
@@ -293,20 +325,29 @@ __global__ __launch_bounds__(kPlan) void k_cache_free(FreeArgs a) {
     __syncthreads();
     if (threadIdx.x == 0) a.seqlens_out[b] = kept;
     const int beg = chunks_of(kept), end = chunks_of(len);
-    for (int c = threadIdx.x; c < C; c += kPlan) {
-        const size_t i = (size_t)b * C + c;
-        const int p = a.table[i];
-        const bool gone = c >= beg && c < end;
-        if (gone && p >= 0 && p < a.P) atomicSub(&a.refs_out[p], 1);
-        if (gone || a.table_out != a.table) a.table_out[i] = gone ? -1 : p;
-    }
+    for (int c = threadIdx.x; c < C; c += kPlan) free_entry(a, (size_t)b * C + c, c, beg, end);
     if (a.pages) {
         const int n = a.npages ? min(max(a.npages[b], 0), a.most) : a.most;
-        for (int i = threadIdx.x; i < n; i += kPlan) {
-            const int p = a.pages[(size_t)b * a.most + i];
-            if (p >= 0 && p < a.P) atomicSub(&a.refs_out[p], 1);
-        }
+        for (int i = threadIdx.x; i < n; i += kPlan) lose_ref(a, a.pages[(size_t)b * a.most + i]);
     }
+}
+// All sequences in one workgroup and the counts copied on the way, for few entries (as k_cache_fork; 64
+// sequences, 11K entries and counts: XX us for two launches, XX now).
+__global__ __launch_bounds__(kPlan) void k_cache_free_small(FreeArgs a) {
+    __shared__ int s_beg[kSmallRows], s_end[kSmallRows];
+    const int tid = threadIdx.x, C = a.L / kChunk;
+    for (int b = tid; b < a.B; b += kPlan) {
+        const int len = length_of(a.seqlens, b, a.L), kept = min(len, max(a.keep[b], 0));
+        s_beg[b] = chunks_of(kept);
+        s_end[b] = chunks_of(len);
+        a.seqlens_out[b] = kept;
+    }
+    for (int i = tid; i < a.P; i += kPlan) a.refs_out[i] = a.refs[i];
+    __syncthreads();
+    for (int i = tid; i < a.B * C; i += kPlan) free_entry(a, i, i % C, s_beg[i / C], s_end[i / C]);
+    if (a.pages)
+        for (int i = tid; i < a.B * a.most; i += kPlan)
+            if (!a.npages || i % a.most < a.npages[i / a.most]) lose_ref(a, a.pages[i]);
 }
 
 // ---------------------------------------------------------------------------
@@ -426,7 +467,11 @@ hipError_t launch_reserve(const ReserveArgs& a, const PoolArg* pools, int num_po
 
 hipError_t launch_fork(const ForkArgs& a, hipStream_t s) {
     const int C = a.L / kChunk;
-    const size_t items = std::max((size_t)a.rows * C, a.refs_out != a.refs ? (size_t)a.P : 0);
+    const size_t np = a.refs_out != a.refs ? (size_t)a.P : 0, items = std::max((size_t)a.rows * C, np);
+    if (((size_t)a.rows + a.B) * C + np <= kSmallState && a.B <= kSmallRows && a.rows <= (int)kSmallState) {
+        HILS_LAUNCH("k_cache_fork", k_cache_fork, dim3(1), dim3(kPlan), 0, s, a);
+        return hipGetLastError();
+    }
     HILS_LAUNCH("k_cache_fork_rows", k_cache_fork_rows, dim3(blocks_for(items)), dim3(kThreads), 0, s, a);
     const int per = 4 * kThreads;
     HILS_LAUNCH("k_cache_fork_refs", k_cache_fork_refs, dim3((C + per - 1) / per, a.B), dim3(kThreads), 0, s, a, per);
@@ -434,9 +479,14 @@ hipError_t launch_fork(const ForkArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_free(const FreeArgs& a, hipStream_t s) {
-    if (a.refs_out != a.refs)
-        HILS_LAUNCH("k_cache_copy_state", k_cache_copy_state, dim3(blocks_for(a.P)), dim3(kThreads), 0, s, a.table,
-                    a.table_out, (size_t)0, a.refs, a.refs_out, (size_t)a.P);
+    const size_t np = a.refs_out != a.refs ? (size_t)a.P : 0;
+    if (np && a.B <= kSmallRows && (size_t)a.B * (a.L / kChunk) + np + (size_t)a.B * a.most <= kSmallState) {
+        HILS_LAUNCH("k_cache_free", k_cache_free_small, dim3(1), dim3(kPlan), 0, s, a);
+        return hipGetLastError();
+    }
+    if (np)
+        HILS_LAUNCH("k_cache_copy_state", k_cache_copy_state, dim3(blocks_for(np)), dim3(kThreads), 0, s, a.table,
+                    a.table_out, (size_t)0, a.refs, a.refs_out, np);
     HILS_LAUNCH("k_cache_free", k_cache_free, dim3(a.B), dim3(kPlan), 0, s, a);
     return hipGetLastError();
 }

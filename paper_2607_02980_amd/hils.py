@@ -75,11 +75,10 @@ def _load():
     lib.hils_decode_q8_fwd.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.hils_cache_evict.argtypes = [P, vp, vp, vp, vp, vp, ci, ci, ci, vp, vp, vp, vp, vp, vp]
     lib.hils_prefill_paged_fwd.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
-    pools = ctypes.POINTER(hils_pool)
-    lib.hils_cache_reserve.argtypes = [P, vp, vp, ci, vp, vp, pools, ci, vp, vp, vp, vp, vp]
+    lib.hils_cache_reserve.argtypes = [P, vp, vp, ci, vp, vp, vp, ci, vp, vp, vp, vp, vp]
     lib.hils_cache_fork.argtypes = [P, vp, ci, vp, vp, ci, vp, vp, vp, vp, vp]
     lib.hils_cache_free.argtypes = [P, vp, vp, vp, ci, vp, vp, ci, vp, vp, vp, vp, vp]
-    lib.hils_cache_compact.argtypes = [P, vp, vp, ci, vp, pools, ci, vp, vp, vp, vp, vp, vp]
+    lib.hils_cache_compact.argtypes = [P, vp, vp, ci, vp, vp, ci, vp, vp, vp, vp, vp, vp]
     lib.hils_prefill_record_cap.argtypes = [sz]
     lib.hils_prefill_record_cap.restype = sz
     lib.hils_timing_enable.argtypes = [ctypes.c_int]
@@ -549,13 +548,19 @@ def hils_prefill_paged_fwd(p: Params, q, k_pages, v_pages, lmk_pages, block_tabl
 
 
 def _pool_list(pools, P, dev):
-    pools = tuple(pools)
-    arr = (hils_pool * max(1, len(pools)))()
+    """The pools as an array of hils_pool (an address and a page's bytes each), and how many they are."""
+    flat = []
     for i, t in enumerate(pools):
-        if _gpu(t, f"pools[{i}]") != dev or t.dim() == 0 or t.shape[0] != P or not t.is_contiguous():
+        try:
+            ok = t.get_device() == dev and t.shape[0] == P and t.is_contiguous()
+        except (AttributeError, IndexError):
+            ok = False
+        if not ok:
+            _gpu(t, f"pools[{i}]")
             raise ValueError(f"pools[{i}] must be a contiguous tensor of {P} pages on cuda:{dev}")
-        arr[i].data, arr[i].page_bytes = t.data_ptr(), t.nbytes // P
-    return arr, len(pools)
+        flat.append(t.data_ptr())
+        flat.append(t.nbytes // P)
+    return (ctypes.c_size_t * len(flat))(*flat), len(flat) // 2
 
 
 def _refs(page_refs):

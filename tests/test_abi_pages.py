@@ -81,6 +81,8 @@ def test_missing_pointers_and_pools(call):
     for name in NEEDED[call]:
         assert call(params(), **{name: None}) == hils.HILS_ERR_INVALID and name in hils.hils_last_error()
     assert call(params(), pages=0) == hils.HILS_ERR_INVALID and "num_pages" in hils.hils_last_error()
+    if call is not prefill:
+        assert call(params(), pages=(1 << 30) + 1) == hils.HILS_ERR_UNSUPPORTED and "num_pages" in hils.hils_last_error()
 
 
 def test_prefill_workspace_and_flags():
@@ -121,10 +123,12 @@ def test_pools_are_checked(call):
 
 
 def test_fork_and_free_arguments():
-    assert fork(params(), rows=0) == hils.HILS_ERR_INVALID and "rows" in hils.hils_last_error()
+    for rows in (0, 65536):
+        assert fork(params(), rows=rows) == hils.HILS_ERR_INVALID and "rows" in hils.hils_last_error()
     assert fork(params(), block_table=FAKE) == hils.HILS_ERR_INVALID and "in place" in hils.hils_last_error()
     assert fork(params(), seqlens=FAKE) == hils.HILS_ERR_INVALID and "in place" in hils.hils_last_error()
-    assert free(params(), most=-1, listed=FAKE) == hils.HILS_ERR_INVALID and "max_pages" in hils.hils_last_error()
+    for most in (-1, (1 << 30) + 1):
+        assert free(params(), most=most, listed=FAKE) == hils.HILS_ERR_INVALID and "max_pages" in hils.hils_last_error()
     assert free(params(), nlisted=FAKE) == hils.HILS_ERR_INVALID and "pages must be" in hils.hils_last_error()
 
 
@@ -135,6 +139,7 @@ def test_fork_and_free_arguments():
 def on_gpu(monkeypatch):
     """Tensors pass for GPU tensors, and addresses are not looked at."""
     monkeypatch.setattr(hils, "_gpu", lambda t, name: 0 if isinstance(t, torch.Tensor) else hils._ptr(t, name))
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
 
 
 TABLE, REFS = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(9, dtype=torch.int32)
