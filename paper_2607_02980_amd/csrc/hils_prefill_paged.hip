@@ -524,23 +524,33 @@ __global__ __launch_bounds__(kSelWaves * kWave) void k_pp_select(FwdArgs f, cons
     } else {
         const float* row = sigma + r * nC;
         int m = 0;
-        for (int c0 = 0; c0 < lim; c0 += E * kWave) {
-            float sc[E + 1];
-            int id[E + 1];
-            bool ok[E + 1];
+        auto best = [&](auto e_tag) {
+            constexpr int EE = decltype(e_tag)::value;
+            for (int c0 = 0; c0 < lim; c0 += EE * kWave) {
+                float sc[EE + 1];
+                int id[EE + 1];
+                bool ok[EE + 1];
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                id[e] = c0 + e * kWave + lane;
-                ok[e] = id[e] < lim;
-                sc[e] = ok[e] ? row[id[e]] : 0.f;
+                for (int e = 0; e < EE; ++e) {
+                    id[e] = c0 + e * kWave + lane;
+                    ok[e] = id[e] < lim;
+                    sc[e] = ok[e] ? row[id[e]] : 0.f;
+                }
+                ok[EE] = lane < m;
+                sc[EE] = ok[EE] ? s_osc[w][lane] : 0.f;
+                id[EE] = ok[EE] ? s_oid[w][lane] : -1;
+                m = wave_topk_reg<EE + 1, EE>(sc, id, ok, f.K, s_oid[w], s_osc[w], s_tid[w], s_tsc[w]);
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
-            ok[E] = lane < m;
-            sc[E] = ok[E] ? s_osc[w][lane] : 0.f;
-            id[E] = ok[E] ? s_oid[w][lane] : -1;
-            m = wave_topk_reg<E + 1, E>(sc, id, ok, f.K, s_oid[w], s_osc[w], s_tid[w], s_tsc[w]);
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        }
+        };
+        // (the row's own candidates may be far fewer than the call's)
+        if (E >= 4 && lim <= kWave)
+            best(std::integral_constant<int, 1>{});
+        else if (E >= 16 && lim <= 4 * kWave)
+            best(std::integral_constant<int, 4>{});
+        else
+            best(std::integral_constant<int, E>{});
         if (lane < m) c = s_oid[w][lane];
         if (lane < f.K) orow[lane] = c;
     }
