@@ -501,60 +501,90 @@ __global__ __launch_bounds__(256) void k_pp_clear(int* p, size_t n) {
 
 // One wave per row: the K best of its candidates (E registers of 64 at a time, the best so far
 // beside them), or the valid entries of a given selection; each counts the row for its chunk.
-template <int E>
-__global__ __launch_bounds__(kSelWaves * kWave) void k_pp_select(FwdArgs f, const int32_t* newlens, const float* sigma,
-                                                                int* counts, int* ranks, int n0, int Ns, int r0,
-                                                                int Rs) {
-    __shared__ int s_tid[kSelWaves][kWave];
-    __shared__ __align__(16) float s_tsc[kSelWaves][kWave];
-    __shared__ int s_oid[kSelWaves][kWave];
-    __shared__ float s_osc[kSelWaves][kWave];
-    const int w = wave_id(), lane = threadIdx.x % kWave;
-    const size_t r = (size_t)blockIdx.x * kSelWaves + w;
-    if (r >= (size_t)f.B * f.Hkv * Rs) return;  // whole wave
-    const size_t bg = r / Rs;
-    const int b = (int)(bg / f.Hkv), n = r0 + (int)(r % Rs);
+// MANY: a workgroup of 16 waves takes 64 rows of a (b, g) and counts in LDS first, with one atomic per
+// chunk that any of them chose, which pays where many rows share a counter: K = 16, 4096 rows over
+// 1000 tokens (820 entries a chunk) 157 us without, 30 with; over 16000 (209) 148 and 45; over 64000 (61) 87
+// and 78; over 131K (31) 85 and 112.
+constexpr int kSelHist = 4096;  // chunks counted in LDS
+template <int E, bool MANY>
+__global__ __launch_bounds__((MANY ? 16 : kSelWaves) * kWave) void k_pp_select(FwdArgs f, const int32_t* newlens,
+                                                                              const float* sigma, int* counts,
+                                                                              int* ranks, int n0, int Ns, int r0,
+                                                                              int Rs) {
+    constexpr int NW = MANY ? 16 : kSelWaves, ROWS = MANY ? 64 : kSelWaves;
+    __shared__ int s_tid[NW][kWave];
+    __shared__ __align__(16) float s_tsc[NW][kWave];
+    __shared__ int s_oid[NW][kWave];
+    __shared__ float s_osc[NW][kWave];
+    extern __shared__ int s_cnt[];  // MANY: rows of each chunk, then where they begin
+    const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave, nC = f.L / kChunk;
+    const int tiles = (Rs + ROWS - 1) / ROWS, first = r0 + (int)(blockIdx.x % tiles) * ROWS;
+    const size_t bg = blockIdx.x / tiles;
+    const int b = (int)(bg / f.Hkv);
     const Seq sq = sequence(f, newlens, b);
-    if (n >= sq.fresh) return;
-    const int nC = f.L / kChunk, lim = n_candidates(sq.pos0 + n, f.W);
-    int32_t* orow = f.idx + (bg * f.N + n) * f.K;
-    int c = -1;
-    if (f.given_idx) {
-        if (lane < f.K && idx_entry_valid(orow, lane, lim)) c = orow[lane];
-    } else {
-        const float* row = sigma + r * nC;
-        int m = 0;
-        auto best = [&](auto e_tag) {
-            constexpr int EE = decltype(e_tag)::value;
-            for (int c0 = 0; c0 < lim; c0 += EE * kWave) {
-                float sc[EE + 1];
-                int id[EE + 1];
-                bool ok[EE + 1];
-#pragma unroll
-                for (int e = 0; e < EE; ++e) {
-                    id[e] = c0 + e * kWave + lane;
-                    ok[e] = id[e] < lim;
-                    sc[e] = ok[e] ? row[id[e]] : 0.f;
-                }
-                ok[EE] = lane < m;
-                sc[EE] = ok[EE] ? s_osc[w][lane] : 0.f;
-                id[EE] = ok[EE] ? s_oid[w][lane] : -1;
-                m = wave_topk_reg<EE + 1, EE>(sc, id, ok, f.K, s_oid[w], s_osc[w], s_tid[w], s_tsc[w]);
-                __builtin_amdgcn_wave_barrier();
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            }
-        };
-        // (the row's own candidates may be far fewer than the call's)
-        if (E >= 4 && lim <= kWave)
-            best(std::integral_constant<int, 1>{});
-        else if (E >= 16 && lim <= 4 * kWave)
-            best(std::integral_constant<int, 4>{});
-        else
-            best(std::integral_constant<int, E>{});
-        if (lane < m) c = s_oid[w][lane];
-        if (lane < f.K) orow[lane] = c;
+    const int end = min(min(first + ROWS, r0 + Rs), sq.fresh);
+    if (first >= end) return;
+    const int chunks = min(nC, n_candidates(sq.pos0 + end - 1, f.W));  // that any row may choose
+    if constexpr (MANY) {
+        for (int c = tid; c < chunks; c += NW * kWave) s_cnt[c] = 0;
+        __syncthreads();
     }
-    if (lane < f.K) ranks[(bg * Ns + (n - n0)) * f.K + lane] = c >= 0 ? atomicAdd(&counts[bg * nC + c], 1) : -1;
+    for (int n = first + w; n < end; n += NW) {
+        const int lim = n_candidates(sq.pos0 + n, f.W);
+        int32_t* orow = f.idx + (bg * f.N + n) * f.K;
+        int c = -1;
+        if (f.given_idx) {
+            if (lane < f.K && idx_entry_valid(orow, lane, lim)) c = orow[lane];
+        } else {
+            const float* row = sigma + (bg * Rs + (n - r0)) * nC;
+            int m = 0;
+            auto best = [&](auto e_tag) {
+                constexpr int EE = decltype(e_tag)::value;
+                for (int c0 = 0; c0 < lim; c0 += EE * kWave) {
+                    float sc[EE + 1];
+                    int id[EE + 1];
+                    bool ok[EE + 1];
+#pragma unroll
+                    for (int e = 0; e < EE; ++e) {
+                        id[e] = c0 + e * kWave + lane;
+                        ok[e] = id[e] < lim;
+                        sc[e] = ok[e] ? row[id[e]] : 0.f;
+                    }
+                    ok[EE] = lane < m;
+                    sc[EE] = ok[EE] ? s_osc[w][lane] : 0.f;
+                    id[EE] = ok[EE] ? s_oid[w][lane] : -1;
+                    m = wave_topk_reg<EE + 1, EE>(sc, id, ok, f.K, s_oid[w], s_osc[w], s_tid[w], s_tsc[w]);
+                    __builtin_amdgcn_wave_barrier();
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                }
+            };
+            // (the row's own candidates may be far fewer than the call's)
+            if (E >= 4 && lim <= kWave)
+                best(std::integral_constant<int, 1>{});
+            else if (E >= 16 && lim <= 4 * kWave)
+                best(std::integral_constant<int, 4>{});
+            else
+                best(std::integral_constant<int, E>{});
+            if (lane < m) c = s_oid[w][lane];
+            if (lane < f.K) orow[lane] = c;
+        }
+        if (lane < f.K)
+            ranks[(bg * Ns + (n - n0)) * f.K + lane] = c < 0 ? -1 : atomicAdd(MANY ? &s_cnt[c] : &counts[bg * nC + c], 1);
+        __builtin_amdgcn_wave_barrier();
+    }
+    if constexpr (MANY) {
+        __syncthreads();
+        for (int c = tid; c < chunks; c += NW * kWave) {
+            const int x = s_cnt[c];
+            s_cnt[c] = x ? atomicAdd(&counts[bg * nC + c], x) : 0;
+        }
+        __syncthreads();
+        for (int e = tid; e < (end - first) * f.K; e += NW * kWave) {
+            const int n = first + e / f.K, slot = e % f.K;
+            int& rank = ranks[(bg * Ns + (n - n0)) * f.K + slot];
+            if (rank >= 0) rank += s_cnt[f.idx[(bg * f.N + n) * f.K + slot]];
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -1155,11 +1185,16 @@ struct Run {
                     else
                         score(std::integral_constant<int, 1>{});
                 }
-                const dim3 grid((unsigned)((bg * Rs + kSelWaves - 1) / kSelWaves));
                 auto select = [&](auto e_tag) {
                     constexpr int E = decltype(e_tag)::value;
-                    HILS_LAUNCH("k_pp_select", k_pp_select<E>, grid, dim3(kSelWaves * kWave), 0, s, f, a.newlens,
-                                (const float*)ws.sigma, ws.counts, ws.ranks, n0, Ns, r0, Rs);
+                    if ((size_t)Rs * f.K >= 64 * (size_t)nC && Rs >= 64 && nC <= kSelHist)
+                        HILS_LAUNCH("k_pp_select", (k_pp_select<E, true>), dim3((unsigned)(bg * ((Rs + 63) / 64))),
+                                    dim3(16 * kWave), nC * sizeof(int), s, f, a.newlens, (const float*)ws.sigma, ws.counts,
+                                    ws.ranks, n0, Ns, r0, Rs);
+                    else
+                        HILS_LAUNCH("k_pp_select", (k_pp_select<E, false>),
+                                    dim3((unsigned)(bg * ((Rs + kSelWaves - 1) / kSelWaves))), dim3(kSelWaves * kWave), 0, s,
+                                    f, a.newlens, (const float*)ws.sigma, ws.counts, ws.ranks, n0, Ns, r0, Rs);
                 };
                 if (maxc <= kWave)
                     select(std::integral_constant<int, 1>{});
