@@ -84,8 +84,8 @@ __device__ __forceinline__ f32x4 mma(const uint4& a, const uint4& b, f32x4 c) {
 }
 
 // o += V^T P^T for the 64 keys of a V tile in LDS, P as the accumulators st of S^T hold it.  bf16:
-// the weights (unnormalised, at most 1) are rounded to bf16, 2^-9 of each, the type they are
-// multiplied in.
+// the weights (unnormalised, at most 1) are rounded to bf16, at most 2^-8 of each, the type they
+// are multiplied in.
 template <typename T, int D>
 __device__ __forceinline__ void add_pv(const char* s_v, const f32x4 (&st)[4], f32x4 (&o)[D / 16], int lane) {
     using C = Cfg<T, D>;
