@@ -300,6 +300,7 @@ constexpr size_t kSigmaBytes = size_t(512) << 20;
 // 70, 256 (200K) 89 and 97, 512 (400K) 118 and 117, 1024 (800K) 218 and 185; f32: 512 291 and 314, 1024
 // 565 and 497; f32, 16 heads in groups of 8, d = 64: 1024 (400K) 188 and 212.
 constexpr size_t kFewRecords = size_t(5) << 16;
+constexpr size_t kMaxRows = size_t(1) << 24;  // rows of a segment: a row and a slot in 31 bits, and their entries
 
 Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf16) {
     Layout w;
@@ -309,8 +310,8 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf1
     w.slots = w.few ? K + (int)pieces : K;
     const size_t rec = (bf16 ? 2 : 4) * (size_t)d + sizeof(float2), per_row = (size_t)B * Hq * w.slots * rec;
     const size_t cap = prefill_record_cap(0);
-    size_t ns = N;
-    if (ns * per_row > cap) ns = std::min<size_t>(N, std::max<size_t>(kScoreRows, cap / per_row / kScoreRows * kScoreRows));
+    size_t ns = std::min<size_t>(N, kMaxRows);
+    if (ns * per_row > cap) ns = std::min(ns, std::max<size_t>(kScoreRows, cap / per_row / kScoreRows * kScoreRows));
     size_t rs = kSigmaBytes / (bg * nC * sizeof(float)) / kScoreRows * kScoreRows;
     rs = std::max<size_t>(rs, kScoreRows);
     const size_t parts = (ns + rs - 1) / rs;  // as equal as whole tiles allow
@@ -1200,8 +1201,6 @@ struct Run {
                     select(std::integral_constant<int, 1>{});
                 else if (maxc <= 4 * kWave)
                     select(std::integral_constant<int, 4>{});
-                else if (maxc <= 16 * kWave)
-                    select(std::integral_constant<int, 16>{});
                 else
                     select(std::integral_constant<int, 16>{});
             }

@@ -565,8 +565,8 @@ def _pool_list(pools, P, dev):
 
 def _refs(page_refs):
     dev = _gpu(page_refs, "page_refs")
-    if page_refs.dim() != 1:
-        raise ValueError(f"page_refs has shape {tuple(page_refs.shape)}, expected one dimension")
+    if page_refs.dim() != 1 or not len(page_refs):
+        raise ValueError(f"page_refs has shape {tuple(page_refs.shape)}, expected one dimension of at least one page")
     return dev, page_refs.shape[0]
 
 

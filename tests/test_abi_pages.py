@@ -108,6 +108,16 @@ def test_prefill_workspace_grows_with_batch_rows_and_cache():
         hils.hils_prefill_record_cap(before)
 
 
+def test_prefill_segments_keep_a_row_and_a_slot_in_31_bits():
+    size = lambda rows: hils.hils_workspace_size(  # noqa: E731
+        params(B=1, Hq=1, Hkv=1, N=rows, L=1 << 26, topk=1), hils.HILS_OP_PREFILL_PAGED)
+    before = hils.hils_prefill_record_cap(1 << 40)
+    try:
+        assert size(1 << 23) < size(1 << 24) == size(1 << 25) == size(3 << 24)
+    finally:
+        hils.hils_prefill_record_cap(before)
+
+
 def test_workspace_of_the_page_operators_is_none():
     for op in range(hils.HILS_OP_CACHE_RESERVE, hils.HILS_OP_CACHE_COMPACT + 1):
         assert hils.hils_workspace_size(params(flags=hils.HILS_FLAG_GIVEN_IDX), op) == 0
@@ -170,3 +180,9 @@ def test_dimensions_of_the_binding(on_gpu):
         hils.hils_prefill_paged_fwd(params(), torch.zeros(1), 7, 7, 7, TABLE)
     with pytest.raises(ValueError, match="needs idx"):
         hils.hils_prefill_paged_fwd(params(flags=1), torch.zeros(1), torch.zeros(4), 7, 7, TABLE, out=REFS, lse=REFS)
+
+
+@pytest.mark.parametrize("fn", ["hils_cache_reserve", "hils_cache_compact"])
+def test_a_pool_without_pages_is_refused(on_gpu, fn):
+    with pytest.raises(ValueError, match="page_refs"):
+        getattr(hils, fn)(params(), TABLE, REFS[:0], [torch.zeros(0, 2)])
