@@ -237,19 +237,21 @@ struct Record {
 template <typename T, int D, int NR>
 __device__ __forceinline__ void add_records(const Record<T, D> (&r)[NR], const float2 (&sv)[NR], const bool (&valid)[NR],
                                             f32x4 (&o)[D / 16], float& m, float& l) {
+    // (s^ in log2 units is -inf for a bias of the lowest value too, whose weight is 0 beside any token of the window)
+    float s[NR], mnew = m;
     bool ok[NR];
-    float mnew = m;
 #pragma unroll
     for (int u = 0; u < NR; ++u) {
-        ok[u] = valid[u] && sv[u].x != -INFINITY;  // (a masked chunk's record may hold anything)
-        mnew = ok[u] ? fmaxf(mnew, sv[u].x * kLog2e) : mnew;
+        s[u] = sv[u].x * kLog2e;
+        ok[u] = valid[u] && s[u] != -INFINITY;  // (a masked chunk's record may hold anything)
+        mnew = ok[u] ? fmaxf(mnew, s[u]) : mnew;
     }
     float rs = mnew == m ? 1.f : fexp2(m - mnew);
     m = mnew;
     l *= rs;
 #pragma unroll
     for (int u = 0; u < NR; ++u) {
-        const float wk = ok[u] ? fexp2(sv[u].x * kLog2e - m) : 0.f;
+        const float wk = ok[u] ? fexp2(s[u] - m) : 0.f;
         l += wk;
         r[u].add(o, rs, ok[u] ? wk * sv[u].y : 0.f, ok[u]);
         rs = 1.f;
@@ -1084,15 +1086,16 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void k_pp_join(FwdArgs f, const
         float mnew = m;
 #pragma unroll
         for (int u = 0; u < SB; ++u) {
-            ok[u] = ok[u] && sv[u].x != -INFINITY;  // (a masked chunk's record may hold anything)
-            mnew = ok[u] ? fmaxf(mnew, sv[u].x * kLog2e) : mnew;
+            sv[u].x *= kLog2e;
+            ok[u] = ok[u] && sv[u].x != -INFINITY;  // (as in add_records)
+            mnew = ok[u] ? fmaxf(mnew, sv[u].x) : mnew;
         }
         float rs = mnew == m ? 1.f : fexp2(m - mnew);
         m = mnew;
         l *= rs;
 #pragma unroll
         for (int u = 0; u < SB; ++u) {
-            const float wk = ok[u] ? fexp2(sv[u].x * kLog2e - m) : 0.f, wu = ok[u] ? wk * sv[u].y : 0.f;
+            const float wk = ok[u] ? fexp2(sv[u].x - m) : 0.f, wu = ok[u] ? wk * sv[u].y : 0.f;
             l += wk;
 #pragma unroll
             for (int t = 0; t < PCS; ++t) {

@@ -49,6 +49,56 @@ def test_windows_over_everything(dtype):
     w.check(got, rows=some(w))
 
 
+# enough workgroups that some of sequence 1's take the records first, the window after them
+ORDERS = {t: dict(B=2, Hq=32, Hkv=4, N=1100, L=2560, d=64, topk=4, window=100, dtype=t) for t in ("bf16", "f32")}
+
+
+def two_orders(dtype, **opt):
+    return World(hils_().Params(**ORDERS[dtype]), [2500, 2533], [1100, 1090], 31, **opt)
+
+
+ORDER_ROWS = [(b, n) for b in range(2) for n in (0, 17, 255, 400, 640, 801, 1000, 1089)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_records_before_and_after_the_window(dtype):
+    w = two_orders(dtype, bias=True)
+    w.check(w.run(), rows=ORDER_ROWS)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinite_values_of_later_tokens_in_either_order(dtype):
+    w = two_orders(dtype)
+    clean = w.run()
+    for row in (101, 700):
+        at = 2533 - 1090 + row
+        w.v[w.table[1, at // 64], 0, at % 64, 3] = np.inf
+    got = w.run()
+    bound = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -20  # (as above)
+    assert ((got[0][1, :, :101] - clean[0][1, :, :101]).float().abs() <= bound * 4).all()
+    assert torch.isfinite(got[0][1, :8, 300:700][..., :3].float()).all()
+    assert not torch.isfinite(got[0][1, :8, [101, 700], 3]).any()
+    assert torch.equal(got[0][1, 8:], clean[0][1, 8:])
+
+
+@pytest.mark.parametrize("case", ["few", "few_f32", "bf16", "f32"])
+def test_biases_of_the_lowest_value(case):
+    """Every chunk hidden from all or half of the heads by a bias of float32's lowest value: no weight, as -inf."""
+    if case in ORDERS:
+        w, rows = two_orders(case, bias=True), ORDER_ROWS
+    else:
+        kw = dict(SHAPES["g4_f32" if case == "few_f32" else "g4_bf16"], N=40)
+        w, rows = World(hils_().Params(**kw), [2533, 777], [40, 33], 7, bias=True), [(0, 0), (0, 39), (1, 0), (1, 32)]
+    w.bias[:, ::2] = -np.inf
+    w.bias[w.table[1, 3:w.len[1] // 64]] = -np.inf
+    w.check(w.run(), rows=rows)
+    w.bias[np.isneginf(w.bias)] = np.finfo(np.float32).min
+    got = w.run()
+    w.check(got, rows=rows)
+    for b in range(2):
+        assert all(torch.isfinite(x[b, :, :w.fresh[b]].float()).all() for x in got[:2])
+
+
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("name", SHAPES)
 def test_later_tokens_do_not_reach_earlier_rows(name, value):
