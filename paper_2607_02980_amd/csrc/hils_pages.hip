@@ -231,8 +231,11 @@ __device__ __forceinline__ void copy_listed(const PoolList& pools, const CopyLis
         const char* x = pools.data[k] + (size_t)src * bytes + at;
         char* y = pools.data[k] + (size_t)dst * bytes + at;
         if ((((size_t)pools.data[k] | bytes) & 15) == 0) {
+            // (non-temporal stores leave the caches to the reads: 350 pages of 270 KB 47.5 -> 39.3 us a call; the loads
+            // too: 42.5, the loads alone: 39.8)
+            typedef int v4i __attribute__((ext_vector_type(4)));
             for (size_t j = threadIdx.x; j < len / 16; j += kThreads)
-                reinterpret_cast<uint4*>(y)[j] = reinterpret_cast<const uint4*>(x)[j];
+                __builtin_nontemporal_store(reinterpret_cast<const v4i*>(x)[j], reinterpret_cast<v4i*>(y) + j);
         } else if ((((size_t)pools.data[k] | bytes) & 3) == 0) {
             for (size_t j = threadIdx.x; j < len / 4; j += kThreads)
                 reinterpret_cast<uint32_t*>(y)[j] = reinterpret_cast<const uint32_t*>(x)[j];
