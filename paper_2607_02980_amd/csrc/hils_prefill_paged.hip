@@ -8,7 +8,8 @@
 //   k_pp_select   the K best of each row (exact radix select, ties to the smaller chunk); each
 //                 chosen chunk counts the row and gives it a rank
 //   k_pp_plan     per (b, g): where each chunk's rows start, and the work items
-//   k_pp_fill     the rows of every chunk, by offset and rank (few rows: k_pp_plan does it)
+//   k_pp_fill     the rows of every chunk, by offset and rank (few rows: k_pp_plan does it; very
+//                 few: k_pp_select does the work of both)
 //   k_pp_chunks   chunk-major: a chunk's K and V are read once and attended by all the rows that
 //                 chose it, 16 (row, head) columns at a time; o_c and s^ of every (row, slot,
 //                 head) go to the workspace as records
@@ -502,24 +503,59 @@ __global__ __launch_bounds__(256) void k_pp_clear(int* p, size_t n) {
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
 }
 
+// Exclusive prefix sum of pairs (rows, and work items in the upper half) over NW waves; `all` is the total.
+template <int NW>
+__device__ __forceinline__ unsigned long long scan_pairs(unsigned long long mine, unsigned long long* s_sum,
+                                                         unsigned long long& all) {
+    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
+    unsigned long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const unsigned long long y = __shfl_up(incl, o, kWave);
+        if (lane >= o) incl += y;
+    }
+    if (lane == kWave - 1) s_sum[w] = incl;
+    __syncthreads();
+    unsigned long long at = incl - mine;
+    all = 0;
+    for (int i = 0; i < NW; ++i) {
+        at += i < w ? s_sum[i] : 0;
+        all += s_sum[i];
+    }
+    return at;
+}
+__device__ __forceinline__ unsigned long long pair_of(int rows, int seg) {
+    return (unsigned long long)((rows + seg - 1) / seg) << 32 | (unsigned)rows;
+}
+
 // One wave per row: the K best of its candidates (E registers of 64 at a time, the best so far
 // beside them), or the valid entries of a given selection; each counts the row for its chunk.
-// MANY: a workgroup of 16 waves takes 64 rows of a (b, g) and counts in LDS first, with one atomic per
+// kMany: a workgroup of 16 waves takes 64 rows of a (b, g) and counts in LDS first, with one atomic per
 // chunk that any of them chose, which pays where many rows share a counter: K = 16, 4096 rows over
 // 1000 tokens (820 entries a chunk) 157 us without, 30 with; over 16000 (209) 148 and 45; over 64000 (61) 87
 // and 78; over 131K (31) 85 and 112.
+// kPlanToo: where a segment has so few rows that one such workgroup takes all of a (b, g), it goes on with
+// what is left for k_pp_plan and k_pp_fill otherwise, from the counts and ranks in LDS.  Whole calls, bf16, K = 16, with
+// k_pp_plan and so: 16 rows over 15 candidates 30.1 and 27.5 us, 64 41.9 and 41.1; 16 over 242 39.6 and 37.9, 33 47.1
+// and 48.2, 64 53.6 and 58.8 (one CU selects for all); 1 over 2040 34.9 and 33.0, 16 49.0 and 49.8.
 constexpr int kSelHist = 4096;  // chunks counted in LDS
-template <int E, bool MANY>
-__global__ __launch_bounds__((MANY ? 16 : kSelWaves) * kWave) void k_pp_select(FwdArgs f, const int32_t* newlens,
-                                                                              const float* sigma, int* counts,
-                                                                              int* ranks, int n0, int Ns, int r0,
-                                                                              int Rs) {
+enum Select { kPerRow, kMany, kPlanToo };
+constexpr int kPlanTooScores = 4096;  // of a (b, g), at most
+template <int E, Select MODE>
+__global__ __launch_bounds__((MODE != kPerRow ? 16 : kSelWaves) * kWave) void k_pp_select(FwdArgs f,
+                                                                                        const int32_t* newlens,
+                                                                                        const float* sigma, Ws ws,
+                                                                                        int* nwork, int n0, int Ns,
+                                                                                        int r0, int Rs, int seg) {
+    constexpr bool MANY = MODE != kPerRow;
     constexpr int NW = MANY ? 16 : kSelWaves, ROWS = MANY ? 64 : kSelWaves;
+    int *counts = ws.counts, *ranks = ws.ranks;
     __shared__ int s_tid[NW][kWave];
     __shared__ __align__(16) float s_tsc[NW][kWave];
     __shared__ int s_oid[NW][kWave];
     __shared__ float s_osc[NW][kWave];
     extern __shared__ int s_cnt[];  // MANY: rows of each chunk, then where they begin
+    int* s_ent = s_cnt + (MODE == kPlanToo ? f.L / kChunk : 0);  // kPlanToo: chunk << 6 | rank of a row's slot, or -1
     const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave, nC = f.L / kChunk;
     const int tiles = (Rs + ROWS - 1) / ROWS, first = r0 + (int)(blockIdx.x % tiles) * ROWS;
     const size_t bg = blockIdx.x / tiles;
@@ -571,11 +607,38 @@ __global__ __launch_bounds__((MANY ? 16 : kSelWaves) * kWave) void k_pp_select(F
             if (lane < m) c = s_oid[w][lane];
             if (lane < f.K) orow[lane] = c;
         }
-        if (lane < f.K)
-            ranks[(bg * Ns + (n - n0)) * f.K + lane] = c < 0 ? -1 : atomicAdd(MANY ? &s_cnt[c] : &counts[bg * nC + c], 1);
+        if (lane < f.K) {
+            const int rank = c < 0 ? -1 : atomicAdd(MANY ? &s_cnt[c] : &counts[bg * nC + c], 1);
+            if constexpr (MODE == kPlanToo)
+                s_ent[(n - first) * f.K + lane] = c < 0 ? -1 : c << 6 | rank;
+            else
+                ranks[(bg * Ns + (n - n0)) * f.K + lane] = rank;
+        }
         __builtin_amdgcn_wave_barrier();
     }
-    if constexpr (MANY) {
+    if constexpr (MODE == kPlanToo) {
+        __shared__ unsigned long long s_sum[NW];
+        __shared__ int s_base;
+        __syncthreads();
+        int rows0 = 0;
+        for (int c0 = 0; c0 < chunks; c0 += NW * kWave) {
+            const int c = c0 + tid, cnt = c < chunks ? s_cnt[c] : 0;
+            unsigned long long all;
+            const unsigned long long at = scan_pairs<NW>(pair_of(cnt, seg), s_sum, all);
+            if (tid == 0) s_base = atomicAdd(nwork, (int)(all >> 32));
+            __syncthreads();
+            const int row = rows0 + (int)(unsigned)at;
+            int item = s_base + (int)(at >> 32);
+            if (c < chunks) s_cnt[c] = row;
+            for (int k = 0; k < cnt; k += seg) ws.work[item++] = make_int4((int)bg, c, row + k, min(seg, cnt - k));
+            rows0 += (int)(unsigned)all;
+        }
+        __syncthreads();
+        for (int e = tid; e < (end - first) * f.K; e += NW * kWave) {
+            const int x = s_ent[e];
+            if (x >= 0) ws.list[bg * Ns * f.K + s_cnt[x >> 6] + (x & 63)] = (first - n0 + e / f.K) << 6 | e % f.K;
+        }
+    } else if constexpr (MANY) {
         __syncthreads();
         for (int c = tid; c < chunks; c += NW * kWave) {
             const int x = s_cnt[c];
@@ -615,7 +678,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_pp_plan(FwdArgs f, const int32
     constexpr int NW = kPlanThreads / kWave;
     __shared__ unsigned long long s_sum[NW];
     __shared__ int s_base;
-    const int bg = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, nC = f.L / kChunk;
+    const int bg = blockIdx.x, tid = threadIdx.x, nC = f.L / kChunk;
     const int* cnt = counts + (size_t)bg * nC;
     int rows0 = 0;
     for (int c0 = 0; c0 < nC; c0 += kPlanThreads * PER) {
@@ -625,21 +688,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_pp_plan(FwdArgs f, const int32
         for (int i = 0; i < PER; ++i) {
             const int c = c0 + tid * PER + i;
             n[i] = c < nC ? cnt[c] : 0;
-            mine += (unsigned long long)((n[i] + seg - 1) / seg) << 32 | (unsigned)n[i];
+            mine += pair_of(n[i], seg);
         }
-        unsigned long long incl = mine;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            const unsigned long long y = __shfl_up(incl, o, kWave);
-            if (lane >= o) incl += y;
-        }
-        if (lane == kWave - 1) s_sum[w] = incl;
-        __syncthreads();
-        unsigned long long at = incl - mine, all = 0;
-        for (int i = 0; i < NW; ++i) {
-            at += i < w ? s_sum[i] : 0;
-            all += s_sum[i];
-        }
+        unsigned long long all;
+        const unsigned long long at = scan_pairs<NW>(mine, s_sum, all);
         if (tid == 0) s_base = atomicAdd(nwork, (int)(all >> 32));
         __syncthreads();
         int row = rows0 + (int)(unsigned)at, item = s_base + (int)(at >> 32);
@@ -1160,8 +1212,10 @@ struct Run {
         const int nC = f.L / kChunk, maxc = n_candidates(f.L - 1, f.W);  // candidates of any row, at most
         const size_t bg = (size_t)f.B * f.Hkv, ncount = bg * nC;
         const int cus = device_cus(), seg = seg_rows(f.bf16, G);
+        int* nwork = ws.counts + ncount;
         for (int n0 = 0; n0 < f.N; n0 += ly.Ns) {
             const int Ns = std::min(ly.Ns, f.N - n0);
+            const bool plan_too = Ns <= 64 && nC <= kSelHist && Ns * maxc <= kPlanTooScores;
             if (f.given_idx && maxc > 0)
                 HILS_LAUNCH("k_pp_clear", k_pp_clear, dim3((unsigned)std::min<size_t>((ncount + 256) / 256, 4096)),
                             dim3(256), 0, s, ws.counts, ncount + 1);
@@ -1191,14 +1245,18 @@ struct Run {
                 }
                 auto select = [&](auto e_tag) {
                     constexpr int E = decltype(e_tag)::value;
-                    if ((size_t)Rs * f.K >= 64 * (size_t)nC && Rs >= 64 && nC <= kSelHist)
-                        HILS_LAUNCH("k_pp_select", (k_pp_select<E, true>), dim3((unsigned)(bg * ((Rs + 63) / 64))),
-                                    dim3(16 * kWave), nC * sizeof(int), s, f, a.newlens, (const float*)ws.sigma, ws.counts,
-                                    ws.ranks, n0, Ns, r0, Rs);
+                    auto launch = [&](auto mode_tag, int rows, int waves, size_t lds) {
+                        constexpr Select MODE = decltype(mode_tag)::value;
+                        HILS_LAUNCH("k_pp_select", (k_pp_select<E, MODE>), dim3((unsigned)(bg * ((Rs + rows - 1) / rows))),
+                                    dim3(waves * kWave), lds, s, f, a.newlens, (const float*)ws.sigma, ws, nwork, n0, Ns,
+                                    r0, Rs, seg);
+                    };
+                    if (plan_too)
+                        launch(std::integral_constant<Select, kPlanToo>{}, 64, 16, (nC + 64 * f.K) * sizeof(int));
+                    else if ((size_t)Rs * f.K >= 64 * (size_t)nC && Rs >= 64 && nC <= kSelHist)
+                        launch(std::integral_constant<Select, kMany>{}, 64, 16, nC * sizeof(int));
                     else
-                        HILS_LAUNCH("k_pp_select", (k_pp_select<E, false>),
-                                    dim3((unsigned)(bg * ((Rs + kSelWaves - 1) / kSelWaves))), dim3(kSelWaves * kWave), 0, s,
-                                    f, a.newlens, (const float*)ws.sigma, ws.counts, ws.ranks, n0, Ns, r0, Rs);
+                        launch(std::integral_constant<Select, kPerRow>{}, kSelWaves, kSelWaves, 0);
                 };
                 if (maxc <= kWave)
                     select(std::integral_constant<int, 1>{});
@@ -1207,9 +1265,8 @@ struct Run {
                 else
                     select(std::integral_constant<int, 16>{});
             }
-            int* nwork = ws.counts + ncount;
             const size_t most = bg * (std::min<size_t>(maxc, (size_t)Ns * f.K) + (size_t)Ns * f.K / seg);
-            if (maxc > 0) {
+            if (maxc > 0 && !plan_too) {
                 const bool fill = (size_t)Ns * f.K <= kPlanFill;
                 auto plan = [&](auto per_tag) {
                     constexpr int PER = decltype(per_tag)::value;
