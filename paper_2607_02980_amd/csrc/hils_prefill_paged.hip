@@ -4,9 +4,11 @@
 // is the prefill's (Eqs. (1), (9), (10)), with chunk c of sequence b in page block_table[b, c]:
 //
 //   k_pp_score    sigma_ic = max_h s^_hc of 128 rows of a KV group against a slice of the
-//                 candidates, on MFMA tiles; to the workspace, a block of rows at a time
-//   k_pp_select   the K best of each row (exact radix select, ties to the smaller chunk); each
-//                 chosen chunk counts the row and gives it a rank
+//                 candidates, on MFMA tiles; to the workspace, a block of rows at a time; where
+//                 candidates are many, with the maxima of blocks of 16
+//   k_pp_select   the K best of each row (exact radix select, ties to the smaller chunk; many
+//                 candidates: the best blocks first, then theirs); each chosen chunk counts the
+//                 row and gives it a rank
 //   k_pp_plan     per (b, g): where each chunk's rows start, and the work items
 //   k_pp_fill     the rows of every chunk, by offset and rank (few rows: k_pp_plan does it; very
 //                 few: k_pp_select does the work of both)
@@ -281,19 +283,24 @@ struct Ws {
     int* ranks;    // [bg][Ns][K] rank of a row among its chunk's, -1: no chunk
     int* list;     // [bg][Ns * K] row << 6 | slot
     int4* work;    // (bg, chunk, offset, rows)
-    float* sigma;  // [bg][Rs][nC]
+    float* sigma;  // [bg][Rs][nS], nS: nC in whole blocks
+    float* bmax;   // [bg][Rs][nS / kBlock] the maxima of its blocks
     float2* rec_s; // [bg][Ns][slots][G] s^ and the record's unit
     char* rec_o;   // [bg][Ns][slots][G] records
 };
 struct Layout {
-    size_t counts, offs, ranks, list, work, sigma, rec_s, rec_o, total;
+    size_t counts, offs, ranks, list, work, sigma, bmax, rec_s, rec_o, total;
     int Ns, Rs, slots;  // records of a (row, head)
     bool few;           // the windows' pieces among them
     size_t max_work;
 };
 
-// sigma of a block of rows, in whole score tiles (4096 rows over 131K, 270 MB: in one block 121 us of scores and 88 of
-// selection; in two of 135 MB, which stay in the last-level cache, 137 and 96; in three 156 and 105).
+// Scores of so many candidates in a row have their maximum beside them.
+constexpr int kBlock = 16;
+__host__ __device__ constexpr int score_stride(int nC) { return (nC + kBlock - 1) / kBlock * kBlock; }
+
+// sigma of a block of rows, in whole score tiles (4096 rows over 131K, 270 MB: in one block 123 us of scores and 65 of
+// selection; in two of 135 MB 143 and 72).
 constexpr size_t kSigmaBytes = size_t(512) << 20;
 
 // Calls of so many records or fewer, those of the windows' pieces among them, take the windows as
@@ -315,7 +322,8 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf1
     const size_t cap = prefill_record_cap(0);
     size_t ns = std::min<size_t>(N, kMaxRows);
     if (ns * per_row > cap) ns = std::min(ns, std::max<size_t>(kScoreRows, cap / per_row / kScoreRows * kScoreRows));
-    size_t rs = kSigmaBytes / (bg * nC * sizeof(float)) / kScoreRows * kScoreRows;
+    const size_t nS = score_stride((int)nC);
+    size_t rs = kSigmaBytes / (bg * nS * sizeof(float)) / kScoreRows * kScoreRows;
     rs = std::max<size_t>(rs, kScoreRows);
     const size_t parts = (ns + rs - 1) / rs;  // as equal as whole tiles allow
     rs = std::min(ns, (ns + parts * kScoreRows - 1) / (parts * kScoreRows) * kScoreRows);
@@ -333,11 +341,12 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf1
     w.ranks = take(bg * ns * K * sizeof(int));
     w.list = take(bg * ns * K * sizeof(int));
     w.work = take(w.max_work * sizeof(int4));
-    w.sigma = take(bg * rs * nC * sizeof(float));
+    w.sigma = take(bg * rs * nS * sizeof(float));
     // (no less than a call of fewer rows may need)
     const size_t records = std::max((size_t)B * Hq * ns * w.slots, w.few ? 0 : std::min(kFewRecords, cap / rec));
     w.rec_s = take(records * sizeof(float2));
     w.rec_o = take(records * (rec - sizeof(float2)));
+    w.bmax = take(bg * rs * (nS / kBlock) * sizeof(float));
     w.total = at;
     return w;
 }
@@ -349,9 +358,13 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf1
 // landmark rows of one head at a time come through LDS (double-buffered) and serve all rows;
 // the maximum over the heads stays in registers until a block of candidates is done.  It also
 // clears the words that the next launches count in.
+template <int PERM>
+__device__ __forceinline__ float quad_perm(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), PERM, 0xf, 0xf, true));
+}
 template <typename T, int D, int G, int RT>
 __global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave, sizeof(T) == 2 && RT * G * D <= 512 ? 4 : 1) void k_pp_score(FwdArgs f, const int32_t* newlens,
-                                                                                 float* sigma, int r0, int Rs, int slice,
+                                                                                 float* sigma, float* bmax, int r0, int Rs, int slice,
                                                                                  int nslices, int* counts, size_t nclear) {
     using C = Cfg<T, D>;
     constexpr int NW = score_waves(C::ES == 2), NT = NW * kWave, WROWS = 16 * RT, ROWS = WROWS * NW;
@@ -374,7 +387,7 @@ __global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave, sizeof(T) == 2
     const int q0 = r0 + tile * ROWS;
     const int qend = min(min(q0 + ROWS, r0 + Rs), sq.fresh);
     if (q0 >= qend) return;
-    const int nC = f.L / kChunk;
+    const int nS = score_stride(f.L / kChunk);
     const int c_beg = part * slice, c_end = min(n_candidates(sq.pos0 + qend - 1, f.W), c_beg + slice);
     if (c_beg >= c_end) return;
     const bool shared_lmk = f.Hl != f.Hq;
@@ -413,13 +426,15 @@ __global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave, sizeof(T) == 2
         r.bv = f.bias && tid < kScoreCand ? f.bias[(size_t)s_pg[min(c0 + tid, last)] * f.Hl + hl] : 0.f;
         return r;
     };
+    // candidate j of a block as row 16 (j % 4) + j / 4, so that a lane's four results are neighbours
+    auto place = [](int j) { return j % 4 * 16 + j / 4; };
     auto store = [&](int buf, const Regs& r) {
 #pragma unroll
         for (int u = 0; u < PPT; ++u) {
             const int e = tid + u * NT, j = e / (D / C::EP), d0 = (e % (D / C::EP)) * C::EP;
-            *reinterpret_cast<uint4*>(&s_l[buf][j * C::KROW + d0 * C::ES]) = r.x[u];
+            *reinterpret_cast<uint4*>(&s_l[buf][place(j) * C::KROW + d0 * C::ES]) = r.x[u];
         }
-        if (tid < kScoreCand) s_b[buf][tid] = r.bv;
+        if (tid < kScoreCand) s_b[buf][place(tid)] = r.bv;
     };
     const size_t bg = (size_t)b * f.Hkv + g;
     f32x4 sg[RT][4];
@@ -474,17 +489,28 @@ __global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave, sizeof(T) == 2
             }
         }
         if (lh == NH - 1) {
+            // (past c_end up to a whole block: nobody reads these)
+            const int c = c_beg + (t / NH) * kScoreCand + 4 * (lane % 16);
 #pragma unroll
-            for (int nb = 0; nb < 4; ++nb) {
-                const int c = c_beg + (t / NH) * kScoreCand + nb * 16 + lane % 16;
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int n = q0 + WROWS * w + 16 * rt + 4 * lg + i;
-                        if (n < qend && c < c_end) sigma[(bg * Rs + (n - r0)) * nC + c] = sg[rt][nb][i];
+                for (int i = 0; i < 4; ++i) {
+                    const int n = q0 + WROWS * w + 16 * rt + 4 * lg + i;
+                    const bool in = n < qend && c < c_end;
+                    const f32x4 x = {sg[rt][0][i], sg[rt][1][i], sg[rt][2][i], sg[rt][3][i]};
+                    const size_t at = (bg * Rs + (n - r0)) * nS + c;
+                    if (!bmax) {
+                        if (in) *reinterpret_cast<f32x4*>(sigma + at) = x;
+                        continue;
                     }
-            }
+                    // (few of them will be read: past the last-level cache, whose lines the chunks' pass would
+                    // have to write back: 4096 rows over 131K, that pass 291 -> 277 us)
+                    if (in) __builtin_nontemporal_store(x, reinterpret_cast<f32x4*>(sigma + at));
+                    float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+                    top = fmaxf(top, quad_perm<0xb1>(top));  // lane ^ 1
+                    top = fmaxf(top, quad_perm<0x4e>(top));  // lane ^ 2
+                    if (in && lane % 4 == 0) bmax[at / kBlock] = top;
+                }
         }
         store(buf ^ 1, next);
         __syncthreads();
@@ -540,16 +566,18 @@ __device__ __forceinline__ unsigned long long pair_of(int rows, int seg) {
 // and 48.2, 64 53.6 and 58.8 (one CU selects for all); 1 over 2040 34.9 and 33.0, 16 49.0 and 49.8.
 constexpr int kSelHist = 4096;  // chunks counted in LDS
 enum Select { kPerRow, kMany, kPlanToo };
+// Candidates above which a row's blocks are looked at first: more than one pass over all of them takes, and of which
+// the blocks hold half or fewer (K = 16, selection: 4096 rows over 131K 92 -> 67 us, 512 over 1M 71 -> 14, 16 over
+// 1M 45 -> 10; 16 x 512 rows over up to 500 candidates 47 -> 52).
+constexpr int kBlocks = 0;  // as E: by blocks
+__host__ __device__ constexpr int blocks_above(int K) { return K <= 32 ? 16 * kWave : 32 * K; }
 constexpr int kPlanTooScores = 4096;  // of a (b, g), at most
 template <int E, Select MODE>
-__global__ __launch_bounds__((MODE != kPerRow ? 16 : kSelWaves) * kWave) void k_pp_select(FwdArgs f,
-                                                                                        const int32_t* newlens,
-                                                                                        const float* sigma, Ws ws,
-                                                                                        int* nwork, int n0, int Ns,
-                                                                                        int r0, int Rs, int seg) {
+__global__ __launch_bounds__((MODE != kPerRow ? 16 : kSelWaves) * kWave) void k_pp_select(
+    FwdArgs f, const int32_t* newlens, const float* sigma, const float* bmax, int* counts, int* ranks, int n0, int Ns,
+    int r0, int Rs, int* nwork, int4* work, int* list, int seg) {
     constexpr bool MANY = MODE != kPerRow;
     constexpr int NW = MANY ? 16 : kSelWaves, ROWS = MANY ? 64 : kSelWaves;
-    int *counts = ws.counts, *ranks = ws.ranks;
     __shared__ int s_tid[NW][kWave];
     __shared__ __align__(16) float s_tsc[NW][kWave];
     __shared__ int s_oid[NW][kWave];
@@ -575,19 +603,22 @@ __global__ __launch_bounds__((MODE != kPerRow ? 16 : kSelWaves) * kWave) void k_
         if (f.given_idx) {
             if (lane < f.K && idx_entry_valid(orow, lane, lim)) c = orow[lane];
         } else {
-            const float* row = sigma + (bg * Rs + (n - r0)) * nC;
+            const float* row = sigma + (bg * Rs + (n - r0)) * score_stride(nC);
             int m = 0;
-            auto best = [&](auto e_tag) {
+            // the K best of `src` at id_of(0 .. count - 1), in ascending order, to s_oid
+            auto best_of = [&](auto e_tag, int count, auto id_of, const float* src) {
                 constexpr int EE = decltype(e_tag)::value;
-                for (int c0 = 0; c0 < lim; c0 += EE * kWave) {
+                m = 0;
+                for (int c0 = 0; c0 < count; c0 += EE * kWave) {
                     float sc[EE + 1];
                     int id[EE + 1];
                     bool ok[EE + 1];
 #pragma unroll
                     for (int e = 0; e < EE; ++e) {
-                        id[e] = c0 + e * kWave + lane;
-                        ok[e] = id[e] < lim;
-                        sc[e] = ok[e] ? row[id[e]] : 0.f;
+                        const int at = c0 + e * kWave + lane;
+                        ok[e] = at < count;
+                        id[e] = id_of(at);
+                        sc[e] = ok[e] ? src[id[e]] : 0.f;
                     }
                     ok[EE] = lane < m;
                     sc[EE] = ok[EE] ? s_osc[w][lane] : 0.f;
@@ -598,12 +629,32 @@ __global__ __launch_bounds__((MODE != kPerRow ? 16 : kSelWaves) * kWave) void k_
                 }
             };
             // (the row's own candidates may be far fewer than the call's)
-            if (E >= 4 && lim <= kWave)
-                best(std::integral_constant<int, 1>{});
-            else if (E >= 16 && lim <= 4 * kWave)
-                best(std::integral_constant<int, 4>{});
-            else
-                best(std::integral_constant<int, E>{});
+            auto all_of = [](int i) { return i; };
+            if constexpr (E != kBlocks) {
+                if (E >= 4 && lim <= kWave)
+                    best_of(std::integral_constant<int, 1>{}, lim, all_of, row);
+                else if (E >= 16 && lim <= 4 * kWave)
+                    best_of(std::integral_constant<int, 4>{}, lim, all_of, row);
+                else
+                    best_of(std::integral_constant<int, E>{}, lim, all_of, row);
+            } else {
+                // The K best are in the K blocks of the largest maxima (ties: the smaller; whatever is in another
+                // has K before it), or past the whole blocks.
+                const bool two = lim > blocks_above(f.K);
+                const int whole = lim / kBlock, count = two ? whole : lim;
+                const float* src = two ? bmax + (bg * Rs + (n - r0)) * (score_stride(nC) / kBlock) : row;
+                if (count <= 5 * kWave)
+                    best_of(std::integral_constant<int, 5>{}, count, all_of, src);
+                else
+                    best_of(std::integral_constant<int, 16>{}, count, all_of, src);
+                if (two) {
+                    const int blocks = m, picked = m * kBlock, held = s_oid[w][min(lane, m - 1)];
+                    best_of(std::integral_constant<int, 5>{}, picked + lim - whole * kBlock, [&](int i) {
+                        const int b = __shfl(held, min(i / kBlock, blocks - 1), kWave);
+                        return i < picked ? b * kBlock + i % kBlock : whole * kBlock + i - picked;
+                    }, row);
+                }
+            }
             if (lane < m) c = s_oid[w][lane];
             if (lane < f.K) orow[lane] = c;
         }
@@ -630,13 +681,13 @@ __global__ __launch_bounds__((MODE != kPerRow ? 16 : kSelWaves) * kWave) void k_
             const int row = rows0 + (int)(unsigned)at;
             int item = s_base + (int)(at >> 32);
             if (c < chunks) s_cnt[c] = row;
-            for (int k = 0; k < cnt; k += seg) ws.work[item++] = make_int4((int)bg, c, row + k, min(seg, cnt - k));
+            for (int k = 0; k < cnt; k += seg) work[item++] = make_int4((int)bg, c, row + k, min(seg, cnt - k));
             rows0 += (int)(unsigned)all;
         }
         __syncthreads();
         for (int e = tid; e < (end - first) * f.K; e += NW * kWave) {
             const int x = s_ent[e];
-            if (x >= 0) ws.list[bg * Ns * f.K + s_cnt[x >> 6] + (x & 63)] = (first - n0 + e / f.K) << 6 | e % f.K;
+            if (x >= 0) list[bg * Ns * f.K + s_cnt[x >> 6] + (x & 63)] = (first - n0 + e / f.K) << 6 | e % f.K;
         }
     } else if constexpr (MANY) {
         __syncthreads();
@@ -1207,6 +1258,7 @@ struct Run {
         ws.list = reinterpret_cast<int*>(base + ly.list);
         ws.work = reinterpret_cast<int4*>(base + ly.work);
         ws.sigma = reinterpret_cast<float*>(base + ly.sigma);
+        ws.bmax = reinterpret_cast<float*>(base + ly.bmax);
         ws.rec_s = reinterpret_cast<float2*>(base + ly.rec_s);
         ws.rec_o = base + ly.rec_o;
         const int nC = f.L / kChunk, maxc = n_candidates(f.L - 1, f.W);  // candidates of any row, at most
@@ -1231,7 +1283,7 @@ struct Run {
                         const int slice = std::min(kScoreSlice, kScoreCand * (int)((blocks + want - 1) / want));
                         const int nslices = (maxc + slice - 1) / slice;
                         HILS_LAUNCH("k_pp_score", (k_pp_score<T, D, G, RT>), dim3((unsigned)(tiles * nslices)),
-                                    dim3(waves * kWave), 0, s, f, a.newlens, ws.sigma, r0, Rs, slice, nslices, ws.counts,
+                                    dim3(waves * kWave), 0, s, f, a.newlens, ws.sigma, maxc > blocks_above(f.K) ? ws.bmax : nullptr, r0, Rs, slice, nslices, ws.counts,
                                     r0 == n0 ? ncount + 1 : 0);
                     };
                     // two row tiles per wave, each landmark operand feeding two products, where the heads' queries
@@ -1248,8 +1300,9 @@ struct Run {
                     auto launch = [&](auto mode_tag, int rows, int waves, size_t lds) {
                         constexpr Select MODE = decltype(mode_tag)::value;
                         HILS_LAUNCH("k_pp_select", (k_pp_select<E, MODE>), dim3((unsigned)(bg * ((Rs + rows - 1) / rows))),
-                                    dim3(waves * kWave), lds, s, f, a.newlens, (const float*)ws.sigma, ws, nwork, n0, Ns,
-                                    r0, Rs, seg);
+                                    dim3(waves * kWave), lds, s, f, a.newlens, (const float*)ws.sigma,
+                                    (const float*)ws.bmax, ws.counts, ws.ranks, n0, Ns, r0, Rs, nwork, ws.work, ws.list,
+                                    seg);
                     };
                     if (plan_too)
                         launch(std::integral_constant<Select, kPlanToo>{}, 64, 16, (nC + 64 * f.K) * sizeof(int));
@@ -1262,8 +1315,10 @@ struct Run {
                     select(std::integral_constant<int, 1>{});
                 else if (maxc <= 4 * kWave)
                     select(std::integral_constant<int, 4>{});
-                else
+                else if (maxc <= blocks_above(f.K))
                     select(std::integral_constant<int, 16>{});
+                else
+                    select(std::integral_constant<int, kBlocks>{});
             }
             const size_t most = bg * (std::min<size_t>(maxc, (size_t)Ns * f.K) + (size_t)Ns * f.K / seg);
             if (maxc > 0 && !plan_too) {

@@ -173,3 +173,22 @@ def test_replays_of_a_captured_call(dtype):
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(outs, refs[i]))
         w.run()  # eager work between replays
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("topk,chunks", [(1, 1100), (7, 1100), (16, 1301), (33, 1100), (64, 2200)])
+def test_ties_over_many_candidates(topk, chunks, dtype):
+    """Landmarks of six kinds: equal scores by the dozen, of which the lower chunks are chosen, bit for bit."""
+    p = hils_().Params(B=1, Hq=2, Hkv=1, N=70, L=64 * chunks, d=64, topk=topk, window=64, dtype=dtype)
+    w = World(p, [64 * chunks - 7], [70], 3)
+    r = np.random.default_rng(5)
+    kinds, kind = w.lmk[w.table[0, :6]].copy(), r.integers(0, 6, chunks)
+    kind[r.random(chunks) < 0.6] = 0
+    kind[:500] = 5  # (for some rows the best kind begins late, for others at once)
+    w.lmk[w.table[0, :chunks - 1]] = kinds[kind[:chunks - 1]]
+    got = w.run()[2].cpu().numpy()
+    score = np.einsum("hnd,khd->nkh", w.q[0].astype(np.float64), kinds.astype(np.float64)).max(-1)  # [N, kinds]
+    for n in range(70):
+        have = (w.len[0] - w.fresh[0] + n - 64 + 1) // 64
+        order = np.lexsort((np.arange(have), -score[n][kind[:have]]))
+        assert (got[0, 0, n] == np.sort(order[:topk])).all(), f"row {n}"
