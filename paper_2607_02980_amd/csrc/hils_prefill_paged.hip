@@ -292,7 +292,6 @@ struct Layout {
     size_t counts, offs, ranks, list, work, sigma, bmax, rec_s, rec_o, total;
     int Ns, Rs, slots;  // records of a (row, head)
     bool few;           // the windows' pieces among them
-    size_t max_work;
 };
 
 // Scores of so many candidates in a row have their maximum beside them.
@@ -329,7 +328,16 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf1
     rs = std::min(ns, (ns + parts * kScoreRows - 1) / (parts * kScoreRows) * kScoreRows);
     w.Ns = (int)ns;
     w.Rs = (int)rs;
-    w.max_work = bg * (std::min(nC, ns * K) + ns * K / seg_rows(bf16, Hq / Hkv));
+    // Sizes by what any call of as many sequences, rows and tokens or fewer may need: bg * Ns is at most rows(slots)
+    // and sigma at most kSigmaBytes, or their smallest blocks.
+    const size_t G = Hq / Hkv, smallest = bg * std::min<size_t>(N, kScoreRows);
+    auto rows = [&](size_t slots) {
+        return std::min(bg * std::min<size_t>(N, kMaxRows), std::max(cap / (G * slots * rec), smallest));
+    };
+    const size_t most = rows(K), entries = most * K;
+    const size_t scores = std::min(most * nS, std::max(kSigmaBytes / sizeof(float), smallest * nS));
+    const size_t few_records = std::min(kFewRecords, rows(K + pieces) * G * (K + pieces));
+    const size_t records = w.few ? few_records : std::max(most * G * K, few_records);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -338,15 +346,13 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf1
     };
     w.counts = take((bg * nC + 1) * sizeof(int));
     w.offs = take(bg * nC * sizeof(int));
-    w.ranks = take(bg * ns * K * sizeof(int));
-    w.list = take(bg * ns * K * sizeof(int));
-    w.work = take(w.max_work * sizeof(int4));
-    w.sigma = take(bg * rs * nS * sizeof(float));
-    // (no less than a call of fewer rows may need)
-    const size_t records = std::max((size_t)B * Hq * ns * w.slots, w.few ? 0 : std::min(kFewRecords, cap / rec));
+    w.ranks = take(entries * sizeof(int));
+    w.list = take(entries * sizeof(int));
+    w.work = take((std::min(bg * nC, entries) + entries / seg_rows(bf16, (int)G)) * sizeof(int4));
+    w.sigma = take(scores * sizeof(float));
     w.rec_s = take(records * sizeof(float2));
     w.rec_o = take(records * (rec - sizeof(float2)));
-    w.bmax = take(bg * rs * (nS / kBlock) * sizeof(float));
+    w.bmax = take(scores / kBlock * sizeof(float));
     w.total = at;
     return w;
 }
@@ -354,14 +360,16 @@ Layout layout(int B, int Hq, int Hkv, int N, int L, int d, int K, int W, int bf1
 // ---------------------------------------------------------------------------
 // scores
 // ---------------------------------------------------------------------------
-// A workgroup takes 128 rows (f32: 64) of a KV group, 16 per wave, and `slice` candidates; 64
-// landmark rows of one head at a time come through LDS (double-buffered) and serve all rows;
-// the maximum over the heads stays in registers until a block of candidates is done.  It also
-// clears the words that the next launches count in.
+// The value of the lane that PERM names among the four of a group.
 template <int PERM>
 __device__ __forceinline__ float quad_perm(float x) {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), PERM, 0xf, 0xf, true));
 }
+
+// A workgroup takes 128 rows (f32: 64) of a KV group, 16 per wave, and `slice` candidates; 64
+// landmark rows of one head at a time come through LDS (double-buffered) and serve all rows;
+// the maximum over the heads stays in registers until a block of candidates is done.  It also
+// clears the words that the next launches count in.
 template <typename T, int D, int G, int RT>
 __global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave, sizeof(T) == 2 && RT * G * D <= 512 ? 4 : 1) void k_pp_score(FwdArgs f, const int32_t* newlens,
                                                                                  float* sigma, float* bmax, int r0, int Rs, int slice,

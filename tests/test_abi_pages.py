@@ -1,5 +1,6 @@
 """Refusals of the entry points for a shared paged cache, on the CPU: every check runs before any HIP call."""
 import ctypes
+import random
 
 import pytest
 import torch
@@ -104,6 +105,26 @@ def test_prefill_workspace_grows_with_batch_rows_and_cache():
     before = hils.hils_prefill_record_cap(1 << 20)
     try:
         assert size(N=6000, L=64000) < 40 << 20  # (records of 128 rows, and 4 lists of all ranks)
+    finally:
+        hils.hils_prefill_record_cap(before)
+
+
+@pytest.mark.parametrize("cap", [0, 1, 1 << 20, 1 << 28])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_prefill_workspace_serves_all_smaller_calls(dtype, cap):
+    """The size rises with batch, rows and cache, also where scores or records are cut into blocks of rows and where
+    few rows turn into many."""
+    r = random.Random(cap)
+    size = lambda B, N, L: hils.hils_workspace_size(  # noqa: E731
+        params(B=B, N=N, L=L, Hq=32, Hkv=8, topk=16, window=512, dtype=dtype), hils.HILS_OP_PREFILL_PAGED)
+    before = hils.hils_prefill_record_cap(cap)
+    try:
+        for _ in range(3000):
+            B, N, L = r.choice([1, 2, 3, 7, 16, 33]), r.randint(1, r.choice([40, 600, 9000])), 64 * r.choice([150, 999, 2100, 16001])
+            more = [(B + r.choice([1, 2, 9]), N, L), (B, N + r.choice([1, 60, 128, 2000]), L), (B, N, L + 64 * r.choice([1, 900]))]
+            here = size(B, min(N, L), L)
+            for b in more:
+                assert here <= size(b[0], min(b[1], b[2]), b[2]), ((B, N, L), b)
     finally:
         hils.hils_prefill_record_cap(before)
 
