@@ -167,7 +167,8 @@ __device__ __forceinline__ void add_pv_by_key(const char* s_v, const f32x4 (&st)
     }
 }
 
-// Records: a chunk's output o_c for one (row, head), as the accumulators hold it, with s^ and a scale.
+// Records: a chunk's output o_c for one (row, head), as the accumulators hold it, with s^ in log2 units and the unit it
+// is held in (bf16 calls) or the sum it stands for (f32: 1 for a chunk, a block's own for a piece of the window).
 // They are written once and read once, a pass's largest traffic, so that bf16 calls keep them in
 // float16, in units of the power of two below the vector's largest finite element: 2^-11 of that
 // at most is lost, a fraction of what rounding the weights to bf16 loses (in bf16, 2^-8, it would be
@@ -240,23 +241,22 @@ struct Record {
 template <typename T, int D, int NR>
 __device__ __forceinline__ void add_records(const Record<T, D> (&r)[NR], const float2 (&sv)[NR], const bool (&valid)[NR],
                                             f32x4 (&o)[D / 16], float& m, float& l) {
-    // (s^ in log2 units is -inf for a bias of the lowest value too, whose weight is 0 beside any token of the window)
-    float s[NR], mnew = m;
+    // (a logit in log2 units is -inf for a bias of the lowest value too, whose weight is 0 beside any token of the window)
+    float mnew = m;
     bool ok[NR];
 #pragma unroll
     for (int u = 0; u < NR; ++u) {
-        s[u] = sv[u].x * kLog2e;
-        ok[u] = valid[u] && s[u] != -INFINITY;  // (a masked chunk's record may hold anything)
-        mnew = ok[u] ? fmaxf(mnew, s[u]) : mnew;
+        ok[u] = valid[u] && sv[u].x != -INFINITY;  // (a masked chunk's record may hold anything)
+        mnew = ok[u] ? fmaxf(mnew, sv[u].x) : mnew;
     }
     float rs = mnew == m ? 1.f : fexp2(m - mnew);
     m = mnew;
     l *= rs;
 #pragma unroll
     for (int u = 0; u < NR; ++u) {
-        const float wk = ok[u] ? fexp2(s[u] - m) : 0.f;
-        l += wk;
-        r[u].add(o, rs, ok[u] ? wk * sv[u].y : 0.f, ok[u]);
+        const float wk = ok[u] ? fexp2(sv[u].x - m) : 0.f, wy = ok[u] ? wk * sv[u].y : 0.f;
+        l += sizeof(T) == 4 ? wy : wk;
+        r[u].add(o, rs, sizeof(T) == 4 ? wk : wy, ok[u]);
         rs = 1.f;
     }
 }
@@ -285,7 +285,7 @@ struct Ws {
     int4* work;    // (bg, chunk, offset, rows)
     float* sigma;  // [bg][Rs][nS], nS: nC in whole blocks
     float* bmax;   // [bg][Rs][nS / kBlock] the maxima of its blocks
-    float2* rec_s; // [bg][Ns][slots][G] s^ and the record's unit
+    float2* rec_s; // [bg][Ns][slots][G] logit in log2 units, and the record's unit or sum
     char* rec_o;   // [bg][Ns][slots][G] records
 };
 struct Layout {
@@ -937,16 +937,22 @@ __global__ __launch_bounds__(kChunkWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
                 add_pv_by_key<T, D>(s_v, st, o, lane, pos - c * kChunk, ell - c * kChunk);
             else
                 add_pv<T, D>(s_v, st, o, lane);
-            const float inv = sum > 0.f ? 1.f / sum : 0.f;
+            float inv = sum > 0.f ? 1.f / sum : 0.f, logit = shat * kLog2e, mass = 1.f;
             bool keep = live;
             if (win) {
                 slot = f.K + c - ell / kChunk;
                 keep = live && slot >= f.K && c <= pos / kChunk;
-                shat = (mx + __log2f(sum)) * (1.f / kLog2e);
+                if constexpr (C::ES == 4) {  // (the sum beside the maximum: a rounded logarithm of it would cost 2^-22)
+                    inv = 1.f;
+                    logit = sum > 0.f ? mx : sum == 0.f ? -INFINITY : sum;
+                    mass = sum;
+                } else {
+                    logit = mx + __log2f(sum);
+                }
             }
             const size_t rec = ((bg * Ns + n) * slots + slot) * G + hh;
             const float unit = Record<T, D>::store(ws.rec_o + rec * Record<T, D>::BYTES, o, inv, lg, keep);
-            if (keep && lg == 0) ws.rec_s[rec] = make_float2(shat, unit);
+            if (keep && lg == 0) ws.rec_s[rec] = make_float2(logit, C::ES == 4 ? mass : unit);
         }
     }
 }
@@ -1197,7 +1203,6 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void k_pp_join(FwdArgs f, const
         float mnew = m;
 #pragma unroll
         for (int u = 0; u < SB; ++u) {
-            sv[u].x *= kLog2e;
             ok[u] = ok[u] && sv[u].x != -INFINITY;  // (as in add_records)
             mnew = ok[u] ? fmaxf(mnew, sv[u].x) : mnew;
         }
@@ -1206,8 +1211,9 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void k_pp_join(FwdArgs f, const
         l *= rs;
 #pragma unroll
         for (int u = 0; u < SB; ++u) {
-            const float wk = ok[u] ? fexp2(sv[u].x - m) : 0.f, wu = ok[u] ? wk * sv[u].y : 0.f;
-            l += wk;
+            const float wk = ok[u] ? fexp2(sv[u].x - m) : 0.f, wy = ok[u] ? wk * sv[u].y : 0.f;
+            const float wu = C::ES == 4 ? wk : wy;
+            l += C::ES == 4 ? wy : wk;
 #pragma unroll
             for (int t = 0; t < PCS; ++t) {
                 const uint4 y = ok[u] ? x[u][t] : make_uint4(0, 0, 0, 0);
