@@ -580,6 +580,17 @@ enum Select { kPerRow, kMany, kPlanToo };
 constexpr int kBlocks = 0;  // as E: by blocks
 __host__ __device__ constexpr int blocks_above(int K) { return K <= 32 ? 16 * kWave : 32 * K; }
 constexpr int kPlanTooScores = 4096;  // of a (b, g), at most
+// kPlanToo: what a row's slot chose, in a word of LDS: the chunk, and the rank among its uses.  The uses of a chunk may be more
+// than the rows: a given row that does not ascend ([4, -1, 4, ...]) uses it several times.
+constexpr int kPlanRows = 64, kMaxSlots = 64;
+constexpr int kRankBits = 12;
+constexpr int plan_entry(int chunk, int rank) { return chunk << kRankBits | rank; }
+constexpr int entry_chunk(int x) { return x >> kRankBits; }
+constexpr int entry_rank(int x) { return x & ((1 << kRankBits) - 1); }
+static_assert(entry_chunk(plan_entry(kSelHist - 1, kPlanRows * kMaxSlots - 1)) == kSelHist - 1 &&
+                  entry_rank(plan_entry(kSelHist - 1, kPlanRows * kMaxSlots - 1)) == kPlanRows * kMaxSlots - 1 &&
+                  plan_entry(kSelHist - 1, kPlanRows * kMaxSlots - 1) >= 0,
+              "a chunk and a rank fit side by side, and -1 is neither");
 template <int E, Select MODE>
 __global__ __launch_bounds__((MODE != kPerRow ? 16 : kSelWaves) * kWave) void k_pp_select(
     FwdArgs f, const int32_t* newlens, const float* sigma, const float* bmax, int* counts, int* ranks, int n0, int Ns,
@@ -591,7 +602,7 @@ __global__ __launch_bounds__((MODE != kPerRow ? 16 : kSelWaves) * kWave) void k_
     __shared__ int s_oid[NW][kWave];
     __shared__ float s_osc[NW][kWave];
     extern __shared__ int s_cnt[];  // MANY: rows of each chunk, then where they begin
-    int* s_ent = s_cnt + (MODE == kPlanToo ? f.L / kChunk : 0);  // kPlanToo: chunk << 6 | rank of a row's slot, or -1
+    int* s_ent = s_cnt + (MODE == kPlanToo ? f.L / kChunk : 0);  // kPlanToo: plan_entry of a row's slot, or -1
     const int tid = threadIdx.x, w = wave_id(), lane = tid % kWave, nC = f.L / kChunk;
     const int tiles = (Rs + ROWS - 1) / ROWS, first = r0 + (int)(blockIdx.x % tiles) * ROWS;
     const size_t bg = blockIdx.x / tiles;
@@ -669,7 +680,7 @@ __global__ __launch_bounds__((MODE != kPerRow ? 16 : kSelWaves) * kWave) void k_
         if (lane < f.K) {
             const int rank = c < 0 ? -1 : atomicAdd(MANY ? &s_cnt[c] : &counts[bg * nC + c], 1);
             if constexpr (MODE == kPlanToo)
-                s_ent[(n - first) * f.K + lane] = c < 0 ? -1 : c << 6 | rank;
+                s_ent[(n - first) * f.K + lane] = c < 0 ? -1 : plan_entry(c, rank);
             else
                 ranks[(bg * Ns + (n - n0)) * f.K + lane] = rank;
         }
@@ -695,7 +706,7 @@ __global__ __launch_bounds__((MODE != kPerRow ? 16 : kSelWaves) * kWave) void k_
         __syncthreads();
         for (int e = tid; e < (end - first) * f.K; e += NW * kWave) {
             const int x = s_ent[e];
-            if (x >= 0) list[bg * Ns * f.K + s_cnt[x >> 6] + (x & 63)] = (first - n0 + e / f.K) << 6 | e % f.K;
+            if (x >= 0) list[bg * Ns * f.K + s_cnt[entry_chunk(x)] + entry_rank(x)] = (first - n0 + e / f.K) << 6 | e % f.K;
         }
     } else if constexpr (MANY) {
         __syncthreads();
@@ -1281,7 +1292,7 @@ struct Run {
         int* nwork = ws.counts + ncount;
         for (int n0 = 0; n0 < f.N; n0 += ly.Ns) {
             const int Ns = std::min(ly.Ns, f.N - n0);
-            const bool plan_too = Ns <= 64 && nC <= kSelHist && Ns * maxc <= kPlanTooScores;
+            const bool plan_too = Ns <= kPlanRows && nC <= kSelHist && Ns * maxc <= kPlanTooScores;
             if (f.given_idx && maxc > 0)
                 HILS_LAUNCH("k_pp_clear", k_pp_clear, dim3((unsigned)std::min<size_t>((ncount + 256) / 256, 4096)),
                             dim3(256), 0, s, ws.counts, ncount + 1);
@@ -1319,7 +1330,7 @@ struct Run {
                                     seg);
                     };
                     if (plan_too)
-                        launch(std::integral_constant<Select, kPlanToo>{}, 64, 16, (nC + 64 * f.K) * sizeof(int));
+                        launch(std::integral_constant<Select, kPlanToo>{}, kPlanRows, 16, (nC + kPlanRows * f.K) * sizeof(int));
                     else if ((size_t)Rs * f.K >= 64 * (size_t)nC && Rs >= 64 && nC <= kSelHist)
                         launch(std::integral_constant<Select, kMany>{}, 64, 16, nC * sizeof(int));
                     else
