@@ -480,8 +480,8 @@ int hils_cache_free(const hils_params* p, const int32_t* keep, const int32_t* pa
 
 /*
  * Compact: with n pages in use, the i-th used page at or past n moves to the i-th free page before
- * it, in every pool; counts move along and entries in use follow, so that the pool can be cut to
- * n pages.
+ * it, in every pool; counts move along (of a free page: 0, also where it was below) and entries
+ * in use follow, so that the pool can be cut to n pages.
  *   new_page [num_pages]  where each page is now (-1: free before the call), for holders of
  *                         pages outside the table
  *   moved    [num_pages]  the pages that moved, ascending, then -1

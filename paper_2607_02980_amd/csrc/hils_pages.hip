@@ -390,7 +390,8 @@ __global__ __launch_bounds__(kPlan) void k_cache_compact(CompactArgs a) {
             const int p = p0 + tid * PER + i;
             if (p >= a.P) continue;
             a.new_page[p] = r[i] > 0 ? p : -1;
-            if (a.refs_out != a.refs) a.refs_out[p] = max(r[i], 0);
+            // (in place too: all have counted the used pages by now, and from here each thread uses its own counts only)
+            if (a.refs_out != a.refs || r[i] < 0) a.refs_out[p] = max(r[i], 0);
             if (p >= used && r[i] > 0) a.moved[at++] = p;
             if (p < used && r[i] <= 0) a.moved[half + to++] = p;
         }
