@@ -505,7 +505,8 @@ __global__ __launch_bounds__(score_waves(sizeof(T) == 2) * kWave, sizeof(T) == 2
                 for (int i = 0; i < 4; ++i) {
                     const int n = q0 + WROWS * w + 16 * rt + 4 * lg + i;
                     const bool in = n < qend && c < c_end;
-                    const f32x4 x = {sg[rt][0][i], sg[rt][1][i], sg[rt][2][i], sg[rt][3][i]};
+                    // (-0 as 0: equal scores rank by index)
+                    const f32x4 x = {sg[rt][0][i] + 0.f, sg[rt][1][i] + 0.f, sg[rt][2][i] + 0.f, sg[rt][3][i] + 0.f};
                     const size_t at = (bg * Rs + (n - r0)) * nS + c;
                     if (!bmax) {
                         if (in) *reinterpret_cast<f32x4*>(sigma + at) = x;
