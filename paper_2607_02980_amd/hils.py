@@ -629,6 +629,9 @@ def hils_cache_free(p: Params, keep, block_table, page_refs, seqlens=None, pages
     if pages is not None and (not isinstance(pages, torch.Tensor) or pages.dim() != 2):
         raise ValueError("pages must be a GPU tensor of two dimensions")
     most = 0 if pages is None else pages.shape[1]
+    nlisted = None if npages is None else _address(npages, "npages", (p.B,), _I32, dev)
+    if pages is not None and not most:  # lists of no entries have no address, so their counts are left out too
+        nlisted = None
     if table_out is None:
         table_out = torch.empty(shape, dtype=_I32, device=on)
     if seqlens_out is None:
@@ -636,8 +639,7 @@ def hils_cache_free(p: Params, keep, block_table, page_refs, seqlens=None, pages
     if refs_out is None:
         refs_out = torch.empty(P, dtype=_I32, device=on)
     _run(LIB.hils_cache_free, dev, ctypes.byref(p.c()), _address(keep, "keep", (p.B,), _I32, dev),
-         None if pages is None else _address(pages, "pages", (p.B, most), _I32, dev),
-         None if npages is None else _address(npages, "npages", (p.B,), _I32, dev), most,
+         None if pages is None else _address(pages, "pages", (p.B, most), _I32, dev), nlisted, most,
          _address(block_table, "block_table", shape, _I32, dev), _address(page_refs, "page_refs", (P,), _I32, dev), P,
          None if seqlens is None else _address(seqlens, "seqlens", (p.B,), _I32, dev),
          _address(table_out, "table_out", shape, _I32, dev), _address(seqlens_out, "seqlens_out", (p.B,), _I32, dev),
