@@ -237,6 +237,17 @@ struct Record {
     }
 };
 
+// s^ in log2 units, and back.  log2 e times a bias near float32's largest value would pass it, so from 2^127 on the
+// units are halves of s^ itself: still in order, and no two such logits need their difference but to be told apart (it is
+// 0 or at least 2^104).
+constexpr float kFarLogit = 0x1p127f;
+__device__ __forceinline__ float to_log2(float s) {
+    return s < kFarLogit ? s * kLog2e : kFarLogit * kLog2e + (s - kFarLogit) * 0.5f;
+}
+__device__ __forceinline__ float from_log2(float x) {
+    return x < kFarLogit * kLog2e ? x * (1.f / kLog2e) : kFarLogit + (x - kFarLogit * kLog2e) * 2.f;
+}
+
 // Adds NR records to a running softmax (maximum m in log2 units, sum l, numerator o).
 template <typename T, int D, int NR>
 __device__ __forceinline__ void add_records(const Record<T, D> (&r)[NR], const float2 (&sv)[NR], const bool (&valid)[NR],
@@ -949,7 +960,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, sizeof(T) == 2 ? 4 : 2) void k
                 add_pv_by_key<T, D>(s_v, st, o, lane, pos - c * kChunk, ell - c * kChunk);
             else
                 add_pv<T, D>(s_v, st, o, lane);
-            float inv = sum > 0.f ? 1.f / sum : 0.f, logit = shat * kLog2e, mass = 1.f;
+            float inv = sum > 0.f ? 1.f / sum : 0.f, logit = to_log2(shat), mass = 1.f;
             bool keep = live;
             if (win) {
                 slot = f.K + c - ell / kChunk;
@@ -1169,7 +1180,7 @@ __global__ __launch_bounds__(kLocalWaves * kWave, D * sizeof(T) <= 256 ? 4 : 2) 
             __builtin_memcpy(out + 64 * dd + 16 * lg + 4 * i, &r, 16);
         }
     }
-    if (lg == 0) f.lse[row] = (m + __log2f(l)) * (1.f / kLog2e);
+    if (lg == 0) f.lse[row] = from_log2(m + __log2f(l));
 }
 
 // ---------------------------------------------------------------------------
@@ -1268,7 +1279,7 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void k_pp_join(FwdArgs f, const
             for (int i = 0; i < 4; ++i) out[dim_of<T>(pt, i, lg)] = acc[t][i];
         }
     }
-    if (sub == 0) f.lse[row] = (M + __log2f(l)) * (1.f / kLog2e);
+    if (sub == 0) f.lse[row] = from_log2(M + __log2f(l));
 }
 
 struct Run {
