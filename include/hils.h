@@ -42,7 +42,12 @@
  *     A chunk's K (or V) block is one contiguous S*d span.
  *   - `dtype` fixes the element type of q, k, v, lmk, q_route, out, dout and
  *     of every gradient except dlmk_bias (float32 storage or bf16 storage).
- *     Arithmetic is float32 throughout; outputs are rounded to nearest-even.
+ *     Scores, softmax statistics and sums are float32; outputs are rounded to
+ *     nearest-even.  Calls on bf16 storage multiply on bf16 matrix units into float32
+ *     sums: the softmax weights (and in the backward their gradients) may be rounded
+ *     to bf16, 2^-8 of themselves at most, as operands, and results of single chunks
+ *     that a call keeps in its workspace to 16 bits.  Calls on float32 storage round
+ *     nothing below float32.
  *   - Landmark heads: Hl == Hq (one landmark key per query head, Appendix C)
  *     or Hl == Hkv (one per KV group).  The bias has the landmark heads.
  *   - `idx` rows list the selected chunks in ascending order, padded with -1
@@ -246,6 +251,10 @@ int hils_decode_paged_fwd(const hils_params* p, const void* q, const void* k_pag
  * every complete chunk have been written, those of the new tokens' chunks among them.
  *   q, q_route, out [B, Hq, N, d], lse [B, Hq, N], idx [B, Hkv, N, K]; rows at or past
  *   newlens[b] are neither read nor written.
+ * bf16 calls keep the results of chunks (and of pieces of the windows, in calls of few rows) as
+ * float16 in units of the power of two below the result's largest finite element: 2^-11 of an element is
+ * lost at most, or 2^-25 of the largest one, so that dimensions whose values are 2^17 times smaller than
+ * another's have less than bf16's precision.  float32 calls keep float32.
  * A bias of -inf masks a chunk for its head, whatever NaN its landmark and keys hold (and its
  * values, if every head of the group masks it); it is still chosen where candidates are few.
  * Tokens at or past a sequence's length may hold anything, and what a later token holds does
@@ -442,7 +451,8 @@ typedef struct {
  * hils_prefill_paged_fwd.  Every chunk that begins with a new token is given a free page
  * (whatever its entry held).  A page that holds older tokens and is about to get new ones is
  * left to its other sequences and copied to a free page if its count is above 1; where all that
- * count it write to it in this call, the first of them (lowest b) keeps it.  Given pages have
+ * count it write to it in this call, the first of them (lowest b) keeps it; where the entry of such a
+ * chunk names no page of the pool, a free one takes its place and nothing is copied.  Given pages have
  * count 1.  All or nothing: if the pool has fewer free pages than the call needs, table and
  * counts stay as they were.
  *   copied [B, 2]  the page copied from and to, -1 -1 where none was

@@ -3,7 +3,7 @@
 // Row n < fresh_b of sequence b is the query at position len_b - fresh_b + n; everything else
 // is the prefill's (Eqs. (1), (9), (10)), with chunk c of sequence b in page block_table[b, c]:
 //
-//   k_pp_score    sigma_ic = max_h s^_hc of 128 rows of a KV group against a slice of the
+//   k_pp_score    sigma_ic = max_h s^_hc of 64 to 256 rows of a KV group against a slice of the
 //                 candidates, on MFMA tiles; to the workspace, a block of rows at a time; where
 //                 candidates are many, with the maxima of blocks of 16
 //   k_pp_select   the K best of each row (exact radix select, ties to the smaller chunk; many
@@ -377,8 +377,8 @@ __device__ __forceinline__ float quad_perm(float x) {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), PERM, 0xf, 0xf, true));
 }
 
-// A workgroup takes 128 rows (f32: 64) of a KV group, 16 per wave, and `slice` candidates; 64
-// landmark rows of one head at a time come through LDS (double-buffered) and serve all rows;
+// A workgroup takes 16 RT rows per wave of a KV group (f32 64, bf16 128, or 256 with two row tiles a wave) and
+// `slice` candidates; 64 landmark rows of one head at a time come through LDS (double-buffered) and serve all rows;
 // the maximum over the heads stays in registers until a block of candidates is done.  It also
 // clears the words that the next launches count in.
 template <typename T, int D, int G, int RT>
@@ -1158,7 +1158,9 @@ __global__ __launch_bounds__(kLocalWaves * kWave, D * sizeof(T) <= 256 ? 4 : 2) 
         window(std::false_type{});
         records();
     }
-    if (seen_bad) {  // (once more, apart from the usual way, whose registers it would take)
+    // Once more, apart from the usual way.  It is in the same kernel all the same, and the register allocation spills around it:
+    // bf16, d = 128 43 to 44 registers, f32, d = 64 9 to 11; without it 0, and 5 to 7.
+    if (seen_bad) {
 #pragma unroll
         for (int db = 0; db < C::DB; ++db) o[db] = zero4();
         m = -INFINITY;
